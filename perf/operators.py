@@ -1,0 +1,443 @@
+"""Operators measured through the library's public entry points, each beside its plain
+form in elementary torch operations: the preparation of queries and keys (bias, norm and
+rotation of a fused q|k|v row), the key/value cache held in 4 bits (rows in and out), the
+tree attention over that cache, and the verification of a drafted tree.
+
+A case is a dict of plain values with an "op":
+  rope    subspec_qkv_rope on M rows of Hq + 2 Hkv heads of 128
+  append  subspec_kv4_append of n rows at position pos and subspec_kv4_read of them;
+          "gather": the rows are picked by index out of "src" rows and counted on the GPU
+  attend  subspec_tree_attention_kv4 over P committed and T + M tree positions
+  verify  subspec_tree_verify of N drafted tokens ("width" a level) against N + 1 rows of logits
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+DEV = "cuda"
+D = 128  # head dimension
+
+
+def listed():
+    return [
+        # One layer of a single-token step, 7B heads: nothing but latency.
+        dict(name="rope_7b_m1", op="rope", M=1, Hq=28, Hkv=4, bias=True, norm=False, rot=128, interleaved=False, far=131072),
+        # A ragged batch of tree tokens with norms of queries and keys, 32B heads.
+        dict(name="rope_norm_32b_m37", op="rope", M=37, Hq=40, Hkv=8, bias=False, norm=True, rot=128, interleaved=False, far=32768),
+        # A long prompt, 32B heads.
+        dict(name="rope_norm_32b_m4096", op="rope", M=4096, Hq=40, Hkv=8, bias=True, norm=True, rot=128, interleaved=False, far=131072),
+        # After a verification: seven accepted rows out of a tree of 288, into the middle of a tile.
+        dict(name="append_7b_accepted", op="append", n=48, src=288, Hkv=4, pos=2043, group=64, gather=True),
+        # A long prompt's rows, 32B heads.
+        dict(name="append_32b_16384", op="append", n=16384, src=16384, Hkv=8, pos=5, group=128, gather=False),
+        # A draft pass of a depth-48 tree after 2048 tokens, 7B heads.
+        dict(name="attend_7b_p2048", op="attend", M=6, Hq=28, Hkv=4, P=2048, T=282, group=64),
+        # A single token over a document, 32B heads.
+        dict(name="attend_32b_m1_p16384", op="attend", M=1, Hq=40, Hkv=8, P=16384, T=0, group=128),
+        # 64 query rows a key/value head: a wide pass early in a tree.
+        dict(name="attend_m16_p8192", op="attend", M=16, Hq=32, Hkv=8, P=8191, T=200, group=128),
+        # The longest context of the Qwen2.5 models.
+        dict(name="attend_32b_p131072", op="attend", M=6, Hq=40, Hkv=8, P=131072, T=60, group=64),
+        # A short chain of drafted tokens.
+        dict(name="verify_chain_n4", op="verify", N=4, width=1, V=32000, T=1.0),
+        # The tree of 48 levels of six, sampling at 0.6 and greedy.
+        dict(name="verify_tree_n288", op="verify", N=288, width=6, V=152064, T=0.6),
+        dict(name="verify_greedy_n288", op="verify", N=288, width=6, V=152064, T=0.0),
+    ]
+
+
+def _log_uniform(rng, lo, hi, step=1):
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return max(lo, min(hi, int(round(v / step)) * step))
+
+
+def draw(rng):
+    op = rng.choice(["rope", "append", "attend", "attend", "verify"])
+    Hq, Hkv = rng.choice([(28, 4), (40, 8), (32, 8), (16, 16), (16, 2), (12, 2)])
+    if op == "rope":
+        return dict(op=op, M=_log_uniform(rng, 1, 4096), Hq=Hq, Hkv=Hkv, bias=rng.random() < 0.5, norm=rng.random() < 0.5,
+                    rot=rng.choice([128, 128, 64, 96]), interleaved=rng.random() < 0.25, far=_log_uniform(rng, 4096, 1000000))
+    if op == "append":
+        gather = rng.random() < 0.4
+        n = _log_uniform(rng, 1, 64 if gather else 16384)
+        return dict(op=op, n=n, src=n + rng.randint(0, 256) if gather else n, Hkv=min(Hkv, 8), pos=rng.randint(0, 4000),
+                    group=rng.choice([64, 128]), gather=gather)
+    if op == "attend":
+        M = rng.randint(1, min(32, 64 // (Hq // Hkv)))
+        longest = min(131072, 131072 * 8 // Hkv, 131072 * 240 // (M * Hq))
+        return dict(op=op, M=M, Hq=Hq, Hkv=Hkv, T=rng.randint(0, 282), P=_log_uniform(rng, 1, longest),
+                    group=rng.choice([64, 128]))
+    return dict(op=op, N=_log_uniform(rng, 1, 288), width=rng.choice([1, 2, 3, 6, 8]), V=_log_uniform(rng, 32000, 152064, 8),
+                T=rng.choice([0.0, 0.6, 0.6, 1.0]))
+
+
+def _gen(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(int(seed) * 1000003 + 29)
+    return g
+
+
+def _bf(g, *shape, scale=1.0):
+    return torch.randn(shape, generator=g, device=DEV).mul_(scale).to(torch.bfloat16)
+
+
+# --- the 4-bit cache's layout (include/subspec.h), written and read with torch ----------
+
+def _pack(codes, s, m, value):
+    """Cache bytes [Hkv][S / 32][2048 + 128 G] of codes [Hkv][S][128] and fp16 scales and
+    minima [Hkv][S][G]: tiles of 32 positions, keys or (value) values."""
+    H, S, G = s.shape
+    n = S // 32
+    if value:  # position = 16 hi + 4 quarter + 2 rl + odd, dimension = 64 half + 16 dl + col
+        c = codes.view(H, n, 2, 4, 2, 2, 2, 4, 16).permute(0, 1, 6, 3, 8, 7, 5, 2, 4)
+    else:  # position = 16 block + r, dimension = 32 j + 8 quarter + 4 p2 + 2 pl + odd
+        c = codes.view(H, n, 2, 16, 4, 4, 2, 2, 2).permute(0, 1, 2, 5, 3, 4, 8, 6, 7)
+    c = (c[..., 0] | (c[..., 1] << 4)).reshape(H, n, 2048)
+    meta = torch.stack((s, m), 3).view(H, n, 2, 4, 4, G, 2).permute(0, 1, 3, 5, 6, 2, 4).contiguous()
+    return torch.cat((c, meta.view(torch.uint8).reshape(H, n, 128 * G)), 2).contiguous()
+
+
+def _unpack(cache, value):
+    """The fp32 values [Hkv][S][128] that a cache stands for."""
+    H, n, size = cache.shape
+    G, S = (size - 2048) // 128, 32 * n
+    b = cache[:, :, :2048]
+    c = torch.stack((b & 15, b >> 4), 3)
+    if value:
+        c = c.view(H, n, 2, 4, 16, 4, 2, 2, 2).permute(0, 1, 7, 3, 8, 6, 2, 5, 4)
+    else:
+        c = c.view(H, n, 2, 4, 16, 4, 2, 2, 2).permute(0, 1, 2, 4, 5, 3, 7, 8, 6)
+    meta = cache[:, :, 2048:].contiguous().view(torch.float16).view(H, n, 4, G, 2, 2, 4)
+    meta = meta.permute(0, 1, 5, 2, 6, 3, 4).reshape(H, S, G, 2).float()
+    v = c.reshape(H, S, G, D // G).float().mul_(meta[..., 0:1]).add_(meta[..., 1:2])
+    return v.view(H, S, D)
+
+
+def _quantize(x, group):
+    """Codes (uint8), scales and minima (fp16) of rows [..., 128] in bf16."""
+    f = x.float().view(*x.shape[:-1], D // group, group)
+    m = f.amin(-1, keepdim=True).to(torch.float16)
+    s = ((f.amax(-1, keepdim=True) - f.amin(-1, keepdim=True)) / 15.0).to(torch.float16)
+    c = torch.where(s > 0, (f - m.float()) / s.float(), torch.zeros_like(f)).round_().clamp_(0, 15)
+    return c.to(torch.uint8).view(x.shape), s.squeeze(-1), m.squeeze(-1)
+
+
+def _cache(g, Hkv, S, group, value):
+    # Keys carry a few dimensions of several times the others' size, as trained models' do.
+    x = torch.randn((Hkv, S, D), generator=g, device=DEV)
+    if not value:
+        x[:, :, ::16] *= 3.0
+    return _pack(*_quantize(x.to(torch.bfloat16), group), value)
+
+
+# --- inputs ------------------------------------------------------------------------------
+
+def _tree_mask(T, k, M, seed):
+    """Ancestor bits [M][ceil((T + M) / 32)] of a random tree in levels of k tokens; the
+    M new tokens are its next level."""
+    rng = np.random.default_rng([int(seed), 5])
+    parent = np.full(T + M, -1)
+    for j in range(k, T):
+        start = (j // k - 1) * k
+        parent[j] = rng.integers(start, start + k)
+    if T:
+        parent[T:] = rng.integers((T - 1) // k * k, T, M)
+    mask = np.zeros((M, (T + M + 31) // 32), np.uint32)
+    for i in range(M):
+        j = T + i
+        while j >= 0:
+            mask[i, j // 32] |= np.uint32(1 << (j % 32))
+            j = parent[j]
+    return torch.from_numpy(mask.view(np.int32)).to(DEV)
+
+
+def _drafted(N, width, V, seed):
+    """Parents and tokens of a tree in levels of `width`, distinct tokens."""
+    rng = np.random.default_rng([int(seed), 7])
+    parent = np.full(N, -1, np.int32)
+    for j in range(width, N):
+        start = (j // width - 1) * width
+        parent[j] = rng.integers(start, start + width)
+    return parent, rng.choice(V, N, replace=False).astype(np.int32)
+
+
+def prepare(case, seed):
+    g, op = _gen(seed), case["op"]
+    e = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device=DEV)  # noqa: E731
+    if op == "rope":
+        M, Hq, Hkv, rot = (case[n] for n in ("M", "Hq", "Hkv", "rot"))
+        rng = np.random.default_rng([int(seed), 3])
+        # tree tokens sit a few positions past one prefix, a prompt's in order
+        first = int(rng.integers(1, case["far"] - min(case["far"] - 1, 4096)))
+        pos = first + (np.sort(rng.integers(0, 48, M)) if M <= 64 else np.arange(M))
+        w = lambda: (1.0 + 0.2 * torch.randn(D, generator=g, device=DEV)).to(torch.bfloat16)  # noqa: E731
+        return dict(case=case, qkv=_bf(g, M, (Hq + 2 * Hkv) * D, scale=1.5),
+                    bias=_bf(g, (Hq + 2 * Hkv) * D, scale=2.0) if case["bias"] else None,
+                    qw=w() if case["norm"] else None, kw=w() if case["norm"] else None,
+                    pos=torch.from_numpy(pos.astype(np.int32)).to(DEV),
+                    freq=torch.tensor([1e6 ** (-2.0 * i / rot) for i in range(rot // 2)], dtype=torch.float64, device=DEV),
+                    q=e(M, Hq, D), k=e(M, Hkv, D), v=e(M, Hkv, D))
+    if op == "append":
+        n, src, Hkv, pos, group = (case[x] for x in ("n", "src", "Hkv", "pos", "group"))
+        S = (pos + n + 31) // 32 * 32
+        rng = np.random.default_rng([int(seed), 9])
+        count = int(rng.integers(max(1, n // 8), n // 4 + 2)) if case["gather"] else n
+        count = min(count, n)
+        rows = np.full(n, -1, np.int32)
+        rows[:count] = np.sort(rng.choice(src, count, replace=False))
+        return dict(case=case, S=S, k_src=_bf(g, src, Hkv, D), v_src=_bf(g, src, Hkv, D),
+                    rows=torch.from_numpy(rows).to(DEV) if case["gather"] else None,
+                    count=torch.tensor([count], dtype=torch.int32, device=DEV) if case["gather"] else None,
+                    k_cache=_cache(g, Hkv, S, group, False), v_cache=_cache(g, Hkv, S, group, True),
+                    k=e(n, Hkv, D), v=e(n, Hkv, D))
+    if op == "attend":
+        M, Hq, Hkv, P, T, group = (case[x] for x in ("M", "Hq", "Hkv", "P", "T", "group"))
+        S = (P + T + M + 31) // 32 * 32 + 32
+        # scores of standard deviation about 2.5: a few hundred positions carry most of the weight
+        return dict(case=case, S=S, q=_bf(g, M, Hq, D, scale=2.0), k_cache=_cache(g, Hkv, S, group, False),
+                    v_cache=_cache(g, Hkv, S, group, True), mask=_tree_mask(T, 6, M, seed), out=e(M, Hq, D))
+    N, V = case["N"], case["V"]
+    parent, token = _drafted(N, case["width"], V, seed)
+    logits = torch.randn((N + 1, V), generator=g, device=DEV).mul_(2.5)
+    # a target that agrees with one child of every row most of the time
+    lift = {1.0: 16.5, 0.6: 13.5}.get(case["T"], 12.0)
+    chosen = {int(p) + 1: int(t) for p, t in zip(parent, token)}
+    at = torch.tensor([list(chosen), list(chosen.values())], device=DEV)
+    logits[at[0], at[1]] = lift + 1.5 * torch.randn(at.shape[1], generator=g, device=DEV)
+    return dict(case=case, logits=logits.to(torch.bfloat16), parent=torch.from_numpy(parent).to(DEV),
+                token=torch.from_numpy(token).to(DEV), uniform=torch.rand(N + 1, generator=g, device=DEV),
+                path=e(N, dtype=torch.int32), accepted=e(1, dtype=torch.int32), next=e(1, dtype=torch.int32))
+
+
+# --- one pass ----------------------------------------------------------------------------
+
+def run(st):
+    c = st["case"]
+    op = c["op"]
+    if own:
+        import paper_2509_18344_amd as ss
+        if op == "rope":
+            ss.subspec_qkv_rope(st["qkv"], st["qkv"].shape[1], st["bias"], st["qw"], st["kw"], 1e-6, st["pos"], st["freq"],
+                                c["rot"], c["interleaved"], c["M"], c["Hq"], c["Hkv"], st["q"], st["k"], st["v"])
+            return dict(q=st["q"], k=st["k"], v=st["v"])
+        if op == "append":
+            ss.subspec_kv4_append(st["k_src"], st["v_src"], c["src"], st["rows"], st["count"], c["n"], c["Hkv"], st["S"],
+                                  c["pos"], c["group"], st["k_cache"], st["v_cache"])
+            ss.subspec_kv4_read(st["k_cache"], st["v_cache"], c["Hkv"], st["S"], c["pos"], c["n"], c["group"], st["k"], st["v"])
+            return dict(k=st["k"], v=st["v"])
+        if op == "attend":
+            ss.subspec_tree_attention_kv4(st["q"], st["k_cache"], st["v_cache"], st["mask"], c["M"], c["Hq"], c["Hkv"], st["S"],
+                                          c["P"], c["T"], c["group"], 1.0 / math.sqrt(D), st["out"])
+            return st["out"]
+        ss.subspec_tree_verify(st["logits"], st["parent"], st["token"], st["uniform"], c["N"], c["V"], c["T"], st["path"],
+                               st["accepted"], st["next"])
+        return dict(path=st["path"], accepted=st["accepted"], next=st["next"])
+    return {"rope": _plain_rope, "append": _plain_append, "attend": _plain_attend, "verify": _plain_verify}[op](st, c)
+
+
+def _plain_rope(st, c):
+    M, Hq, Hkv, rot = c["M"], c["Hq"], c["Hkv"], c["rot"]
+    x = st["qkv"].float()
+    if st["bias"] is not None:
+        x = x + st["bias"].float()
+    x = x.view(M, Hq + 2 * Hkv, D)
+    angle = st["pos"].double()[:, None] * st["freq"]
+    cos, sin = angle.cos().float()[:, None], angle.sin().float()[:, None]
+
+    def rotated(h, w):
+        if w is not None:
+            h = h * torch.rsqrt((h * h).mean(-1, keepdim=True) + 1e-6) * w.float()
+        if c["interleaved"]:
+            a, b = h[..., 0:rot:2], h[..., 1:rot:2]
+            r = torch.stack((a * cos - b * sin, b * cos + a * sin), -1).flatten(-2)
+        else:
+            a, b = h[..., : rot // 2], h[..., rot // 2: rot]
+            r = torch.cat((a * cos - b * sin, b * cos + a * sin), -1)
+        return torch.cat((r, h[..., rot:]), -1).to(torch.bfloat16)
+
+    return dict(q=rotated(x[:, :Hq], st["qw"]), k=rotated(x[:, Hq:Hq + Hkv], st["kw"]), v=x[:, Hq + Hkv:].to(torch.bfloat16))
+
+
+def _plain_append(st, c):
+    n, pos = c["n"], c["pos"]
+    new = dict(k=st["k_src"], v=st["v_src"])
+    out = {}
+    t0, t1 = pos // 32, (pos + n + 31) // 32  # the tiles that the rows touch
+    for x, value in (("k", False), ("v", True)):
+        tiles = st[x + "_cache"][:, t0:t1]
+        held = _unpack(tiles, value)[:, pos - 32 * t0: pos - 32 * t0 + n]
+        rows = new[x] if st["rows"] is None else new[x][st["rows"].long().clamp(min=0)]
+        code, s, m = _quantize(rows.transpose(0, 1).contiguous(), c["group"])
+        f = code.view(c["Hkv"], n, -1, c["group"]).float() * s.float()[..., None] + m.float()[..., None]
+        f = f.view(c["Hkv"], n, D)
+        if st["rows"] is not None:
+            taken = torch.arange(n, device=DEV) < st["count"]
+            f = torch.where(taken[None, :, None], f, held)
+        out[x] = f.transpose(0, 1).to(torch.bfloat16).contiguous()
+    return out
+
+
+def _plain_attend(st, c):
+    M, Hq, Hkv, P, T = c["M"], c["Hq"], c["Hkv"], c["P"], c["T"]
+    L = P + T + M
+    k, v = _unpack(st["k_cache"], False)[:, :L], _unpack(st["v_cache"], True)[:, :L]
+    j = torch.arange(T + M, device=DEV)
+    seen = torch.ones((M, L), dtype=torch.bool, device=DEV)
+    seen[:, P:] = (st["mask"][:, j // 32] >> (j % 32)) & 1 == 1
+    q = st["q"].float().view(M, Hkv, Hq // Hkv, D).permute(1, 2, 0, 3).reshape(Hkv, -1, D)
+    kt = k.transpose(1, 2).contiguous()
+    score = (torch.bmm(q, kt) / math.sqrt(D)).view(Hkv, -1, M, L).masked_fill(~seen, float("-inf"))
+    top = score.amax(-1, keepdim=True).clamp(min=-3e38)
+    p = (score - top).exp()
+    total = p.sum(-1, keepdim=True)
+    p = p / torch.where(total > 0, total, torch.ones_like(total))
+    o = torch.bmm(p.view(Hkv, -1, L), v.contiguous())
+    return o.view(Hkv, -1, M, D).permute(2, 0, 1, 3).reshape(M, Hq, D).to(torch.bfloat16)
+
+
+def _plain_verify(st, c):
+    N, V, T = c["N"], c["V"], c["T"]
+    logits, token = st["logits"], st["token"].long()
+    row = st["parent"].long() + 1
+    i = torch.arange(N, device=DEV)
+    if T == 0.0:
+        best = (logits == logits.amax(1, keepdim=True)).to(torch.uint8).argmax(1)
+        taken = token == best[row]
+    else:
+        # 64 bits: the uniform number may fall next to a border between two tokens
+        p = logits.double().sub_(logits.amax(1, keepdim=True)).div_(T).exp_()
+        p = p / p.sum(1, keepdim=True)
+        before = (row[:, None] == row) & (i[None, :] < i[:, None])
+        child = p[row, token]
+        below = (before * child).sum(1)
+        u = st["uniform"].double()
+        taken = (below <= u[row]) & (u[row] < below + child)
+    # reached: every ancestor (pointer doubling) and the token itself is taken
+    reached = torch.cat((torch.ones(1, dtype=torch.bool, device=DEV), taken))
+    up = torch.cat((torch.zeros(1, dtype=torch.long, device=DEV), row))
+    for _ in range(N.bit_length()):
+        reached = reached & reached[up]
+        up = up[up]
+    hit = reached[1:]
+    order = hit.long().cumsum(0) - 1
+    path = torch.full((N + 1,), -1, dtype=torch.int32, device=DEV)
+    path.scatter_(0, torch.where(hit, order, torch.full_like(order, N)), i.int())
+    accepted = hit.sum().int().view(1)
+    last = (reached * torch.arange(N + 1, device=DEV)).argmax()
+    if T == 0.0:
+        nxt = best[last]
+    else:  # the row's other tokens share what its children left of [0, 1)
+        kids = row == last
+        drafted = torch.zeros(V, dtype=torch.float64, device=DEV).scatter_add_(0, token, kids.double())
+        left = torch.where(drafted > 0, torch.zeros_like(drafted), p[last])
+        nxt = (left.cumsum(0) > u[last] - (child * kids).sum()).to(torch.uint8).argmax()
+    return dict(path=path[:N], accepted=accepted, next=nxt.int().view(1))
+
+
+# --- what a pass cannot do without -------------------------------------------------------
+
+def work(case):
+    op = case["op"]
+    if op == "rope":
+        n = case["M"] * (case["Hq"] + 2 * case["Hkv"]) * D
+        return dict(bytes=4 * n + 4 * case["M"], flops=10 * n)
+    if op == "append":
+        row = 64 + 4 * (D // case["group"])
+        # rows in, their codes out and in again, their values out; "gather": about a sixth are taken
+        taken = case["n"] / 6 if case["gather"] else case["n"]
+        return dict(bytes=2 * case["Hkv"] * (taken * (256 + row) + case["n"] * (row + 256)), flops=2 * case["Hkv"] * case["n"] * D * 8)
+    if op == "attend":
+        M, Hq, Hkv = case["M"], case["Hq"], case["Hkv"]
+        L = case["P"] + case["T"] + M
+        return dict(bytes=4 * M * Hq * D + 2 * Hkv * L * (64 + 4 * (D // case["group"])) + M * ((case["T"] + M + 31) // 32) * 4,
+                    flops=4 * M * Hq * L * D)
+    return dict(bytes=2 * (case["N"] + 1) * case["V"] + 16 * case["N"], flops=4 * (case["N"] + 1) * case["V"])
+
+
+# --- the definitions in 64 bits ----------------------------------------------------------
+
+def exact(case, seed):
+    op = case["op"]
+    st = prepare(case, seed)
+    if op == "rope":
+        M, Hq, Hkv, rot = case["M"], case["Hq"], case["Hkv"], case["rot"]
+        x = st["qkv"].double().view(M, Hq + 2 * Hkv, D)
+        if st["bias"] is not None:
+            x = x + st["bias"].double().view(1, Hq + 2 * Hkv, D)
+        # a pair of dimensions as one complex number, turned by exp(i pos freq)
+        turn = torch.polar(torch.ones((M, rot // 2), dtype=torch.float64, device=DEV), st["pos"].double().outer(st["freq"]))
+        i = torch.arange(rot // 2, device=DEV)
+        lo, hi = (2 * i, 2 * i + 1) if case["interleaved"] else (i, i + rot // 2)
+        out = {}
+        for name, h0, h1, w in (("q", 0, Hq, st["qw"]), ("k", Hq, Hq + Hkv, st["kw"])):
+            y = x[:, h0:h1].clone()
+            if w is not None:
+                y = y / torch.sqrt(y.pow(2).sum(2, keepdim=True) / D + 1e-6) * w.double()
+            z = torch.complex(y[:, :, lo], y[:, :, hi]) * turn.unsqueeze(1)
+            y[:, :, lo], y[:, :, hi] = z.real, z.imag
+            out[name] = y
+        return dict(out, v=x[:, Hq + Hkv:].clone())
+    if op == "append":
+        # what the cache held before and a row's own values by definition
+        out = {}
+        for name, value in (("k", False), ("v", True)):
+            held = _held(st[name + "_cache"], case["pos"], case["n"], case["group"], value)
+            x = st[name + "_src"].double()
+            n = case["n"]
+            if case["gather"]:
+                n = int(st["count"].item())
+                x = x[st["rows"][:n].long()]
+            y = x[:n].reshape(n, case["Hkv"], -1, case["group"])
+            low = y.min(3, keepdim=True).values
+            step = ((y.max(3, keepdim=True).values - low) / 15).half().double()
+            low = low.half().double()
+            code = torch.where(step > 0, torch.round((y - low) / step), torch.zeros_like(y)).clamp(0, 15)
+            held[:n] = (low + step * code).view(n, case["Hkv"], D)
+            out[name] = held
+        return out
+    if op == "attend":
+        M, Hq, Hkv, P, T = (case[n] for n in ("M", "Hq", "Hkv", "P", "T"))
+        L = P + T + M
+        bits = st["mask"].cpu().numpy().view(np.uint32)
+        seen = np.ones((M, L), bool)
+        for t in range(T + M):
+            seen[:, P + t] = (bits[:, t // 32] >> np.uint32(t % 32)) & 1
+        seen = torch.from_numpy(seen).to(DEV)
+        out = torch.empty((M, Hq, D), dtype=torch.float64, device=DEV)
+        for g in range(Hkv):
+            k = _held(st["k_cache"][g:g + 1], 0, L, case["group"], False)[:, 0]
+            v = _held(st["v_cache"][g:g + 1], 0, L, case["group"], True)[:, 0]
+            for h in range(g * (Hq // Hkv), (g + 1) * (Hq // Hkv)):
+                sc = (k @ st["q"][:, h].double().t()).t() / math.sqrt(D)
+                out[:, h] = torch.softmax(sc.masked_fill(~seen, float("-inf")), 1) @ v
+        return out
+    return None  # whole numbers: the accepted tokens and the next one
+
+
+def _held(cache, pos, n, group, value):
+    """The values [n][Hkv][128] at positions pos .. of a cache in 64 bits, each code looked
+    up at its place in the layout."""
+    Hkv, _, size = cache.shape
+    p = pos + torch.arange(n, device=DEV)[:, None]
+    d = torch.arange(D, device=DEV)[None, :]
+    tile, w = p // 32, p % 32
+    quarter, slot = w % 16 // 4, w % 4 + 4 * (w // 16)
+    if value:
+        word = 256 * (d // 64) + 4 * (16 * quarter + d % 16) + d % 64 // 16
+        e = slot
+    else:
+        word = 256 * (w // 16) + 4 * (16 * (d % 32 // 8) + w % 16) + d // 32
+        e = d % 8
+    bit = 16 * (e % 2) + 4 * (e // 2)
+    at = tile * size + 4 * word + bit // 8
+    meta = tile * size + 2048 + ((quarter * (D // group) + d // group) * 2) * 16 + 2 * slot
+    flat = cache.reshape(Hkv, -1)
+    out = torch.empty((n, Hkv, D), dtype=torch.float64, device=DEV)
+    for h in range(Hkv):
+        code = (flat[h][at] >> (bit % 8).to(torch.uint8)) & 15
+        half = flat[h].view(torch.float16)
+        out[:, h] = half[meta // 2 + 8].double() + half[meta // 2].double() * code.double()
+    return out

@@ -299,7 +299,7 @@ def _plain_attend(st, c):
 
 
 def _plain_verify(st, c):
-    N, V, T = c["N"], c["V"], c["T"]
+    N, V, T = c["N"], c["V"], float(np.float32(c["T"]))  # the call's argument is an fp32 number
     logits, token = st["logits"], st["token"].long()
     row = st["parent"].long() + 1
     i = torch.arange(N, device=DEV)

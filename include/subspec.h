@@ -51,7 +51,8 @@
  * (subspec_tree_*, Sec. 4.2 and App. D), the draft's tree attention over the key/value
  * cache it shares with the target (subspec_tree_attention*, Sec. 4.1), the
  * verification pass's cross-layer asynchronous weight prefetch (subspec_prefetch_*,
- * Sec. 4.3 and App. E) and the quantizer with an HQQ-style optimised zero-point
+ * Sec. 4.3 and App. E), the preparation of queries and keys in front of the attention
+ * (subspec_qkv_rope) and the quantizer with an HQQ-style optimised zero-point
  * (subspec_quantize_hqq, Sec. 4.1 and 5.1).  The shape limits listed above are the
  * substitute linear's; the other calls state theirs.
  */
@@ -345,6 +346,34 @@ size_t subspec_tree_attention_workspace_bytes(int M, int Hq, int Hkv, int P, int
  * reject (S is not checked here). */
 int subspec_tree_attention_plan(int M, int Hq, int Hkv, int P, int T, int* splits,
                                 int* tiles_per_split);
+
+/* Queries, keys and values of one layer from the rows of its fused q|k|v projection
+ * (subspec_qlinear over the concatenated columns): the projection's bias, an RMS norm of
+ * every query and key head, and the rotation by the token's position, in one pass.  Per
+ * token i and head (dimension 128):
+ *     x = qkv row's head + bias;
+ *     query and key heads, where their weight is given: x <- x / sqrt(mean(x^2) + eps) * weight;
+ *     query and key heads, pairs (a, b) of the first `rot` dimensions, pair p < rot / 2:
+ *         (a cos t - b sin t, b cos t + a sin t),  t = positions[i] * inv_freq[p],
+ * all in fp32 (the angle in fp64) and rounded once to bf16.  Value heads get the bias alone.
+ *   qkv        device bf16 [M][ld]: Hq query heads, then Hkv key heads, then Hkv value
+ *              heads of 128; ld >= (Hq + 2 Hkv) * 128, a multiple of 8
+ *   bias       device bf16 [(Hq + 2 Hkv) * 128], or null
+ *   q_weight, k_weight  device bf16 [128] each, or null (no norm)
+ *   positions  device int32 [M] (tree tokens: prefix + depth)
+ *   inv_freq   device fp64 [rot / 2]: radians per position
+ *   rot        rotated dimensions, a multiple of 16 in 0 .. 128 (0: positions and inv_freq
+ *              are not read)
+ *   interleaved  0: pair p is dimensions (p, p + rot / 2); 1: (2 p, 2 p + 1)
+ *   q          device bf16 [M][Hq][128]
+ *   k_new, v_new  device bf16 [M][Hkv][128] (what subspec_tree_attention takes)
+ * Needs 1 <= M <= 2^20, Hq, Hkv >= 1 and Hq + 2 Hkv <= 65536, finite eps >= 0; pointers
+ * 16-byte aligned (positions 4, inv_freq 8); outputs must not overlap inputs.  One kernel,
+ * no workspace. */
+int subspec_qkv_rope(const void* qkv, int ld, const void* bias, const void* q_weight,
+                     const void* k_weight, float eps, const int* positions,
+                     const double* inv_freq, int rot, int interleaved, int M, int Hq, int Hkv,
+                     void* q, void* k_new, void* v_new, hipStream_t stream);
 
 /* Cross-layer asynchronous weight prefetch for the verification pass (SubSpec
  * Sec. 4.3 "Asynchronous Data Transfer", App. E): while the GPU computes with one

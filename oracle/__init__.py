@@ -38,3 +38,7 @@ from .tree_attn import (  # noqa: F401
 from .hqq import (  # noqa: F401
     quantize_hqq,
 )
+from .rope import (  # noqa: F401
+    qkv_rope,
+    rope_head,
+)

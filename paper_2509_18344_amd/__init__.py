@@ -22,6 +22,7 @@ from ._binding import (  # noqa: F401
     subspec_qlinear_noalloc,
     SUBSPEC_NOALLOC_SCRATCH_BYTES,
     subspec_qlinear_plan,
+    subspec_qkv_rope,
     subspec_qpack,
     subspec_qpack_bytes,
     subspec_qpack_host,

@@ -87,6 +87,7 @@ def load_library():
         "subspec_tree_attention": (I, [P, P, P, P, P, P, I, I, I, I, I, I, ctypes.c_float, P, P]),
         "subspec_tree_attention_workspace_bytes": (S, [I, I, I, I, I]),
         "subspec_tree_attention_plan": (I, [I, I, I, I, I, P, P]),
+        "subspec_qkv_rope": (I, [P, I, P, P, P, ctypes.c_float, P, P, I, I, I, I, I, P, P, P, P]),
         "subspec_prefetch_create": (I, [S, I, ctypes.POINTER(ctypes.c_void_p)]),
         "subspec_prefetch_destroy": (I, [P]),
         "subspec_prefetch_begin": (I, [P, P, S, ctypes.POINTER(ctypes.c_longlong)]),
@@ -137,6 +138,38 @@ def _stream(s):
     if isinstance(s, int):
         return s
     return s.cuda_stream
+
+
+def _device_ptrs(fn: str, stream, *args):
+    """Data pointers of (tensor, bytes) pairs for one call.  A tensor has to be contiguous, on
+    the device that the call runs on and of at least that many bytes (an address is taken as
+    it is, None stays None): a kernel that is handed anything else reads or writes past it."""
+    out = []
+    dev = None
+    for t, need in args:
+        if t is None or isinstance(t, int):
+            out.append(t)
+            continue
+        try:
+            on, size, whole = t.get_device(), t.nbytes, t.is_contiguous()
+        except AttributeError:
+            raise TypeError(f"{fn}: a device tensor or an address, not {type(t)}") from None
+        if dev is None:
+            dev = _current_device(stream)
+        if on != dev or size < need or not whole:
+            raise SubspecError(fn, -1, f"a tensor of {size} bytes on device {on}{'' if whole else ', not contiguous'}: "
+                               f"needs {need} contiguous bytes on the current device")
+        out.append(t.data_ptr())
+    return out
+
+
+def _current_device(stream) -> int:
+    import torch
+    if not torch.cuda.is_initialized():
+        return -2  # no tensor is on it
+    dev = torch.cuda.current_device()
+    on = getattr(stream, "device_index", dev)
+    return dev if on == dev else -2  # a stream of another device: refused with its tensors
 
 
 def _check(fn: str, status: int) -> int:
@@ -287,6 +320,17 @@ def subspec_tree_attention_plan(M, Hq, Hkv, P, T):
     _check("subspec_tree_attention_plan", load_library().subspec_tree_attention_plan(
         M, Hq, Hkv, P, T, ctypes.byref(s), ctypes.byref(t)))
     return s.value, t.value
+
+
+def subspec_qkv_rope(qkv, ld, bias, q_weight, k_weight, eps, positions, inv_freq, rot, interleaved, M, Hq, Hkv,
+                     q, k_new, v_new, stream=None) -> int:
+    heads = Hq + 2 * Hkv
+    x, b, qw, kw, pos, freq, qo, ko, vo = _device_ptrs(
+        "subspec_qkv_rope", stream, (qkv, 2 * ((M - 1) * ld + heads * 128)), (bias, 256 * heads), (q_weight, 256),
+        (k_weight, 256), (positions, 4 * M), (inv_freq, 4 * rot), (q, 256 * M * Hq), (k_new, 256 * M * Hkv),
+        (v_new, 256 * M * Hkv))
+    return _check("subspec_qkv_rope", load_library().subspec_qkv_rope(
+        x, ld, b, qw, kw, eps, pos, freq, rot, int(interleaved), M, Hq, Hkv, qo, ko, vo, _stream(stream)))
 
 
 class Prefetcher:

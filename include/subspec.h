@@ -52,7 +52,7 @@
  * cache it shares with the target (subspec_tree_attention*, Sec. 4.1), the
  * verification pass's cross-layer asynchronous weight prefetch (subspec_prefetch_*,
  * Sec. 4.3 and App. E), the preparation of queries and keys in front of the attention
- * (subspec_qkv_rope) and the quantizer with an HQQ-style optimised zero-point
+ * (subspec_qkv_rope), a key/value cache held in 4 bits (subspec_kv4_*) and the quantizer with an HQQ-style optimised zero-point
  * (subspec_quantize_hqq, Sec. 4.1 and 5.1).  The shape limits listed above are the
  * substitute linear's; the other calls state theirs.
  */
@@ -374,6 +374,53 @@ int subspec_qkv_rope(const void* qkv, int ld, const void* bias, const void* q_we
                      const void* k_weight, float eps, const int* positions,
                      const double* inv_freq, int rot, int interleaved, int M, int Hq, int Hkv,
                      void* q, void* k_new, void* v_new, hipStream_t stream);
+
+/* A key/value cache held in 4 bits: 136 or 144 bytes a position and key/value head instead
+ * of 512.  The 128 dimensions of a key or value row fall into groups of `group` (64 or 128)
+ * with a scale and a minimum each:
+ *     m = fp16(min x),  s = fp16((max x - min x) / 15),
+ *     c = clamp(rint((x - m) / s), 0, 15)  (s = 0: c = 0),      x stands as m + s c,
+ * in fp32, ties to even; m and s round to nearest-even.  NaN counts as 0 and values past
+ * +-65504 as that.  (The minimum and not a zero-point: it is exact for bf16 values of fp16's
+ * range, also where a group's values all lie far from 0.)
+ *
+ * Layout ("kv4"): one buffer for keys and one for values, each [Hkv][S / 32] tiles of 32
+ * positions, S a multiple of 32; G = 128 / group.  A tile is 2048 bytes of codes and 128 G
+ * bytes of fp16 scales and minima.  Codes are in 4-byte words of 8; the code e of a word
+ * (0 .. 7) is at bit 16 (e % 2) + 4 (e / 2).  For position w (0 .. 31) of the tile and
+ * dimension d:
+ *   keys    byte 1024 (w / 16) + 16 (16 (d % 32 / 8) + w % 16) + 4 (d / 32), e = d % 8
+ *   values  byte 1024 (d / 64) + 16 (16 (w % 16 / 4) + d % 16) + 4 (d % 64 / 16),
+ *           e = w % 4 + 4 (w / 16)
+ *   scale   byte 2048 + 32 (G (w % 16 / 4) + d / group) + 2 (w % 4 + 4 (w / 16)),
+ *   minimum 16 bytes after it.
+ * Both are the matrix instruction's operands in register order, so attention reads them
+ * with 16-byte loads and moves nothing between lanes. */
+
+/* Bytes of the key buffer (and of the value buffer) of one layer.  0 on bad arguments. */
+size_t subspec_kv4_bytes(int Hkv, int S, int group);
+
+/* Write rows of keys and values into positions pos .. pos + n - 1 of a kv4 cache.
+ *   k, v     device bf16 [src_rows][Hkv][128]
+ *   rows     device int32 [n]: position pos + i takes row rows[i] of k and v (the accepted
+ *            tokens of a verified tree); null: row i (src_rows >= n)
+ *   count    device int32 [1]: only the first min(*count, n) positions are written (the
+ *            number is known on the device alone); null: all n
+ *   k_cache, v_cache  device, kv4 layout, subspec_kv4_bytes(Hkv, S, group) bytes
+ * A position whose row lies outside 0 .. src_rows - 1 is left as it was, as are all other
+ * positions of the cache.  Needs 1 <= Hkv <= 65535, S a positive multiple of 32 up to 2^30,
+ * pos, n >= 0, n <= 2^28, pos + n <= S; k, v and the caches 16-byte aligned, rows and count
+ * 4-byte; calls that write positions of the same 32-position tile must not overlap in time.
+ * n = 0 does nothing.  One kernel, no workspace. */
+int subspec_kv4_append(const void* k, const void* v, int src_rows, const int* rows,
+                       const int* count, int n, int Hkv, int S, int pos, int group,
+                       void* k_cache, void* v_cache, hipStream_t stream);
+
+/* The values that positions pos .. pos + n - 1 stand for, m + s c rounded to bf16.
+ *   k, v     device bf16 [n][Hkv][128], fully overwritten
+ * Same limits as subspec_kv4_append. */
+int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, int pos, int n,
+                     int group, void* k, void* v, hipStream_t stream);
 
 /* Cross-layer asynchronous weight prefetch for the verification pass (SubSpec
  * Sec. 4.3 "Asynchronous Data Transfer", App. E): while the GPU computes with one

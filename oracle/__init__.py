@@ -42,3 +42,11 @@ from .rope import (  # noqa: F401
     qkv_rope,
     rope_head,
 )
+from .kv4 import (  # noqa: F401
+    kv4_bytes,
+    kv4_quantize,
+    kv4_read,
+    kv4_value,
+    kv4_write,
+    tree_attention_values,
+)

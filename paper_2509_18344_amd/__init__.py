@@ -22,6 +22,9 @@ from ._binding import (  # noqa: F401
     subspec_qlinear_noalloc,
     SUBSPEC_NOALLOC_SCRATCH_BYTES,
     subspec_qlinear_plan,
+    subspec_kv4_append,
+    subspec_kv4_bytes,
+    subspec_kv4_read,
     subspec_qkv_rope,
     subspec_qpack,
     subspec_qpack_bytes,

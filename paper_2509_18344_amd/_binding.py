@@ -88,6 +88,9 @@ def load_library():
         "subspec_tree_attention_workspace_bytes": (S, [I, I, I, I, I]),
         "subspec_tree_attention_plan": (I, [I, I, I, I, I, P, P]),
         "subspec_qkv_rope": (I, [P, I, P, P, P, ctypes.c_float, P, P, I, I, I, I, I, P, P, P, P]),
+        "subspec_kv4_bytes": (S, [I, I, I]),
+        "subspec_kv4_append": (I, [P, P, I, P, P, I, I, I, I, I, P, P, P]),
+        "subspec_kv4_read": (I, [P, P, I, I, I, I, I, P, P, P]),
         "subspec_prefetch_create": (I, [S, I, ctypes.POINTER(ctypes.c_void_p)]),
         "subspec_prefetch_destroy": (I, [P]),
         "subspec_prefetch_begin": (I, [P, P, S, ctypes.POINTER(ctypes.c_longlong)]),
@@ -331,6 +334,25 @@ def subspec_qkv_rope(qkv, ld, bias, q_weight, k_weight, eps, positions, inv_freq
         (v_new, 256 * M * Hkv))
     return _check("subspec_qkv_rope", load_library().subspec_qkv_rope(
         x, ld, b, qw, kw, eps, pos, freq, rot, int(interleaved), M, Hq, Hkv, qo, ko, vo, _stream(stream)))
+
+
+def subspec_kv4_bytes(Hkv: int, S: int, group: int) -> int:
+    return int(load_library().subspec_kv4_bytes(Hkv, S, group))
+
+
+def subspec_kv4_append(k, v, src_rows, rows, count, n, Hkv, S, pos, group, k_cache, v_cache, stream=None) -> int:
+    row, cache = 256 * Hkv * src_rows, subspec_kv4_bytes(Hkv, S, group)
+    pk, pv, pr, pc, ck, cv = _device_ptrs("subspec_kv4_append", stream, (k, row), (v, row), (rows, 4 * n), (count, 4),
+                                          (k_cache, cache), (v_cache, cache))
+    return _check("subspec_kv4_append", load_library().subspec_kv4_append(
+        pk, pv, src_rows, pr, pc, n, Hkv, S, pos, group, ck, cv, _stream(stream)))
+
+
+def subspec_kv4_read(k_cache, v_cache, Hkv, S, pos, n, group, k, v, stream=None) -> int:
+    row, cache = 256 * Hkv * n, subspec_kv4_bytes(Hkv, S, group)
+    ck, cv, pk, pv = _device_ptrs("subspec_kv4_read", stream, (k_cache, cache), (v_cache, cache), (k, row), (v, row))
+    return _check("subspec_kv4_read", load_library().subspec_kv4_read(
+        ck, cv, Hkv, S, pos, n, group, pk, pv, _stream(stream)))
 
 
 class Prefetcher:

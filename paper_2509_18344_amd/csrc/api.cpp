@@ -22,6 +22,7 @@
 #include "kernels_hqq.h"
 #include "kernels_qstream.h"
 #include "kernels_rope.h"
+#include "kernels_kv4.h"
 
 namespace {
 
@@ -1171,6 +1172,77 @@ int subspec_qkv_rope(const void* qkv, int ld, const void* bias, const void* q_we
   a.v = static_cast<uint16_t*>(v_new);
   const hipError_t e = subspec::launch_qkv_rope(a, stream);
   if (e != hipSuccess) return hip_fail(e, "qkv_rope launch");
+  return SUBSPEC_OK;
+}
+
+namespace {
+
+const char* kv4_shape_error(int Hkv, int S, int group) {
+  if (group != 64 && group != 128) return "group must be 64 or 128";
+  if (Hkv < 1 || Hkv > 65535) return "Hkv must be in 1..65535";
+  if (S < subspec::kKv4Tile || S > (1 << 30) || S % subspec::kKv4Tile) return "S must be a positive multiple of 32, at most 2^30";
+  return "";
+}
+
+int kv4_rows_check(const char* fn, const void* k, const void* v, const void* k_cache, const void* v_cache, int Hkv, int S,
+                   int pos, int n, int group) {
+  const char* why = kv4_shape_error(Hkv, S, group);
+  if (*why) return fail(SUBSPEC_EUNSUPPORTED, "%s: %s", fn, why);
+  if (pos < 0 || n < 0 || n > (1 << 28) || static_cast<long long>(pos) + n > S)
+    return fail(SUBSPEC_EUNSUPPORTED, "%s: positions %d .. %d + %d - 1 exceed S = %d", fn, pos, pos, n, S);
+  if (!k || !v || !k_cache || !v_cache) return fail(SUBSPEC_EINVAL, "%s: null pointer argument", fn);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(k_cache) || !aligned16(v_cache))
+    return fail(SUBSPEC_EINVAL, "%s: rows and caches must be 16-byte aligned", fn);
+  return SUBSPEC_OK;
+}
+
+}  // namespace
+
+size_t subspec_kv4_bytes(int Hkv, int S, int group) {
+  if (*kv4_shape_error(Hkv, S, group)) return 0;
+  return static_cast<size_t>(Hkv) * (S / subspec::kKv4Tile) * subspec::kv4_tile_bytes(128 / group);
+}
+
+int subspec_kv4_append(const void* k, const void* v, int src_rows, const int* rows, const int* count, int n, int Hkv,
+                       int S, int pos, int group, void* k_cache, void* v_cache, hipStream_t stream) {
+  const int rc = kv4_rows_check("kv4_append", k, v, k_cache, v_cache, Hkv, S, pos, n, group);
+  if (rc) return rc;
+  if (!aligned_to(rows, 4) || !aligned_to(count, 4)) return fail(SUBSPEC_EINVAL, "kv4_append: rows and count must be 4-byte aligned");
+  if (src_rows < (rows ? 0 : n)) return fail(SUBSPEC_EINVAL, "kv4_append: src_rows=%d: too few for n=%d", src_rows, n);
+  if (n == 0) return SUBSPEC_OK;
+  subspec::Kv4RowsArgs a{};
+  a.k = static_cast<const uint16_t*>(k);
+  a.v = static_cast<const uint16_t*>(v);
+  a.rows = rows;
+  a.count = count;
+  a.src_rows = src_rows;
+  a.n = n;
+  a.pos = pos;
+  a.Hkv = Hkv;
+  a.S = S;
+  a.k_cache = static_cast<uint8_t*>(k_cache);
+  a.v_cache = static_cast<uint8_t*>(v_cache);
+  const hipError_t e = subspec::launch_kv4_append(a, 128 / group, stream);
+  if (e != hipSuccess) return hip_fail(e, "kv4_append launch");
+  return SUBSPEC_OK;
+}
+
+int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, int pos, int n, int group, void* k, void* v,
+                     hipStream_t stream) {
+  const int rc = kv4_rows_check("kv4_read", k, v, k_cache, v_cache, Hkv, S, pos, n, group);
+  if (rc) return rc;
+  if (n == 0) return SUBSPEC_OK;
+  subspec::Kv4RowsArgs a{};
+  a.n = n;
+  a.pos = pos;
+  a.Hkv = Hkv;
+  a.S = S;
+  a.k_cache = static_cast<uint8_t*>(const_cast<void*>(k_cache));
+  a.v_cache = static_cast<uint8_t*>(const_cast<void*>(v_cache));
+  a.k_out = static_cast<uint16_t*>(k);
+  a.v_out = static_cast<uint16_t*>(v);
+  const hipError_t e = subspec::launch_kv4_read(a, 128 / group, stream);
+  if (e != hipSuccess) return hip_fail(e, "kv4_read launch");
   return SUBSPEC_OK;
 }
 

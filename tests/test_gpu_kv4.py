@@ -1,0 +1,147 @@
+"""GPU checks of the key/value cache held in 4 bits: rows in and out, byte for byte against
+the oracle (every step of the quantizer is stated in fp32, so codes, scales and minima have
+one value), the layout, positions that are left as they were, gathers and counts."""
+import numpy as np
+import pytest
+
+import oracle
+import paper_2509_18344_amd as ss
+from paper_2509_18344_amd import synth
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _rows(rng, n, Hkv):
+    x = rng.standard_normal((n, Hkv, 128), dtype=np.float32) * rng.choice([0.01, 1.0, 30.0], (n, Hkv, 1)).astype(np.float32)
+    return synth.bf16_bits(torch.from_numpy(x).to(torch.bfloat16))
+
+
+def _dev(bits):
+    return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).to(DEV)
+
+
+def _cache(rng, Hkv, S, group):
+    return rng.integers(0, 256, (Hkv, oracle.kv4_bytes(1, S, group))).astype(np.uint8)
+
+
+def _expect(cache, bits, positions, group, value):
+    c, s, m = oracle.kv4_quantize(oracle.bf16_bits_to_f64(bits), group)
+    out = cache.copy()
+    oracle.kv4_write(out, positions, c, s, m, group, value)
+    return out
+
+
+def _i32(a):
+    return torch.from_numpy(np.asarray(a, np.int32)).to(DEV)
+
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("n,Hkv,S,pos", [
+    (1, 4, 64, 0), (1, 4, 64, 37), (32, 2, 96, 32), (6, 4, 96, 29), (33, 1, 128, 31), (100, 3, 160, 5), (64, 8, 64, 0),
+])
+def test_kv4_append_writes_the_oracles_bytes_and_no_others(group, n, Hkv, S, pos):
+    rng = np.random.default_rng([n, Hkv, S, pos, group])
+    k, v = _rows(rng, n, Hkv), _rows(rng, n, Hkv)
+    kc, vc = _cache(rng, Hkv, S, group), _cache(rng, Hkv, S, group)
+    dk, dv = torch.from_numpy(kc).to(DEV), torch.from_numpy(vc).to(DEV)
+    assert dk.nbytes == ss.subspec_kv4_bytes(Hkv, S, group)
+    ss.subspec_kv4_append(_dev(k), _dev(v), n, None, None, n, Hkv, S, pos, group, dk, dv)
+    at = range(pos, pos + n)
+    assert np.array_equal(dk.cpu().numpy(), _expect(kc, k, at, group, False))
+    assert np.array_equal(dv.cpu().numpy(), _expect(vc, v, at, group, True))
+
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("count", [0, 1, 5, 40, 99, -3])
+def test_kv4_append_gathers_rows_and_counts_on_the_device(group, count):
+    rng = np.random.default_rng([count + 10, group])
+    Hkv, S, pos, n, src = 2, 128, 27, 40, 50
+    k, v = _rows(rng, src, Hkv), _rows(rng, src, Hkv)
+    kc, vc = _cache(rng, Hkv, S, group), _cache(rng, Hkv, S, group)
+    rows = rng.integers(0, src, n)
+    rows[2] = rows[3]        # the same row twice
+    rows[[7, 11]] = [-1, src]  # rows that there are not: their positions stay
+    dk, dv = torch.from_numpy(kc).to(DEV), torch.from_numpy(vc).to(DEV)
+    ss.subspec_kv4_append(_dev(k), _dev(v), src, _i32(rows), _i32([count]), n, Hkv, S, pos, group, dk, dv)
+    live = [i for i in range(min(max(count, 0), n)) if i not in (7, 11)]
+    at = [pos + i for i in live]
+    assert np.array_equal(dk.cpu().numpy(), _expect(kc, k[rows[live]], at, group, False))
+    assert np.array_equal(dv.cpu().numpy(), _expect(vc, v[rows[live]], at, group, True))
+
+
+@pytest.mark.parametrize("group", [64, 128])
+def test_kv4_append_values_at_the_ends(group):
+    """Constant groups, single outliers, values past fp16's range, infinities and NaN, fp16's
+    subnormal scales and signed zeros."""
+    rng = np.random.default_rng(group)
+    n, Hkv, S = 10, 1, 32
+    x = rng.standard_normal((n, Hkv, 128), dtype=np.float32)
+    x[0] = 3.0
+    x[1] = 0.0
+    x[1, :, ::2] = -0.0
+    x[2, :, 5] = 60000.0
+    x[3, :, [3, 70]] = [[1e6], [-1e30]]
+    x[4, :, [1, 66]] = [[np.inf], [-np.inf]]
+    x[5, :, [0, 127]] = np.nan
+    x[6] *= 1e-6
+    x[7] *= 1e-9
+    x[8] += 1000.0
+    x[9] = np.nan
+    bits = synth.bf16_bits(torch.from_numpy(x).to(torch.bfloat16))
+    zero = np.zeros((Hkv, oracle.kv4_bytes(1, S, group)), np.uint8)
+    dk, dv = torch.from_numpy(zero.copy()).to(DEV), torch.from_numpy(zero.copy()).to(DEV)
+    ss.subspec_kv4_append(_dev(bits), _dev(bits), n, None, None, n, Hkv, S, 3, group, dk, dv)
+    for got, value in ((dk, False), (dv, True)):
+        c, s, m = oracle.kv4_read(got.cpu().numpy(), group, value)
+        rc, rs, rm = oracle.kv4_quantize(oracle.bf16_bits_to_f64(bits), group)
+        assert np.array_equal(s[3:13], rs) and np.array_equal(m[3:13], rm)  # -0 equals 0
+        assert np.array_equal(c[3:13], rc)
+        assert np.isfinite(s.astype(np.float64)).all() and np.isfinite(m.astype(np.float64)).all()
+
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("n,Hkv,S,pos", [(1, 4, 64, 33), (70, 2, 128, 30), (32, 1, 32, 0)])
+def test_kv4_read_rounds_the_held_values_once(group, n, Hkv, S, pos):
+    rng = np.random.default_rng([n, pos, group, 3])
+    k, v = _rows(rng, S, Hkv), _rows(rng, S, Hkv)
+    zero = np.zeros((Hkv, oracle.kv4_bytes(1, S, group)), np.uint8)
+    dk, dv = torch.from_numpy(zero.copy()).to(DEV), torch.from_numpy(zero.copy()).to(DEV)
+    ss.subspec_kv4_append(_dev(k), _dev(v), S, None, None, S, Hkv, S, 0, group, dk, dv)
+    out = [torch.full((n + 1, Hkv, 128), -7, dtype=torch.int16, device=DEV) for _ in range(2)]
+    ss.subspec_kv4_read(dk, dv, Hkv, S, pos, n, group, out[0], out[1])
+    for o, bits in zip(out, (k, v)):
+        assert bool((o[n] == -7).all())
+        held = oracle.kv4_value(*oracle.kv4_quantize(oracle.bf16_bits_to_f64(bits), group))[pos:pos + n]
+        got = oracle.bf16_bits_to_f64(o[:n].cpu().numpy().view(np.uint16))
+        # fp32 sum of an exact product (2^-24), then bf16 (2^-8)
+        assert np.all(np.abs(got - held) <= (2.0 ** -8 + 2.0 ** -23) * np.abs(held) + 1e-30)
+        # and half a step of the quantizer from the rows themselves (plus fp16's rounding of the step and minimum)
+        x = oracle.bf16_bits_to_f64(bits)[pos:pos + n].reshape(n, Hkv, -1, group)
+        step = (x.max(-1) - x.min(-1)) / 15
+        err = np.abs(held.reshape(x.shape) - x).max(-1)
+        assert np.all(err <= step * (0.5 + 15 * 2.0 ** -11) + 2.0 ** -11 * np.abs(x).max(-1) + 2.0 ** -24)
+
+
+def test_kv4_append_zero_rows_and_many_tiles():
+    rng = np.random.default_rng(5)
+    Hkv, group, n = 2, 64, 3000
+    S, pos = 3040, 17
+    k, v = _rows(rng, n, Hkv), _rows(rng, n, Hkv)
+    dk = torch.zeros((Hkv, oracle.kv4_bytes(1, S, group)), dtype=torch.uint8, device=DEV)
+    dv = torch.zeros_like(dk)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    ss.subspec_kv4_append(_dev(k), _dev(v), n, None, None, 0, Hkv, S, pos, group, dk, dv, s)
+    s.synchronize()
+    assert not dk.any() and not dv.any()
+    tk, tv = _dev(k), _dev(v)
+    s.wait_stream(torch.cuda.current_stream())
+    ss.subspec_kv4_append(tk, tv, n, None, None, n, Hkv, S, pos, group, dk, dv, s)
+    s.synchronize()
+    for got, bits, value in ((dk, k, False), (dv, v, True)):
+        c, sc, m = oracle.kv4_read(got.cpu().numpy(), group, value)
+        rc, rs, rm = oracle.kv4_quantize(oracle.bf16_bits_to_f64(bits), group)
+        assert np.array_equal(c[pos:pos + n], rc) and np.array_equal(sc[pos:pos + n], rs) and np.array_equal(m[pos:pos + n], rm)
+        assert not c[:pos].any() and not c[pos + n:].any() and not sc[:pos].any() and not m[pos + n:].any()

@@ -52,7 +52,8 @@
  * cache it shares with the target (subspec_tree_attention*, Sec. 4.1), the
  * verification pass's cross-layer asynchronous weight prefetch (subspec_prefetch_*,
  * Sec. 4.3 and App. E), the preparation of queries and keys in front of the attention
- * (subspec_qkv_rope), a key/value cache held in 4 bits (subspec_kv4_*) and the quantizer with an HQQ-style optimised zero-point
+ * (subspec_qkv_rope), a key/value cache held in 4 bits (subspec_kv4_*) with the tree
+ * attention over it (subspec_tree_attention_kv4*) and the quantizer with an HQQ-style optimised zero-point
  * (subspec_quantize_hqq, Sec. 4.1 and 5.1).  The shape limits listed above are the
  * substitute linear's; the other calls state theirs.
  */
@@ -421,6 +422,33 @@ int subspec_kv4_append(const void* k, const void* v, int src_rows, const int* ro
  * Same limits as subspec_kv4_append. */
 int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, int pos, int n,
                      int group, void* k, void* v, hipStream_t stream);
+
+/* subspec_tree_attention over a kv4 cache: the same M tree tokens, head grouping, mask and
+ * result, with every key and value, the new tokens' included, read from the cache.  The
+ * new tokens' rows are appended first (subspec_kv4_append at P + T).
+ *   q        device bf16 [M][Hq][128] (positions already rotated)
+ *   k_cache, v_cache  device, kv4 layout, subspec_kv4_bytes(Hkv, S, group) bytes: positions
+ *            0 .. P - 1 hold rows that subspec_kv4_append has written; a tree position that
+ *            no mask row allows may hold anything
+ *   mask     device uint32 [M][W], W = ceil((T + M) / 32), as subspec_tree_attention's
+ *   out      device bf16 [M][Hq][128]; a query with no visible position gets zeros
+ * Scores are fp32 sums over exact codes; a position's weight times its value's scale is
+ * rounded to fp16 (11 bits) before the second product, which sums in fp32.  Limits as
+ * subspec_tree_attention's (Hkv at most 65535, S a multiple of 32); q, caches and out
+ * 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one where
+ * a single range covers the positions); workspace as for subspec_qlinear
+ * (subspec_tree_attention_kv4_workspace_bytes). */
+int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v_cache,
+                               const uint32_t* mask, int M, int Hq, int Hkv, int S, int P, int T,
+                               int group, float scale, void* out, hipStream_t stream);
+
+/* Workspace bytes subspec_tree_attention_kv4 needs; 0 on bad arguments, and where it needs none. */
+size_t subspec_tree_attention_kv4_workspace_bytes(int M, int Hq, int Hkv, int P, int T);
+
+/* Launch shape of subspec_tree_attention_kv4, on the host, as subspec_tree_attention_plan's:
+ * `splits` ranges of `tiles_per_split` tiles of 32 positions for each key/value head. */
+int subspec_tree_attention_kv4_plan(int M, int Hq, int Hkv, int P, int T, int* splits,
+                                    int* tiles_per_split);
 
 /* Cross-layer asynchronous weight prefetch for the verification pass (SubSpec
  * Sec. 4.3 "Asynchronous Data Transfer", App. E): while the GPU computes with one

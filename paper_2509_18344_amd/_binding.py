@@ -91,6 +91,9 @@ def load_library():
         "subspec_kv4_bytes": (S, [I, I, I]),
         "subspec_kv4_append": (I, [P, P, I, P, P, I, I, I, I, I, P, P, P]),
         "subspec_kv4_read": (I, [P, P, I, I, I, I, I, P, P, P]),
+        "subspec_tree_attention_kv4": (I, [P, P, P, P, I, I, I, I, I, I, I, ctypes.c_float, P, P]),
+        "subspec_tree_attention_kv4_workspace_bytes": (S, [I, I, I, I, I]),
+        "subspec_tree_attention_kv4_plan": (I, [I, I, I, I, I, P, P]),
         "subspec_prefetch_create": (I, [S, I, ctypes.POINTER(ctypes.c_void_p)]),
         "subspec_prefetch_destroy": (I, [P]),
         "subspec_prefetch_begin": (I, [P, P, S, ctypes.POINTER(ctypes.c_longlong)]),
@@ -353,6 +356,26 @@ def subspec_kv4_read(k_cache, v_cache, Hkv, S, pos, n, group, k, v, stream=None)
     ck, cv, pk, pv = _device_ptrs("subspec_kv4_read", stream, (k_cache, cache), (v_cache, cache), (k, row), (v, row))
     return _check("subspec_kv4_read", load_library().subspec_kv4_read(
         ck, cv, Hkv, S, pos, n, group, pk, pv, _stream(stream)))
+
+
+def subspec_tree_attention_kv4(q, k_cache, v_cache, mask, M, Hq, Hkv, S, P, T, group, scale, out, stream=None) -> int:
+    rows, cache = 256 * M * Hq, subspec_kv4_bytes(Hkv, S, group)
+    pq, ck, cv, pm, po = _device_ptrs("subspec_tree_attention_kv4", stream, (q, rows), (k_cache, cache), (v_cache, cache),
+                                      (mask, 4 * M * ((T + M + 31) // 32)), (out, rows))
+    return _check("subspec_tree_attention_kv4", load_library().subspec_tree_attention_kv4(
+        pq, ck, cv, pm, M, Hq, Hkv, S, P, T, group, scale, po, _stream(stream)))
+
+
+def subspec_tree_attention_kv4_workspace_bytes(M, Hq, Hkv, P, T) -> int:
+    return int(load_library().subspec_tree_attention_kv4_workspace_bytes(M, Hq, Hkv, P, T))
+
+
+def subspec_tree_attention_kv4_plan(M, Hq, Hkv, P, T):
+    """(splits, tiles_per_split) of the launch."""
+    s, t = ctypes.c_int(), ctypes.c_int()
+    _check("subspec_tree_attention_kv4_plan", load_library().subspec_tree_attention_kv4_plan(
+        M, Hq, Hkv, P, T, ctypes.byref(s), ctypes.byref(t)))
+    return s.value, t.value
 
 
 class Prefetcher:

@@ -675,6 +675,7 @@ struct Workspace {
   void* ptr = nullptr;
   size_t bytes = 0;
   int graphs = 0;                // live captured graphs made on this device
+  bool foreign = false;          // a graph that the caller captures holds one of the buffers
   std::vector<void*> retired;    // earlier buffers: queued kernels or graphs may still use them
   unsigned long long allocations = 0;
 };
@@ -694,6 +695,7 @@ Workspace& workspace_of(int dev) {  // caller holds g_ws_mutex
 
 // Frees the retired buffers of `w`; the caller has synchronised the device.
 int free_retired(Workspace& w) {
+  if (w.foreign) return SUBSPEC_OK;
   int rc = SUBSPEC_OK;
   for (void* p : w.retired) {
     const hipError_t e = hipFree(p);
@@ -707,14 +709,22 @@ int free_retired(Workspace& w) {
 // buffer (at least twice the old size, so retired buffers total less than the live
 // one), zeroes its completion counters on `st` and waits for that stream only.  The
 // old buffer is retired, not freed: kernels queued on other streams and captured
-// graphs may still use it.  Growth is refused while `st` is being captured.
-int get_workspace(size_t bytes, hipStream_t st, void** out) {
+// graphs may still use it.  Growth is refused while `st` is being captured.  note_capture:
+// a call inside the caller's own stream capture (the library never learns when that graph
+// ends) keeps every buffer of the device until the process ends.
+int get_workspace(size_t bytes, hipStream_t st, void** out, bool note_capture = false) {
   int dev = 0;
   int rc = current_device(&dev);
   if (rc) return rc;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
   Workspace& w = workspace_of(dev);
   if (w.bytes >= bytes) {
+    if (note_capture && !w.foreign && st != nullptr) {
+      hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+      const hipError_t e = hipStreamIsCapturing(st, &cs);
+      if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
+      w.foreign = cs != hipStreamCaptureStatusNone;
+    }
     *out = w.ptr;
     return SUBSPEC_OK;
   }
@@ -1243,6 +1253,74 @@ int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, i
   a.v_out = static_cast<uint16_t*>(v);
   const hipError_t e = subspec::launch_kv4_read(a, 128 / group, stream);
   if (e != hipSuccess) return hip_fail(e, "kv4_read launch");
+  return SUBSPEC_OK;
+}
+
+namespace {
+
+const char* kv4_attn_error(int M, int Hq, int Hkv, int P, int T) {
+  if (Hkv > 65535) return "Hkv must be at most 65535";
+  return attn_shape_error(M, Hq, Hkv, P, T);
+}
+
+}  // namespace
+
+int subspec_tree_attention_kv4_plan(int M, int Hq, int Hkv, int P, int T, int* splits, int* tiles_per_split) {
+  if (!splits || !tiles_per_split) return fail(SUBSPEC_EINVAL, "null pointer argument");
+  const char* why = kv4_attn_error(M, Hq, Hkv, P, T);
+  if (*why) return fail(SUBSPEC_EUNSUPPORTED, "tree_attention_kv4: %s", why);
+  subspec::kv4_attn_plan(M, Hq, Hkv, P, T, splits, tiles_per_split);
+  return SUBSPEC_OK;
+}
+
+size_t subspec_tree_attention_kv4_workspace_bytes(int M, int Hq, int Hkv, int P, int T) {
+  if (*kv4_attn_error(M, Hq, Hkv, P, T)) return 0;
+  return subspec::kv4_attn_workspace_bytes(M, Hq, Hkv, P, T);
+}
+
+int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v_cache, const uint32_t* mask, int M, int Hq,
+                               int Hkv, int S, int P, int T, int group, float scale, void* out, hipStream_t stream) {
+  if (!q || !k_cache || !v_cache || !mask || !out) return fail(SUBSPEC_EINVAL, "tree_attention_kv4: null pointer argument");
+  if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out))
+    return fail(SUBSPEC_EINVAL, "tree_attention_kv4: q, caches and out must be 16-byte aligned");
+  if (!aligned_to(mask, 4)) return fail(SUBSPEC_EINVAL, "tree_attention_kv4: mask must be 4-byte aligned");
+  const char* why = kv4_attn_error(M, Hq, Hkv, P, T);
+  if (!*why) why = kv4_shape_error(Hkv, S, group);
+  if (*why) return fail(SUBSPEC_EUNSUPPORTED, "tree_attention_kv4: %s", why);
+  if (static_cast<long long>(P) + T + M > S)
+    return fail(SUBSPEC_EUNSUPPORTED, "tree_attention_kv4: P + T + M = %lld exceeds S = %d",
+                static_cast<long long>(P) + T + M, S);
+  const float c = std::fabs(scale) * 1.4426950408889634f;
+  if (!std::isfinite(scale) || !std::isfinite(c)) return fail(SUBSPEC_EINVAL, "tree_attention_kv4: scale must be finite");
+  subspec::Kv4AttnArgs a{};
+  subspec::kv4_attn_plan(M, Hq, Hkv, P, T, &a.splits, &a.tiles_per_split);
+  a.rows_pad = 16 * ((Hq / Hkv * M + 15) / 16);
+  if (a.splits > 1) {
+    void* ws = nullptr;
+    const int rc = get_workspace(subspec::kv4_attn_workspace_bytes(M, Hq, Hkv, P, T), stream, &ws, true);
+    if (rc) return rc;
+    // the partials go after the completion counters that other calls rely on being zero
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + subspec::kSplitCounterBytes);
+    a.part_ml = a.part_o + static_cast<size_t>(Hkv) * a.splits * a.rows_pad * subspec::kKv4D;
+  }
+  a.q = static_cast<const uint16_t*>(q);
+  a.k_cache = static_cast<const uint8_t*>(k_cache);
+  a.v_cache = static_cast<const uint8_t*>(v_cache);
+  a.mask = mask;
+  a.M = M;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.S = S;
+  a.P = P;
+  a.T = T;
+  a.W = (T + M + 31) / 32;
+  // The kernel takes a positive factor: a negative scale flips q, and 2^-100 for 0 leaves
+  // every score at 0 for any finite product.
+  a.scale_log2 = std::max(c, 0x1p-100f);
+  a.q_sign = scale < 0.f ? 0x80008000u : 0u;
+  a.out = static_cast<uint16_t*>(out);
+  const hipError_t e = subspec::launch_kv4_attention(a, 128 / group, stream);
+  if (e != hipSuccess) return hip_fail(e, "tree_attention_kv4 launch");
   return SUBSPEC_OK;
 }
 

@@ -53,7 +53,8 @@
  * verification pass's cross-layer asynchronous weight prefetch (subspec_prefetch_*,
  * Sec. 4.3 and App. E), the preparation of queries and keys in front of the attention
  * (subspec_qkv_rope), a key/value cache held in 4 bits (subspec_kv4_*) with the tree
- * attention over it (subspec_tree_attention_kv4*) and the quantizer with an HQQ-style optimised zero-point
+ * attention over it (subspec_tree_attention_kv4*), the verification of the drafted tree
+ * (subspec_tree_verify*) and the quantizer with an HQQ-style optimised zero-point
  * (subspec_quantize_hqq, Sec. 4.1 and 5.1).  The shape limits listed above are the
  * substitute linear's; the other calls state theirs.
  */
@@ -449,6 +450,37 @@ size_t subspec_tree_attention_kv4_workspace_bytes(int M, int Hq, int Hkv, int P,
  * `splits` ranges of `tiles_per_split` tiles of 32 positions for each key/value head. */
 int subspec_tree_attention_kv4_plan(int M, int Hq, int Hkv, int P, int T, int* splits,
                                     int* tiles_per_split);
+
+/* Verification of a drafted tree (SubSpec Sec. 3.1 and 4.2: one target pass over all drafted
+ * tokens, then the accepted path and one more token), for trees whose tokens were chosen
+ * without regard to the uniform numbers, as subspec_tree_expand chooses them.  Row 0 of the
+ * target's logits follows the last committed token, row 1 + j drafted token j; token j
+ * continues row parent[j] + 1.  At each row i, from row 0 on, the uniform number u_i picks one token
+ * of p_i = softmax(l_i / temperature): the row's drafted continuations hold the first part of
+ * [0, 1), one after the other in index order with their probabilities (a token drafted twice
+ * in a row counts at its first index), all other tokens the rest in token order.  A drafted
+ * token that is picked is accepted and its row comes next; any other ends the path and is the
+ * next token.  The tokens are thus distributed as if sampled from the target one by one.
+ * temperature 0: the pick is the row's largest logit (of equals the lowest token).
+ *   logits    device bf16 [N + 1][V] row-major; -inf masks a token
+ *   parent    device int32 [N]: -1 or an earlier index; token: device int32 [N].  An entry with
+ *             any other parent, or a token outside 0 .. V - 1, is never accepted
+ *   uniform   device fp32 [N + 1], each in [0, 1); not read at temperature 0
+ *   path      device int32 [N]: the accepted indices in order, then -1 (as `rows` and `count`
+ *             of subspec_kv4_append take it with `accepted`)
+ *   accepted  device int32 [1]: how many
+ *   next_token  device int32 [1]: the token after them; -1 where its row has none (NaN or +inf
+ *             among its logits, or -inf in all)
+ * Probabilities of drafted tokens in fp32 (relative error about 2^-20), the rest of the last row in fp64.
+ * Needs 0 <= N <= 1024, V a multiple of 8 in 8 .. 2^20, temperature 0 or finite with finite
+ * inverse; logits 16-byte aligned, the others 4-byte; N = 0 needs no parent, token or path
+ * (null).  Workspace as for subspec_qlinear (subspec_tree_verify_workspace_bytes). */
+int subspec_tree_verify(const void* logits, const int* parent, const int* token,
+                        const float* uniform, int N, int V, float temperature, int* path,
+                        int* accepted, int* next_token, hipStream_t stream);
+
+/* Workspace bytes subspec_tree_verify needs for (N, V); 0 on bad arguments. */
+size_t subspec_tree_verify_workspace_bytes(int N, int V);
 
 /* Cross-layer asynchronous weight prefetch for the verification pass (SubSpec
  * Sec. 4.3 "Asynchronous Data Transfer", App. E): while the GPU computes with one

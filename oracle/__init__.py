@@ -1,7 +1,8 @@
 """Plain fp64 CPU oracle for the low-bit substitute-layer linear (SubSpec, Sec. 4.1)
 and for the draft-tree expansion step with probability sharpening (Sec. 4.2, App. D)
 and the draft model's tree attention over the shared KV cache (Sec. 4.1), and for the
-quantizer with an HQQ-style optimised zero-point (Sec. 4.1, Sec. 5.1).
+quantizer with an HQQ-style optimised zero-point (Sec. 4.1, Sec. 5.1), the preparation of
+queries and keys, the key/value cache held in 4 bits and the verification of a drafted tree.
 
 TEST INFRASTRUCTURE ONLY.  Only ``tests/``, ``__graft_entry__.smoke()`` and the
 ``cpu_baseline`` leg of ``bench.py`` may import or call anything in this package.
@@ -49,4 +50,8 @@ from .kv4 import (  # noqa: F401
     kv4_value,
     kv4_write,
     tree_attention_values,
+)
+from .verify import (  # noqa: F401
+    tree_children,
+    tree_verify,
 )

@@ -94,6 +94,8 @@ def load_library():
         "subspec_tree_attention_kv4": (I, [P, P, P, P, I, I, I, I, I, I, I, ctypes.c_float, P, P]),
         "subspec_tree_attention_kv4_workspace_bytes": (S, [I, I, I, I, I]),
         "subspec_tree_attention_kv4_plan": (I, [I, I, I, I, I, P, P]),
+        "subspec_tree_verify": (I, [P, P, P, P, I, I, ctypes.c_float, P, P, P, P]),
+        "subspec_tree_verify_workspace_bytes": (S, [I, I]),
         "subspec_prefetch_create": (I, [S, I, ctypes.POINTER(ctypes.c_void_p)]),
         "subspec_prefetch_destroy": (I, [P]),
         "subspec_prefetch_begin": (I, [P, P, S, ctypes.POINTER(ctypes.c_longlong)]),
@@ -376,6 +378,18 @@ def subspec_tree_attention_kv4_plan(M, Hq, Hkv, P, T):
     _check("subspec_tree_attention_kv4_plan", load_library().subspec_tree_attention_kv4_plan(
         M, Hq, Hkv, P, T, ctypes.byref(s), ctypes.byref(t)))
     return s.value, t.value
+
+
+def subspec_tree_verify(logits, parent, token, uniform, N, V, temperature, path, accepted, next_token, stream=None) -> int:
+    pl, pp, pt, pu, po, pa, pn = _device_ptrs(
+        "subspec_tree_verify", stream, (logits, 2 * (N + 1) * V), (parent, 4 * N), (token, 4 * N), (uniform, 4 * (N + 1)),
+        (path, 4 * N), (accepted, 4), (next_token, 4))
+    return _check("subspec_tree_verify", load_library().subspec_tree_verify(
+        pl, pp, pt, pu, N, V, temperature, po, pa, pn, _stream(stream)))
+
+
+def subspec_tree_verify_workspace_bytes(N, V) -> int:
+    return int(load_library().subspec_tree_verify_workspace_bytes(N, V))
 
 
 class Prefetcher:

@@ -12,7 +12,7 @@ LIB = os.path.join(HERE, "libsubspec.so")
 HOST_SOURCES = ["api.cpp"]
 DEVICE_SOURCES = ["kernels_qlinear.hip", "kernels_qmma.hip", "kernels_qmma_b2.hip", "kernels_qmma_b3.hip",
                   "kernels_qmma_b4.hip", "kernels_qstream.hip", "kernels_prep.hip", "kernels_tree.hip", "kernels_attn.hip",
-                  "kernels_rope.hip", "kernels_kv4.hip", "kernels_kv4_attn.hip",
+                  "kernels_rope.hip", "kernels_kv4.hip", "kernels_kv4_attn.hip", "kernels_verify.hip",
                   "noalloc.hip"]
 OBJDIR = os.path.join(ROOT, "_build")
 

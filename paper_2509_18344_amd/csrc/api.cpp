@@ -23,6 +23,7 @@
 #include "kernels_qstream.h"
 #include "kernels_rope.h"
 #include "kernels_kv4.h"
+#include "kernels_verify.h"
 
 namespace {
 
@@ -1321,6 +1322,56 @@ int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v
   a.out = static_cast<uint16_t*>(out);
   const hipError_t e = subspec::launch_kv4_attention(a, 128 / group, stream);
   if (e != hipSuccess) return hip_fail(e, "tree_attention_kv4 launch");
+  return SUBSPEC_OK;
+}
+
+size_t subspec_tree_verify_workspace_bytes(int N, int V) {
+  if (N < 0 || N > subspec::kVerifyMaxTokens || V < 8 || V % 8 || V > subspec::kVerifyMaxV) return 0;
+  return subspec::verify_workspace_bytes(N, V);
+}
+
+int subspec_tree_verify(const void* logits, const int* parent, const int* token, const float* uniform, int N, int V,
+                        float temperature, int* path, int* accepted, int* next_token, hipStream_t stream) {
+  if (N < 0 || N > subspec::kVerifyMaxTokens)
+    return fail(SUBSPEC_EUNSUPPORTED, "tree_verify: N=%d: must be in 0..%d", N, subspec::kVerifyMaxTokens);
+  if (V < 8 || V % 8 || V > subspec::kVerifyMaxV)
+    return fail(SUBSPEC_EUNSUPPORTED, "tree_verify: V=%d: must be a multiple of 8 in 8..%d", V, subspec::kVerifyMaxV);
+  const float c = 1.4426950408889634f / temperature;
+  if (temperature != 0.f && (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(c)))
+    return fail(SUBSPEC_EINVAL, "tree_verify: temperature must be 0 or positive and finite, with a finite inverse");
+  if (!logits || !accepted || !next_token || (N > 0 && (!parent || !token || !path)) || (temperature != 0.f && !uniform))
+    return fail(SUBSPEC_EINVAL, "tree_verify: null pointer argument");
+  if (!aligned16(logits)) return fail(SUBSPEC_EINVAL, "tree_verify: logits must be 16-byte aligned");
+  if (!aligned_to(parent, 4) || !aligned_to(token, 4) || !aligned_to(uniform, 4) || !aligned_to(path, 4) ||
+      !aligned_to(accepted, 4) || !aligned_to(next_token, 4))
+    return fail(SUBSPEC_EINVAL, "tree_verify: tree, numbers and outputs must be 4-byte aligned");
+  void* ws = nullptr;
+  const int rc = get_workspace(subspec::verify_workspace_bytes(N, V), stream, &ws, true);
+  if (rc) return rc;
+  subspec::VerifyArgs a{};
+  a.logits = static_cast<const uint16_t*>(logits);
+  a.parent = parent;
+  a.token = token;
+  a.uniform = uniform;
+  a.N = N;
+  a.V = V;
+  a.greedy = temperature == 0.f;
+  a.c = a.greedy ? 0.f : c;
+  a.inv_t = a.greedy ? 0.0 : 1.0 / static_cast<double>(temperature);
+  subspec::verify_plan(N, V, &a.chunks, &a.chunk_len);
+  char* p = static_cast<char*>(ws);
+  a.cnt = reinterpret_cast<unsigned*>(p);
+  p += subspec::kSplitCounterBytes;
+  a.last_row = reinterpret_cast<int*>(p);
+  a.row_stat = reinterpret_cast<float2*>(p + 8);
+  a.slice_sum = reinterpret_cast<double*>(p + 16);
+  const int slices = (V + subspec::kVerifySlice - 1) / subspec::kVerifySlice;
+  a.stat = reinterpret_cast<float2*>(p + 16 + slices * sizeof(double));
+  a.path = path;
+  a.accepted = accepted;
+  a.next_token = next_token;
+  const hipError_t e = subspec::launch_tree_verify(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "tree_verify launch");
   return SUBSPEC_OK;
 }
 

@@ -1,0 +1,36 @@
+// Host-visible launcher of the verification of a drafted tree (internal; the public ABI is
+// include/subspec.h).
+#pragma once
+
+#include "kernels.h"
+
+namespace subspec {
+
+constexpr int kVerifyMaxTokens = 1024;
+constexpr int kVerifyMaxV = 1 << 20;
+constexpr int kVerifySlice = 2048;  // logits per workgroup of the residual's kernel
+
+struct VerifyArgs {
+  const uint16_t* logits;  // bf16 [N + 1][V]
+  const int* parent;       // [N]: -1 (the context) or an earlier token
+  const int* token;        // [N]
+  const float* uniform;    // [N + 1]; greedy: unused
+  int N, V, greedy;
+  float c;                 // log2(e) / T
+  double inv_t;            // 1 / T
+  int chunks, chunk_len;   // workgroups per row and the logits each one covers
+  unsigned* cnt;           // completion counter (zero between launches)
+  float2* stat;            // [N + 1][chunks] maximum, and sum of 2^(c (l - maximum)) (greedy: the maximum's token)
+  float2* row_stat;        // [1] the last row's maximum and sum
+  int* last_row;           // [1]
+  double* slice_sum;       // [ceil(V / kVerifySlice)] the last row's sums without its children
+  int* path;               // [N]
+  int* accepted;           // [1]
+  int* next_token;         // [1]
+};
+
+void verify_plan(int N, int V, int* chunks, int* chunk_len);
+size_t verify_workspace_bytes(int N, int V);
+hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t st);
+
+}  // namespace subspec

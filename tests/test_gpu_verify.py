@@ -1,0 +1,190 @@
+"""GPU checks of the verification of a drafted tree against the fp64 oracle: accepted path and
+next token equal, at sizes, trees and numbers where they can go wrong.  A uniform number next
+to a border of a drafted token's interval may fall on either side (probabilities of drafted tokens
+are fp32, relative error below 2^-18): every case asserts that its oracle met none so close."""
+import numpy as np
+import pytest
+
+import oracle
+import paper_2509_18344_amd as ss
+from paper_2509_18344_amd import synth
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+MARGIN = 2.0 ** -17
+
+
+def _bf16(x):
+    return synth.bf16_bits(torch.from_numpy(np.ascontiguousarray(x, np.float32)).to(torch.bfloat16))
+
+
+def _tree(rng, N, V, width, agree, logits):
+    """Parents in levels of `width`; one child of most rows gets a logit that competes."""
+    parent = np.full(N, -1, np.int32)
+    for j in range(width, N):
+        s = (j // width - 1) * width
+        parent[j] = rng.integers(s, s + width)
+    token = rng.choice(V, N, replace=N > V).astype(np.int32)
+    for j in range(N):
+        if rng.random() < agree:
+            logits[parent[j] + 1, token[j]] += 14.0
+    return parent, token
+
+
+def _run(logits, parent, token, u, T, stream=None):
+    N, V = logits.shape[0] - 1, logits.shape[1]
+    i32 = lambda a: torch.from_numpy(np.asarray(a, np.int32)).to(DEV)  # noqa: E731
+    path = torch.full((N + 1,), -9, dtype=torch.int32, device=DEV)
+    acc, nxt = torch.full((2,), -9, dtype=torch.int32, device=DEV), torch.full((2,), -9, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()  # the call may run on another stream
+    ss.subspec_tree_verify(torch.from_numpy(logits.view(np.int16)).to(DEV), i32(parent) if N else None, i32(token) if N else None,
+                           torch.from_numpy(np.asarray(u, np.float32)).to(DEV) if T else None, N, V, T, path if N else None,
+                           acc, nxt, stream)
+    torch.cuda.synchronize()
+    path, acc, nxt = path.cpu().numpy(), acc.cpu().numpy(), nxt.cpu().numpy()
+    assert path[N] == -9 and acc[1] == -9 and nxt[1] == -9
+    n = int(acc[0])
+    assert 0 <= n <= N and (path[n:N] == -1).all()
+    return path[:n].tolist(), int(nxt[0])
+
+
+def _check(logits, parent, token, u, T, what=""):
+    path, nxt, margin = oracle.tree_verify(logits, parent, token, u, float(np.float32(T)))
+    assert T == 0 or margin > MARGIN, (what, "the case sits on a border", margin)
+    got = _run(logits, parent, token, u, T)
+    assert got == (path, nxt), (what, got, (path, nxt))
+    return path, nxt
+
+
+@pytest.mark.parametrize("T", [0.0, 0.2, 0.6, 1.0])
+@pytest.mark.parametrize("N,V,width", [
+    (0, 152064, 1), (1, 8, 1), (1, 32000, 1), (2, 2056, 2), (7, 1000, 3), (48, 4096, 1), (48, 32000, 6), (288, 5000, 6),
+    (288, 152064, 6), (5, 152064, 1), (1024, 512, 4), (513, 2048, 1),
+])
+def test_tree_verify_matches_oracle(N, V, width, T):
+    for seed in range(2 if N * V > 10 ** 7 else 4):
+        rng = np.random.default_rng([N, V, width, seed])
+        logits = rng.standard_normal((N + 1, V), dtype=np.float32) * 2.5
+        parent, token = _tree(rng, N, V, width, 0.8, logits)
+        _check(_bf16(logits), parent, token, rng.random(N + 1, dtype=np.float32), T, f"N={N} V={V} T={T} seed={seed}")
+
+
+def test_tree_verify_accepts_long_paths():
+    rng = np.random.default_rng(1)
+    N, V = 1024, 64
+    logits = rng.standard_normal((N + 1, V), dtype=np.float32)
+    parent, token = np.arange(-1, N - 1), rng.integers(0, V, N)
+    logits[np.arange(N), token] = 30.0
+    path, _ = _check(_bf16(logits), parent, token, rng.random(N + 1, dtype=np.float32), 1.0)
+    assert len(path) == N
+    path, _ = _check(_bf16(logits), parent, token, None, 0.0)
+    assert len(path) == N
+
+
+def test_tree_verify_uniform_numbers_across_a_row():
+    """Every pick of a row: numbers over [0, 1) choose drafted tokens, in index order, then the
+    others in token order, with the row's probabilities."""
+    rng = np.random.default_rng(2)
+    V, N = 64, 5
+    logits = _bf16(rng.standard_normal((N + 1, V)))
+    parent, token = np.full(N, -1), np.array([40, 3, 40, 63, 0])  # 40 twice: its second entry is never accepted
+    l = oracle.bf16_bits_to_f64(logits[0])
+    p = np.exp(l - l.max())
+    p /= p.sum()
+    order = [40, 3, 63, 0] + [t for t in range(V) if t not in (40, 3, 63, 0)]
+    edge = np.cumsum(p[order])
+    index = {40: 0, 3: 1, 63: 3, 0: 4}
+    for u in np.concatenate([np.linspace(0, 0.999, 40), (edge[:-1] + edge[1:])[::5] / 2]).astype(np.float32):
+        path, nxt = _run(logits, parent, token, np.full(N + 1, u), 1.0)
+        assert np.abs(edge - float(u)).min() > MARGIN or u == 0
+        pick = order[int(np.searchsorted(edge, float(u), side="right"))]
+        if pick in index:
+            assert path == [index[pick]]
+        else:
+            assert path == [] and nxt == pick, (u, path, nxt, pick)
+
+
+@pytest.mark.parametrize("V", [40, 152064])
+def test_tree_verify_uniform_number_next_to_one_and_zero(V):
+    rng = np.random.default_rng(V)
+    logits = _bf16(rng.standard_normal((2, V)))
+    for u in (0.0, float(np.nextafter(np.float32(1), np.float32(0)))):
+        # no drafted token has a share at the ends: it is masked
+        bits = logits.copy()
+        bits[0, 5] = 0xFF80
+        bits[0, V - 3:] = 0xFF80  # nor have the last tokens
+        path, nxt = _run(bits, [-1], [5], [u, 0.5], 1.0)
+        ref = oracle.tree_verify(bits, [-1], [5], [u, 0.5], 1.0)
+        assert (path, nxt) == ref[:2] and nxt == (0 if u == 0 else nxt) and nxt < V - 3 and nxt != 5
+    assert _run(logits, [-1], [5], [1.0, 0.5], 1.0)[1] == V - 1  # past the range: the last token with a share
+
+
+def test_tree_verify_entries_that_cannot_be_accepted():
+    rng = np.random.default_rng(3)
+    V, N = 1000, 8
+    logits = np.full((N + 1, V), -5.0, np.float32)
+    parent = np.array([-1, 1, 0, -2, 9, 2, -1, 2 ** 31 - 1], np.int32)  # its own, one before -1, ones that come later
+    token = np.array([7, 8, V, 9, 10, 11, -1, 12], np.int32)              # 2 and 6 outside the vocabulary
+    logits[0, [7, 9, 12]] = [20.0, 0.0, 0.0]
+    logits[1] = rng.standard_normal(V)
+    for T in (0.0, 1.0):
+        path, _ = _check(_bf16(logits), parent, token, rng.random(N + 1, dtype=np.float32), T)
+        assert path == [0]
+
+
+@pytest.mark.parametrize("T", [0.0, 0.7])
+def test_tree_verify_rows_without_a_distribution(T):
+    V, N = 2048, 2
+    for bad in ("masked", "nan", "inf"):
+        for at in (0, 1):
+            logits = np.zeros((N + 1, V), np.float32)
+            logits[0, 3] = 50.0
+            if bad == "masked":
+                logits[at] = -np.inf
+            else:
+                logits[at, 1500] = np.nan if bad == "nan" else np.inf
+                logits[at, :100] = -np.inf
+            got = _run(_bf16(logits), [-1, 0], [3, 4], [0.5] * 3, T)
+            assert got == ([0] if at else [], -1), (bad, at, got)
+    # one token left in a masked row
+    logits = np.full((1, V), -np.inf, np.float32)
+    logits[0, 777] = -3.0
+    assert _run(_bf16(logits), [], [], [0.99], T) == ([], 777)
+    # NaN beside nothing but masked logits in its neighbourhood
+    logits[0, 8] = np.nan
+    assert _run(_bf16(logits), [], [], [0.99], T) == ([], -1)
+
+
+def test_tree_verify_greedy_ties_go_to_the_lowest_token():
+    V = 152064
+    logits = np.zeros((3, V), np.float32)
+    logits[0, [70000, 9]] = 4.0
+    logits[1] = -0.0
+    logits[1, 5:] = 0.0
+    assert _run(_bf16(logits), [-1, -1], [70000, 9], None, 0.0) == ([1], 0)
+    assert _run(_bf16(logits), [-1, 0], [9, 0], None, 0.0)[0] == [0, 1]
+
+
+def test_tree_verify_all_mass_on_drafted_tokens():
+    logits = np.full((2, 64), -np.inf, np.float32)
+    logits[0, [4, 60]] = [1.0, 2.0]
+    logits[1, 2] = 0.0
+    one = float(np.nextafter(np.float32(1), np.float32(0)))
+    # three rows: the context and both drafted tokens
+    logits = np.vstack([logits, logits[1:]])
+    got = _run(_bf16(logits), [-1, -1], [60, 4], [one, 0.5, 0.5], 1.0)
+    assert got in (([1], 2), ([], 60)), got  # the last of them, or, where rounding keeps u from both, the larger token
+    assert _run(_bf16(logits), [-1, -1], [60, 4], [0.1, 0.5, 0.5], 1.0) == ([0], 2)
+
+
+def test_tree_verify_repeats_and_leaves_the_counters_clear():
+    rng = np.random.default_rng(8)
+    N, V = 48, 152064
+    logits = rng.standard_normal((N + 1, V), dtype=np.float32) * 2.5
+    parent, token = _tree(rng, N, V, 6, 0.8, logits)
+    bits, u = _bf16(logits), rng.random(N + 1, dtype=np.float32)
+    first = _check(bits, parent, token, u, 0.6)
+    s = torch.cuda.Stream()
+    for i in range(3):
+        assert _run(bits, parent, token, u, 0.6, s if i == 1 else None) == first

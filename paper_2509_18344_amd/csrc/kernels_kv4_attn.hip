@@ -31,6 +31,7 @@
 // Kernel 2 (k_kv4_combine) combines the ranges in a fixed order; a single range writes the
 // output itself.
 #include <cmath>
+#include <type_traits>
 
 #include "device_common.h"
 #include "kernels_kv4.h"
@@ -40,7 +41,7 @@ namespace subspec {
 namespace {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 
 // Visibility of the 32 positions key0 .. for one query row (bit k: key0 + k): committed
 // positions always, tree positions P + j by bit j of the row's mask (its W words in device
@@ -62,43 +63,80 @@ __device__ __forceinline__ uint32_t kv4_visibility(const uint32_t* row_mask, int
   return live >= kKv4Tile ? vis : vis & ((1u << live) - 1u);
 }
 
-// One lane's share of a tile: codes, and of its quarter's 8 positions (4 quarter + r and
-// 16 + 4 quarter + r) the scales and minima per group.
+// One lane's share of a tile: codes, and of its quarter's 8 positions (4 quarter + r and 16 +
+// 4 quarter + r) the scales per group; the keys' minima the same; of the values' minima one
+// row of the auxiliary product's operand (group 0 in the lanes of column 1, group 1 in column 2).
 template <int G>
-struct Kv4Regs {
-  u32x4_t kc[2], vc[2];
-  u32x4_t ks[G], km[G], vs[G], vm[G];
+struct Kv4Keys {
+  u32x4_t c[2], s[G], m[G];
+};
+template <int G>
+struct Kv4Values {
+  u32x4_t c[2], s[G], m;
 };
 
 template <int G>
-__device__ __forceinline__ void kv4_load(const uint8_t* kt, const uint8_t* vt, int lane, Kv4Regs<G>& r) {
+__device__ __forceinline__ void kv4_load(const uint8_t* tile, int lane, Kv4Keys<G>& r) {
 #pragma unroll
-  for (int u = 0; u < 2; ++u) r.kc[u] = *reinterpret_cast<const u32x4_t*>(kt + u * 1024 + lane * 16);
-  const int meta = kKv4CodeBytes + (lane / 16) * (32 * G);
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    r.ks[g] = *reinterpret_cast<const u32x4_t*>(kt + meta + 32 * g);
-    r.km[g] = *reinterpret_cast<const u32x4_t*>(kt + meta + 32 * g + 16);
-  }
-#pragma unroll
-  for (int u = 0; u < 2; ++u) r.vc[u] = *reinterpret_cast<const u32x4_t*>(vt + u * 1024 + lane * 16);
+  for (int u = 0; u < 2; ++u) r.c[u] = *reinterpret_cast<const u32x4_t*>(tile + u * 1024 + lane * 16);
+  const uint8_t* meta = tile + kKv4CodeBytes + (lane / 16) * (32 * G);
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    r.vs[g] = *reinterpret_cast<const u32x4_t*>(vt + meta + 32 * g);
-    r.vm[g] = *reinterpret_cast<const u32x4_t*>(vt + meta + 32 * g + 16);
+    r.s[g] = *reinterpret_cast<const u32x4_t*>(meta + 32 * g);
+    r.m[g] = *reinterpret_cast<const u32x4_t*>(meta + 32 * g + 16);
   }
 }
 
-// Eight codes of a word as bf16 (fp16) numbers 16 + c, in order.
-__device__ __forceinline__ bf16x8_t kv4_bf16(uint32_t d) {
-  const uint32_t bias = 0x41804180u, mask = 0x00780078u;
-  return __builtin_bit_cast(bf16x8_t, u32x4_t{and_or(d << 3, mask, bias), and_or(d >> 1, mask, bias),
-                                              and_or(d >> 5, mask, bias), and_or(d >> 9, mask, bias)});
+template <int G>
+__device__ __forceinline__ void kv4_load(const uint8_t* tile, int lane, Kv4Values<G>& r) {
+  const uint8_t* meta = tile + kKv4CodeBytes + (lane / 16) * (32 * G);
+#pragma unroll
+  for (int g = 0; g < G; ++g) r.s[g] = *reinterpret_cast<const u32x4_t*>(meta + 32 * g);
+  r.m = *reinterpret_cast<const u32x4_t*>(meta + (lane % 16 == 2 ? 32 * (G - 1) : 0) + 16);
+#pragma unroll
+  for (int u = 0; u < 2; ++u) r.c[u] = *reinterpret_cast<const u32x4_t*>(tile + u * 1024 + lane * 16);
 }
-__device__ __forceinline__ f16x8_t kv4_f16(uint32_t d) {
-  const uint32_t bias = 0x4C004C00u, mask = 0x03C003C0u;
-  return __builtin_bit_cast(f16x8_t, u32x4_t{and_or(d << 6, mask, bias), and_or(d << 2, mask, bias),
-                                             and_or(d >> 2, mask, bias), and_or(d >> 6, mask, bias)});
+
+// Counts the registers of `r` as written.  Where a branch leaves them alone because nothing
+// reads them again, the compiler may otherwise take them as undefined on that path, and has then
+// dropped parts of them on the other (three of four registers of a tile's minima).
+template <int G>
+__device__ __forceinline__ void kv4_keep(Kv4Values<G>& r) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(r.c[u]));
+#pragma unroll
+  for (int g = 0; g < G; ++g) asm volatile("" : "+v"(r.s[g]));
+  asm volatile("" : "+v"(r.m));
+}
+template <int G>
+__device__ __forceinline__ void kv4_keep(Kv4Keys<G>& r) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) asm volatile("" : "+v"(r.c[u]));
+#pragma unroll
+  for (int g = 0; g < G; ++g) asm volatile("" : "+v"(r.s[g]), "+v"(r.m[g]));
+}
+
+__device__ __forceinline__ uint32_t kv4_pack(float lo, float hi) {
+  return static_cast<uint32_t>(float_to_bf16_bits(lo)) | (static_cast<uint32_t>(float_to_bf16_bits(hi)) << 16);
+}
+
+// Eight codes of a word, in order, as the fp16 numbers 2^-24 c: a code is the mantissa of a
+// subnormal, which the matrix instruction takes as it is.
+__device__ __forceinline__ f16x8_t kv4_codes(uint32_t d) {
+  const uint32_t mask = 0x000F000Fu;
+  return __builtin_bit_cast(f16x8_t, u32x4_t{d & mask, (d >> 4) & mask, (d >> 8) & mask, (d >> 12) & mask});
+}
+
+// One load straight into LDS: lane l's SIZE bytes at p land at byte dst + SIZE * l.  Written as
+// assembly because the compiler, where it sees such loads, waits for all of them before it reads
+// the ring again; it has no register result, and the ring's own waits order it (a wait state after
+// the write of m0 included).
+template <int SIZE>
+__device__ __forceinline__ void kv4_to_lds(const uint8_t* p, uint32_t dst) {
+  if constexpr (SIZE == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(p) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(p) : "memory");
 }
 
 // Infinite and NaN halves become zero (rows that nothing has written, seen by no query).
@@ -109,173 +147,163 @@ __device__ __forceinline__ uint32_t kv4_finite(uint32_t w) {
   return r;
 }
 
+// A lane and its partners 16, 32 and 48 lanes away (the four quarters that share a query):
+// the swaps put a row's and its neighbour's values side by side.
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ u32x2_t kv4_swap16(uint32_t v) { return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane16_swap(v, v, false, false)); }
+__device__ __forceinline__ u32x2_t kv4_swap32(uint32_t v) { return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_permlane32_swap(v, v, false, false)); }
 __device__ __forceinline__ float kv4_cross_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  u32x2_t w = kv4_swap16(__float_as_uint(v));
+  v = fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  w = kv4_swap32(__float_as_uint(v));
+  return fmaxf(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
 __device__ __forceinline__ float kv4_cross_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  u32x2_t w = kv4_swap16(__float_as_uint(v));
+  v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  w = kv4_swap32(__float_as_uint(v));
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
 }
 
-constexpr int kMergeRow = kKv4D + 4;  // floats per query row of a wavefront's merged output
+// Larger of two pairs of fp16 numbers that are not negative (their bits order them).
+__device__ __forceinline__ uint32_t kv4_max_halves(uint32_t a, uint32_t b) {
+  const u16x2_t x = __builtin_bit_cast(u16x2_t, a), y = __builtin_bit_cast(u16x2_t, b);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
+}
 
-template <int WAVES>
-struct Kv4Lds {
-  alignas(16) float o[WAVES][16][kMergeRow];
-  float m[WAVES][32], l[WAVES][32];
-};
+// The largest half of the four quarters that share a column (the halves not negative).
+__device__ __forceinline__ uint32_t kv4_row_max(uint32_t v) {
+  u32x2_t w = kv4_swap16(v);
+  w = kv4_swap32(kv4_max_halves(w[0], w[1]));
+  v = kv4_max_halves(w[0], w[1]);
+  return max(v & 0xFFFFu, v >> 16);
+}
 
-// QT: query tiles of 16 rows (1 .. 4); a wavefront takes up to two of them.  G: groups of
-// dimensions (1 or 2).
-template <int QT, int G, int WAVES>
-__global__ __launch_bounds__(WAVES* kWave) void k_kv4_partial(Kv4AttnArgs a) {
-  constexpr int QW = QT < 2 ? 1 : 2;
-  constexpr int QG = (QT + 1) / 2;   // wavefronts that share a tile of positions
-  constexpr int KW = WAVES / QG;     // tiles of positions at a time
-  constexpr int kThreads = WAVES * kWave;
-  __shared__ Kv4Lds<WAVES> L;
-  const int s = blockIdx.x, g = blockIdx.y;
-  const int lane = threadIdx.x % kWave;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / kWave));
-  const int qg = wave % QG, kw = wave / QG;
-  const int col = lane & 15, quarter = lane >> 4;
-  const int Gq = a.Hq / a.Hkv;
-  const int rows = Gq * a.M;
-  const int total = a.P + a.T + a.M;
-  const int first = s * a.tiles_per_split;
-  const int last = min((total + kKv4Tile - 1) / kKv4Tile, first + a.tiles_per_split);
-  const size_t head = static_cast<size_t>(g) * (a.S / kKv4Tile) * kv4_tile_bytes(G);
-  const uint8_t* kbase = a.k_cache + head;
-  const uint8_t* vbase = a.v_cache + head;
+// Orders a wavefront's LDS accesses to each other's words, for the compiler (the hardware keeps
+// them in order).
+__device__ __forceinline__ void kv4_wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
-  Kv4Regs<G> r;
-  int n = first + kw;
-  if (n < last) kv4_load<G>(kbase + static_cast<size_t>(n) * kv4_tile_bytes(G), vbase + static_cast<size_t>(n) * kv4_tile_bytes(G), lane, r);
-
-  // this lane's query row in each query tile, its fragments of q and their sums per group
+// Query rows of one wavefront (QW tiles of 16) and what it has summed for them.
+template <int QW, int G>
+struct Kv4Rows {
+  // Per lane the query row's fragments of q times 2^(15 - e), where the row's largest value
+  // lies below 2^e, as fp16 (bf16's 8 bits fit, down to 2^-29 of the largest), their sums per
+  // group times 2^-24, and the factor that takes a score to log2.
+  f16x8_t qf[QW][4];
+  float qs[QW][G], factor[QW];
   bool live[QW];
   int qi[QW];
-  bf16x8_t qf[QW][4];
-  float qs[QW][G];
+  float ref[QW];              // what weights are relative to: 2^(score - ref)
+  f32x4_t o[QW][8], aux[QW];  // aux: in quarter 0 the sum of weights, and of weights times minima
+  u32x4_t raw[QW][4];
+
+  __device__ __forceinline__ void request(const Kv4AttnArgs& a, int g, int row0, int lane) {
+    const int Gq = a.Hq / a.Hkv;
 #pragma unroll
-  for (int t = 0; t < QW; ++t) {
-    const int row = 16 * (QW * qg + t) + col;
-    live[t] = row < rows;
-    qi[t] = live[t] ? row % a.M : 0;
-    const int hl = live[t] ? row / a.M : 0;
+    for (int t = 0; t < QW; ++t) {
+      const int row = row0 + 16 * t + (lane & 15);
+      live[t] = row < Gq * a.M;
+      qi[t] = live[t] ? row % a.M : 0;
+      const int hl = live[t] ? row / a.M : 0;  // (a row past the last repeats the first)
+      const uint16_t* q = a.q + (static_cast<size_t>(qi[t]) * a.Hq + g * Gq + hl) * kKv4D + 8 * (lane >> 4);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      u32x4_t w{0, 0, 0, 0};
-      if (live[t])
-        w = *reinterpret_cast<const u32x4_t*>(a.q + (static_cast<size_t>(qi[t]) * a.Hq + g * Gq + hl) * kKv4D + 32 * j +
-                                              8 * quarter) ^ a.q_sign;
-      qf[t][j] = __builtin_bit_cast(bf16x8_t, w);
-    }
-#pragma unroll
-    for (int gg = 0; gg < G; ++gg) {
-      float sum = 0.f;
-#pragma unroll
-      for (int j = gg * (4 / G); j < (gg + 1) * (4 / G); ++j)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += static_cast<float>(qf[t][j][e]);
-      qs[t][gg] = kv4_cross_sum(sum);
+      for (int j = 0; j < 4; ++j) raw[t][j] = *reinterpret_cast<const u32x4_t*>(q + 32 * j);
     }
   }
 
-  float m[QW], lsum[QW], zsum[QW][G];
-  f32x4_t o[QW][8], osum[QW][G];
+  __device__ __forceinline__ void begin(const Kv4AttnArgs& a) {
 #pragma unroll
-  for (int t = 0; t < QW; ++t) {
-    m[t] = -INFINITY;
-    lsum[t] = 0.f;
+    for (int t = 0; t < QW; ++t) {
+      uint32_t top = 0;
 #pragma unroll
-    for (int gg = 0; gg < G; ++gg) {
-      zsum[t][gg] = 0.f;
-      osum[t][gg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int j = 0; j < 4; ++j) {
+        raw[t][j] ^= a.q_sign;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = kv4_max_halves(top, raw[t][j][i] & 0x7FFF7FFFu);
+      }
+      const int e = static_cast<int>(kv4_row_max(top) >> 7) - 126;  // bf16's exponent field
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          qf[t][j][2 * i] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] << 16), 15 - e));
+          qf[t][j][2 * i + 1] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] & 0xFFFF0000u), 15 - e));
+        }
+#pragma unroll
+      for (int gg = 0; gg < G; ++gg) {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = gg * (4 / G); j < (gg + 1) * (4 / G); ++j)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum += static_cast<float>(qf[t][j][i]);
+        qs[t][gg] = kv4_cross_sum(sum) * 0x1p-24f;
+      }
+      factor[t] = fminf(fmaxf(ldexpf(a.scale_log2, 9 + e), 0x1p-126f), 0x1p126f);
+      ref[t] = -INFINITY;
+      aux[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-#pragma unroll
-    for (int dt = 0; dt < 8; ++dt) o[t][dt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
-  const _Float16 h16 = static_cast<_Float16>(16.f);
-  const f16x8_t sixteen{h16, h16, h16, h16, h16, h16, h16, h16};
 
-  for (; n < last; n += KW) {
-    const int key0 = n * kKv4Tile;
-    const bool masked = key0 + kKv4Tile > a.P;  // the same for the whole wavefront
-    // scores: lane holds positions 16u + 4 quarter + e of its query
-    f32x4_t x[QW][2];
+  // Scores times 2^-24: lane holds positions 16u + 4 quarter + e of its query.
+  __device__ __forceinline__ void scores(const Kv4Keys<G>& k, f32x4_t (&x)[QW][2]) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       f32x4_t st[QW][G];
 #pragma unroll
-      for (int t = 0; t < QW; ++t)
-#pragma unroll
-        for (int gg = 0; gg < G; ++gg) {
-          const float c = -16.f * qs[t][gg];
-          st[t][gg] = f32x4_t{c, c, c, c};
-        }
-#pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const bf16x8_t kf = kv4_bf16(r.kc[u][j]);
+        const f16x8_t kf = kv4_codes(k.c[u][j]);
 #pragma unroll
         for (int t = 0; t < QW; ++t)
-          st[t][j * G / 4] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][j], st[t][j * G / 4], 0, 0, 0);
+          st[t][j * G / 4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              kf, qf[t][j], j % (4 / G) == 0 ? f32x4_t{0.f, 0.f, 0.f, 0.f} : st[t][j * G / 4], 0, 0, 0);
       }
 #pragma unroll
       for (int t = 0; t < QW; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float v = 0.f;
+          float y = 0.f;
 #pragma unroll
-          for (int gg = 0; gg < G; ++gg) {
-            const f16x8_t ks = __builtin_bit_cast(f16x8_t, r.ks[gg]), km = __builtin_bit_cast(f16x8_t, r.km[gg]);
-            v = __builtin_fmaf(static_cast<float>(km[4 * u + e]), qs[t][gg], v);
-            v = __builtin_fmaf(static_cast<float>(ks[4 * u + e]), st[t][gg][e], v);
-          }
-          x[t][u][e] = v;
+          for (int gg = 0; gg < G; ++gg)
+            y = __builtin_fmaf(static_cast<float>(__builtin_bit_cast(f16x8_t, k.m[gg])[4 * u + e]), qs[t][gg], y);
+#pragma unroll
+          for (int gg = 0; gg < G; ++gg)
+            y = __builtin_fmaf(static_cast<float>(__builtin_bit_cast(f16x8_t, k.s[gg])[4 * u + e]), st[t][gg][e], y);
+          x[t][u][e] = y;
         }
     }
-    Kv4Regs<G> c;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) c.vc[u] = r.vc[u];
-#pragma unroll
-    for (int gg = 0; gg < G; ++gg) {
-      c.vs[gg] = r.vs[gg];
-      c.vm[gg] = r.vm[gg];
-    }
-    if (n + KW < last)
-      kv4_load<G>(kbase + static_cast<size_t>(n + KW) * kv4_tile_bytes(G), vbase + static_cast<size_t>(n + KW) * kv4_tile_bytes(G), lane, r);
-    if (masked) {
-#pragma unroll
-      for (int t = 0; t < QW; ++t) {
-        const uint32_t vis = live[t] ? kv4_visibility(a.mask + static_cast<size_t>(qi[t]) * a.W, a.W, a.P, key0, total) : 0u;
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!((vis >> (16 * u + 4 * quarter + e)) & 1u)) x[t][u][e] = -INFINITY;
-      }
-#pragma unroll
-      for (int gg = 0; gg < G; ++gg)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          c.vs[gg][e] = kv4_finite(c.vs[gg][e]);
-          c.vm[gg][e] = kv4_finite(c.vm[gg][e]);
-        }
-    }
-    // the exponent of the tile's largest scale of a value (scales are not negative), at least 2^-14
-    float smax = 0x1p-14f;
-#pragma unroll
-    for (int gg = 0; gg < G; ++gg) {
-      const f16x8_t vs = __builtin_bit_cast(f16x8_t, c.vs[gg]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) smax = fmaxf(smax, static_cast<float>(vs[e]));
-    }
-    smax = kv4_cross_max(smax);
-    const float shift = static_cast<float>(__builtin_amdgcn_frexp_expf(smax) - 14);
+  }
 
-    f16x8_t pf[QW][G];
+  __device__ __forceinline__ void mask(const Kv4AttnArgs& a, int key0, int total, int quarter, f32x4_t (&x)[QW][2]) const {
+#pragma unroll
+    for (int t = 0; t < QW; ++t) {
+      const uint32_t vis = live[t] ? kv4_visibility(a.mask + static_cast<size_t>(qi[t]) * a.W, a.W, a.P, key0, total) : 0u;
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!((vis >> (16 * u + 4 * quarter + e)) & 1u)) x[t][u][e] = -INFINITY;
+    }
+  }
+
+  // Weights of the tile's positions, and their products with the values.  keep, ones: the
+  // auxiliary operand's first row is ones.
+  __device__ __forceinline__ void values(const Kv4Values<G>& v, const f32x4_t (&x)[QW][2], uint32_t keep, uint32_t ones) {
+    // the exponent of the tile's largest scale, at least 0 (fp16's field: s < 2^(field - 14))
+    uint32_t top = 0;
+#pragma unroll
+    for (int gg = 0; gg < G; ++gg)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) top = kv4_max_halves(top, v.s[gg][e]);
+    const int field = static_cast<int>((kv4_row_max(top) & 0x7FFFu) >> 10);
+    const float lift = static_cast<float>(max(field - 14, 0) - 8);
+
+    f16x8_t pf[QW][G], ps[QW];
 #pragma unroll
     for (int t = 0; t < QW; ++t) {
       float mx = -INFINITY;
@@ -283,186 +311,378 @@ __global__ __launch_bounds__(WAVES* kWave) void k_kv4_partial(Kv4AttnArgs a) {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[t][u][e]);
-      mx = kv4_cross_max(mx);
-      const float mn = mx == -INFINITY ? m[t] : fmaxf(m[t], mx * a.scale_log2 + shift);
-      const float ref = mn == -INFINITY ? 0.f : mn;  // nothing visible yet: every weight is 2^-inf
-      const float alpha = __builtin_amdgcn_exp2f(m[t] - ref);
-      m[t] = mn;
-      float add = 0.f, z[G];
+      const float cand = __builtin_fmaf(kv4_cross_max(mx), factor[t], lift);
+      if (__builtin_amdgcn_ballot_w64(cand > ref[t] + 6.f)) {  // some row's weights would pass 2^14
+        const float r = cand > ref[t] + 6.f ? cand : ref[t];
+        const float alpha = ref[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[t] - r);
+        ref[t] = r;
+        aux[t] *= alpha;
 #pragma unroll
-      for (int gg = 0; gg < G; ++gg) z[gg] = 0.f;
+        for (int dt = 0; dt < 8; ++dt) o[t][dt] *= alpha;
+      }
+      const float base = ref[t] == -INFINITY ? 0.f : ref[t];  // nothing visible yet: every weight is 2^-inf
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][u][e], a.scale_log2, -ref));
-          add += p;
+        for (int e = 0; e < 4; ++e)
+          ps[t][4 * u + e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(x[t][u][e], factor[t], -base)));
 #pragma unroll
-          for (int gg = 0; gg < G; ++gg) {
-            const f16x8_t vs = __builtin_bit_cast(f16x8_t, c.vs[gg]), vm = __builtin_bit_cast(f16x8_t, c.vm[gg]);
-            pf[t][gg][4 * u + e] = static_cast<_Float16>(p * static_cast<float>(vs[4 * u + e]));
-            z[gg] = __builtin_fmaf(p, static_cast<float>(vm[4 * u + e]), z[gg]);
-          }
-        }
-      lsum[t] = lsum[t] * alpha + add;
-#pragma unroll
-      for (int gg = 0; gg < G; ++gg) zsum[t][gg] = zsum[t][gg] * alpha + z[gg];
-      if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {  // some row's maximum moved
-#pragma unroll
-        for (int dt = 0; dt < 8; ++dt) o[t][dt] *= alpha;
-#pragma unroll
-        for (int gg = 0; gg < G; ++gg) osum[t][gg] *= alpha;
-      }
-#pragma unroll
-      for (int gg = 0; gg < G; ++gg)
-        osum[t][gg] = __builtin_amdgcn_mfma_f32_16x16x32_f16(sixteen, pf[t][gg], osum[t][gg], 0, 0, 0);
+      for (int gg = 0; gg < G; ++gg) pf[t][gg] = ps[t] * __builtin_bit_cast(f16x8_t, v.s[gg]);
     }
+    u32x4_t w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = and_or(v.m[e], keep, ones);
+#pragma unroll
+    for (int t = 0; t < QW; ++t)
+      aux[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, w), ps[t], aux[t], 0, 0, 0);
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
-      const f16x8_t vf = kv4_f16(c.vc[dt / 4][dt % 4]);
+      const f16x8_t vf = kv4_codes(v.c[dt / 4][dt % 4]);
 #pragma unroll
       for (int t = 0; t < QW; ++t)
         o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][dt * G / 8], o[t][dt], 0, 0, 0);
     }
   }
 
-  // minima added, biases taken off; then the workgroup's maximum per row
+  // Codes back from 2^-24, minima added.
+  __device__ __forceinline__ void finish(int col) {
 #pragma unroll
-  for (int t = 0; t < QW; ++t) {
-    lsum[t] = kv4_cross_sum(lsum[t]);
+    for (int t = 0; t < QW; ++t)
 #pragma unroll
-    for (int gg = 0; gg < G; ++gg) {
-      const float z = kv4_cross_sum(zsum[t][gg]) - osum[t][gg][0];
+      for (int gg = 0; gg < G; ++gg) {
+        const float z = __shfl(aux[t][1 + gg], col);
 #pragma unroll
-      for (int dt = gg * (8 / G); dt < (gg + 1) * (8 / G); ++dt) o[t][dt] += z;
-    }
-    if (quarter == 0) L.m[wave][16 * t + col] = m[t];
+        for (int dt = gg * (8 / G); dt < (gg + 1) * (8 / G); ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][dt][e] = __builtin_fmaf(o[t][dt][e], 0x1p24f, z);
+      }
   }
+};
+
+constexpr int kWaves = 8;
+constexpr int kRing = 4;  // tiles of a wavefront's ring in LDS, all but one in flight
+
+// s_waitcnt immediate: at most `vm` vector memory operations outstanding, nothing said of others.
+constexpr int kv4_wait_vm(int vm) { return (vm & 15) | (7 << 4) | (15 << 8) | ((vm >> 4) << 14); }
+
+constexpr int kKv4WaitLds = 15 | (7 << 4) | (3 << 14);  // no LDS operation outstanding
+
+// A wavefront takes QW query tiles of 16 rows, QG wavefronts share a tile of positions.  G:
+// groups of dimensions (1 or 2).
+//
+// RING: a wavefront's tiles go from memory into a ring of four in LDS of its own (no register is
+// held by a load in flight, so three tiles are, 14 KB a wavefront); otherwise into registers, for
+// ranges of a tile or two per wavefront, which a ring could not get ahead of.
+template <int QW, int QG, int G, bool RING>
+__global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_partial(Kv4AttnArgs a) {
+  constexpr int KW = kWaves / QG;  // tiles of positions at a time
+  constexpr int kThreads = kWaves * kWave;
+  constexpr int kSlot = (2 * kv4_tile_bytes(G)) / 16;  // of a wavefront, in 16 bytes: key codes, value codes, their scales and minima
+  constexpr int kHalfRow = kKv4D / 2 + 4;               // floats of a merged half row of outputs
+  constexpr int kBuffer = kWaves * 16 * kHalfRow / 4;  // the wavefronts' half rows
+  static_assert(kRing * kWaves * kSlot >= 2 * kBuffer, "the merge fits the ring");
+  __shared__ u32x4_t lds[RING ? kRing * kWaves * kSlot : 2 * kBuffer];
+  __shared__ float Lm[kWaves][16 * QW], Ll[kWaves][16 * QW];
+  const int s = blockIdx.x, g = blockIdx.y;
+  const int lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / kWave));
+  const int qg = wave % QG, kw = wave / QG;
+  const int col = lane & 15, quarter = lane >> 4;
+  const int total = a.P + a.T + a.M;
+  const int first = s * a.tiles_per_split;
+  const int last = min((total + kKv4Tile - 1) / kKv4Tile, first + a.tiles_per_split);
+  const size_t head = static_cast<size_t>(g) * (a.S / kKv4Tile) * kv4_tile_bytes(G);
+  const uint8_t* kbase = a.k_cache + head;
+  const uint8_t* vbase = a.v_cache + head;
+  // the auxiliary product's first row is ones
+  const uint32_t keep = col == 0 ? 0u : ~0u, ones = col == 0 ? 0x3C003C00u : 0u;
+  Kv4Rows<QW, G> rows;
+  rows.request(a, g, 16 * QW * qg, lane);
+  int n = first + kw;
+
+  if constexpr (RING) {
+    constexpr int VM = 4 + G;  // vector memory operations of a tile's loads
+    u32x4_t* ring = lds + wave * (kRing * kSlot);
+    const uint32_t ring_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)ring));
+    // Tile `tile` into slot `slot`.  A tile past the range's last is one 16-byte piece of that
+    // one over and over: the count of loads in flight stays what the waits assume, and memory
+    // sees one line.
+    auto request = [&](int slot, int tile) __attribute__((always_inline)) {
+      const bool real = tile < last;
+      const size_t at = static_cast<size_t>(real ? tile : last - 1) * kv4_tile_bytes(G);
+      const int l16 = real ? 16 * lane : 0, l4 = real ? 4 * lane : 0, next = real ? 1024 : 0;
+      const uint8_t* kt = kbase + at;
+      const uint8_t* vt = vbase + at;
+      const uint32_t to = __builtin_amdgcn_readfirstlane(ring_at + slot * (16 * kSlot));
+      kv4_to_lds<16>(kt + l16, to);
+      kv4_to_lds<16>(kt + next + l16, to + 1024);
+      if constexpr (G == 1) {
+        kv4_to_lds<4>((lane < 32 ? kt : vt) + kKv4CodeBytes + (real ? 4 * (lane % 32) : 0), to + 4096);
+      } else {
+        kv4_to_lds<4>(kt + kKv4CodeBytes + l4, to + 4096);
+        kv4_to_lds<4>(vt + kKv4CodeBytes + l4, to + 4096 + 256);
+      }
+      kv4_to_lds<16>(vt + l16, to + 2048);
+      kv4_to_lds<16>(vt + next + l16, to + 2048 + 1024);
+    };
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i) request(i, n + i * KW);
+    rows.begin(a);
+    for (int slot = 0; n < last; n += KW, slot = (slot + 1) % kRing) {
+      // Into the slot whose tile the last step was done with, once that step's reads are back.
+      __builtin_amdgcn_s_waitcnt(kKv4WaitLds);
+      request((slot + kRing - 1) % kRing, n + (kRing - 1) * KW);
+      // Loads complete in order: when the later tiles' are all that is outstanding, this tile
+      // is in LDS.
+      __builtin_amdgcn_s_waitcnt(kv4_wait_vm((kRing - 1) * VM));
+      asm volatile("" ::: "memory");
+      const int key0 = n * kKv4Tile;
+      const bool masked = key0 + kKv4Tile > a.P;  // the same for the whole wavefront
+      u32x4_t* p = ring + slot * kSlot;
+      if (masked && lane < 32 * G) {  // scales and minima of values that nothing has written
+        uint32_t* w = reinterpret_cast<uint32_t*>(p + 256) + 32 * G + lane;
+        *w = kv4_finite(*w);
+      }
+      if (masked) kv4_wave_fence();
+      Kv4Keys<G> k;
+      Kv4Values<G> v;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        k.c[u] = p[64 * u + lane];
+        v.c[u] = p[128 + 64 * u + lane];
+      }
+      const u32x4_t* meta = p + 256 + 2 * G * quarter;
+#pragma unroll
+      for (int gg = 0; gg < G; ++gg) {
+        k.s[gg] = meta[2 * gg];
+        k.m[gg] = meta[2 * gg + 1];
+        v.s[gg] = meta[8 * G + 2 * gg];
+      }
+      v.m = meta[8 * G + (col == 2 ? 2 * (G - 1) : 0) + 1];
+      f32x4_t x[QW][2];
+      rows.scores(k, x);
+      if (masked) rows.mask(a, key0, total, quarter, x);
+      rows.values(v, x, keep, ones);
+    }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);  // nothing may land in the ring once it is used for the merge
+    __syncthreads();
+  } else {
+    Kv4Keys<G> k{};
+    Kv4Values<G> v{};
+    if (n < last) {
+      kv4_load<G>(kbase + static_cast<size_t>(n) * kv4_tile_bytes(G), lane, k);
+      kv4_load<G>(vbase + static_cast<size_t>(n) * kv4_tile_bytes(G), lane, v);
+    }
+    rows.begin(a);
+    auto one_tile = [&](auto masked) __attribute__((always_inline)) {
+      f32x4_t x[QW][2];
+      rows.scores(k, x);
+      const int next = n + KW;
+      if (next < last)
+        kv4_load<G>(kbase + static_cast<size_t>(next) * kv4_tile_bytes(G), lane, k);
+      else
+        kv4_keep(k);
+      if constexpr (decltype(masked)::value) {
+        rows.mask(a, n * kKv4Tile, total, quarter, x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+#pragma unroll
+          for (int gg = 0; gg < G; ++gg) v.s[gg][e] = kv4_finite(v.s[gg][e]);
+          v.m[e] = kv4_finite(v.m[e]);
+        }
+      }
+      rows.values(v, x, keep, ones);
+      if (next < last)
+        kv4_load<G>(vbase + static_cast<size_t>(next) * kv4_tile_bytes(G), lane, v);
+      else
+        kv4_keep(v);
+      n = next;
+    };
+    // tiles of committed positions alone, then those that the masks have a say in
+    for (const int plain = min(last, a.P / kKv4Tile); n < plain;) one_tile(std::false_type{});
+    while (n < last) one_tile(std::true_type{});
+  }
+
+  // The workgroup's largest reference per row; every wavefront scales its outputs to it.
+  rows.finish(col);
+  if (quarter == 0)
+#pragma unroll
+    for (int t = 0; t < QW; ++t) Lm[wave][16 * t + col] = rows.ref[t];
   __syncthreads();
 #pragma unroll
   for (int t = 0; t < QW; ++t) {
     float mall = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < KW; ++w) mall = fmaxf(mall, L.m[w * QG + qg][16 * t + col]);
-    const float sc = m[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[t] - mall);
+    for (int w = 0; w < KW; ++w) mall = fmaxf(mall, Lm[w * QG + qg][16 * t + col]);
+    const float sc = rows.ref[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows.ref[t] - mall);
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) o[t][dt] *= sc;
-    if (quarter == 0) L.l[wave][16 * t + col] = lsum[t] * sc;
+    for (int dt = 0; dt < 8; ++dt) rows.o[t][dt] *= sc;
+    if (quarter == 0) Ll[wave][16 * t + col] = rows.aux[t][0] * sc;
   }
-  // One query tile of every wavefront at a time: outputs [row][dimension] in LDS, then the
-  // workgroup adds the wavefronts' in order, four dimensions a thread.
+  // Half a query tile of every wavefront at a time (64 dimensions), in two buffers in turn: outputs
+  // [row][dimension] in LDS, then the workgroup adds the wavefronts' in order, four dimensions a thread.
+  const int nrows = a.Hq / a.Hkv * a.M;
 #pragma unroll
-  for (int t = 0; t < QW; ++t) {
+  for (int t = 0; t < QW; ++t)
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt)
-      *reinterpret_cast<f32x4_t*>(&L.o[wave][col][16 * dt + 4 * quarter]) = o[t][dt];
-    __syncthreads();
-    for (int i = threadIdx.x; i < QG * 16 * (kKv4D / 4); i += kThreads) {
-      const int qw = i / (16 * (kKv4D / 4)), rr = i / (kKv4D / 4) % 16, d4 = 4 * (i % (kKv4D / 4));
-      const int row = 16 * (QW * qw + t) + rr;
-      if (row >= rows) continue;  // padding rows are never read
-      f32x4_t sum = *reinterpret_cast<const f32x4_t*>(&L.o[qw][rr][d4]);
-      float ls = L.l[qw][16 * t + rr];
+    for (int h = 0; h < 2; ++h) {
+      float* buf = reinterpret_cast<float*>(lds + h * kBuffer);
 #pragma unroll
-      for (int w = 1; w < KW; ++w) {
-        sum += *reinterpret_cast<const f32x4_t*>(&L.o[w * QG + qw][rr][d4]);
-        ls += L.l[w * QG + qw][16 * t + rr];
-      }
-      if (a.splits == 1) {
-        const float inv = ls == 0.f ? 0.f : 1.f / ls;
-        const int token = row % a.M, h = g * Gq + row / a.M;
-        uint2 w2;
-        w2.x = static_cast<uint32_t>(float_to_bf16_bits(sum[0] * inv)) | (static_cast<uint32_t>(float_to_bf16_bits(sum[1] * inv)) << 16);
-        w2.y = static_cast<uint32_t>(float_to_bf16_bits(sum[2] * inv)) | (static_cast<uint32_t>(float_to_bf16_bits(sum[3] * inv)) << 16);
-        *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(token) * a.Hq + h) * kKv4D + d4) = w2;
-        continue;
-      }
-      const size_t base = (static_cast<size_t>(g) * a.splits + s) * a.rows_pad + row;
-      *reinterpret_cast<f32x4_t*>(a.part_o + base * kKv4D + d4) = sum;
-      if (d4 == 0) {
-        float mm = -INFINITY;
+      for (int dt = 0; dt < 4; ++dt)
+        *reinterpret_cast<f32x4_t*>(buf + (wave * 16 + col) * kHalfRow + 16 * dt + 4 * quarter) = rows.o[t][4 * h + dt];
+      __syncthreads();
+      for (int i = threadIdx.x; i < QG * 16 * 16; i += kThreads) {
+        const int qw = i / 256, rr = i / 16 % 16, d4 = 4 * (i % 16);
+        const int row = 16 * (QW * qw + t) + rr;
+        if (row >= nrows) continue;  // padding rows are never read
+        f32x4_t sum = *reinterpret_cast<const f32x4_t*>(buf + (qw * 16 + rr) * kHalfRow + d4);
+        float ls = Ll[qw][16 * t + rr];
 #pragma unroll
-        for (int w = 0; w < KW; ++w) mm = fmaxf(mm, L.m[w * QG + qw][16 * t + rr]);
-        a.part_ml[2 * base] = mm;
-        a.part_ml[2 * base + 1] = ls;
+        for (int w = 1; w < KW; ++w) {
+          sum += *reinterpret_cast<const f32x4_t*>(buf + ((w * QG + qw) * 16 + rr) * kHalfRow + d4);
+          ls += Ll[w * QG + qw][16 * t + rr];
+        }
+        if (a.splits == 1) {
+          const float inv = ls == 0.f ? 0.f : 1.f / ls;
+          const int token = row % a.M, hq = g * (a.Hq / a.Hkv) + row / a.M;
+          *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(token) * a.Hq + hq) * kKv4D + 64 * h + d4) =
+              make_uint2(kv4_pack(sum[0] * inv, sum[1] * inv), kv4_pack(sum[2] * inv, sum[3] * inv));
+          continue;
+        }
+        const size_t base = (static_cast<size_t>(g) * a.splits + s) * a.rows_pad + row;
+        *reinterpret_cast<f32x4_t*>(a.part_o + base * kKv4D + 64 * h + d4) = sum;
+        if (d4 == 0 && h == 0) {
+          float mm = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < KW; ++w) mm = fmaxf(mm, Lm[w * QG + qw][16 * t + rr]);
+          a.part_ml[2 * base] = mm;
+          a.part_ml[2 * base + 1] = ls;
+        }
       }
     }
-    if (t + 1 < QW) __syncthreads();
-  }
 }
 
-// One workgroup per (token i, query head h), one thread per dimension; the ranges' outputs
-// are summed in range order, the first kBatch requested together with the (max, sum) pairs.
-__global__ __launch_bounds__(kKv4D) void k_kv4_combine(Kv4AttnArgs a) {
-  __shared__ float sm[kKv4MaxSplits], sl[kKv4MaxSplits];
-  constexpr int kBatch = 32, kMore = 16;
+constexpr int kCombineThreads = 256;
+
+// One workgroup per (token i, query head h): 8 teams of 32 threads, four dimensions a thread,
+// team c takes the ranges c, c + 8, ...  Every wavefront reads the ranges' (max, sum) pairs
+// itself, one a lane, so the outputs are requested with them and the only barrier is
+// the one in front of the teams' sum, which runs in team order.
+__global__ __launch_bounds__(kCombineThreads) void k_kv4_combine(Kv4AttnArgs a) {
+  constexpr int kTeams = kCombineThreads / 32, kBatch = 8;
+  __shared__ f32x4_t num[kTeams][32];
+  __shared__ float den[kTeams];
   const int i = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
-  const int d = threadIdx.x;
+  const int team = threadIdx.x / 32, d4 = 4 * (threadIdx.x % 32);
+  const int lane = threadIdx.x % kWave;
   const int Gq = a.Hq / a.Hkv;
   const int g = h / Gq, row = h % Gq * a.M + i;
   const int ns = a.splits;
   const size_t base = static_cast<size_t>(g) * ns * a.rows_pad + row;
-  const float* po = a.part_o + base * kKv4D + d;
-  const size_t step = static_cast<size_t>(a.rows_pad) * kKv4D;
-  for (int s = d; s < ns; s += kKv4D) {
-    const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (base + static_cast<size_t>(s) * a.rows_pad));
-    sm[s] = ml.x;
-    sl[s] = ml.y;
-  }
-  float v[kBatch];
+  const float* po = a.part_o + base * kKv4D + d4;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + base;
+  const size_t step = static_cast<size_t>(a.rows_pad);
+  f32x4_t sum{0.f, 0.f, 0.f, 0.f};
+  float total = 0.f, mmax = -INFINITY;
+  for (int s0 = 0; s0 < ns; s0 += kWave) {  // 64 ranges at a time: a lane's pair each
+    f32x4_t v[kBatch];
 #pragma unroll
-  for (int u = 0; u < kBatch; ++u) v[u] = u < ns ? po[u * step] : 0.f;
-  __syncthreads();
-  float mmax = -INFINITY;
-  for (int s = 0; s < ns; ++s) mmax = fmaxf(mmax, sm[s]);
-  __syncthreads();
-  for (int s = d; s < ns; s += kKv4D) sm[s] = sm[s] == -INFINITY ? 0.f : exp2f(sm[s] - mmax);
-  __syncthreads();
-  float den = 0.f, num = 0.f;
-#pragma unroll
-  for (int u = 0; u < kBatch; ++u)
-    if (u < ns) {
-      den += sm[u] * sl[u];
-      num += sm[u] * v[u];
+    for (int u = 0; u < kBatch; ++u) {
+      const int s = s0 + team + kTeams * u;
+      v[u] = s < ns ? *reinterpret_cast<const f32x4_t*>(po + s * step * kKv4D) : f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-  for (int s0 = kBatch; s0 < ns; s0 += kMore) {
+    const float2 own = s0 + lane < ns ? ml[(s0 + lane) * step] : make_float2(-INFINITY, 0.f);
+    float mx = own.x;
 #pragma unroll
-    for (int u = 0; u < kMore; ++u) v[u] = s0 + u < ns ? po[(s0 + u) * step] : 0.f;
+    for (int d = 1; d < kWave; d *= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
+    mx = fmaxf(mmax, mx);
+    const float w = own.x == -INFINITY ? 0.f : exp2f(own.x - mx);
+    const float keep = mmax == -INFINITY ? 0.f : exp2f(mmax - mx);
+    mmax = mx;
+    sum *= keep;
+    total *= keep;
+    const float wl = w * own.y;
 #pragma unroll
-    for (int u = 0; u < kMore; ++u)
-      if (s0 + u < ns) {
-        den += sm[s0 + u] * sl[s0 + u];
-        num += sm[s0 + u] * v[u];
-      }
+    for (int u = 0; u < kBatch; ++u) {
+      const int s = team + kTeams * u;
+      sum += v[u] * __shfl(w, s);
+      total += __shfl(wl, s);
+    }
   }
-  a.out[(static_cast<size_t>(i) * a.Hq + h) * kKv4D + d] = float_to_bf16_bits(den == 0.f ? 0.f : num / den);
+  num[team][d4 / 4] = sum;
+  if (d4 == 0) den[team] = total;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    total = den[0];
+#pragma unroll
+    for (int c = 1; c < kTeams; ++c) {
+      sum += num[c][d4 / 4];
+      total += den[c];
+    }
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(i) * a.Hq + h) * kKv4D + d4) =
+        make_uint2(kv4_pack(sum[0] * inv, sum[1] * inv), kv4_pack(sum[2] * inv, sum[3] * inv));
+  }
 }
 
-constexpr int kPartialWaves = 4;
+// How a call is cut: wavefronts of QW query tiles, QG of them on a tile of positions, each
+// taking `per_wave` tiles of a range.
+struct Kv4Shape {
+  int qw, qg, per_wave;
+  bool ring;
+};
 
-template <int G>
-void launch_partial(const Kv4AttnArgs& a, hipStream_t st) {
-  const dim3 grid(a.splits, a.Hkv), block(kPartialWaves * kWave);
-  switch (a.rows_pad / 16) {
-    case 1: hipLaunchKernelGGL((k_kv4_partial<1, G, kPartialWaves>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((k_kv4_partial<2, G, kPartialWaves>), grid, block, 0, st, a); break;
-    case 3: hipLaunchKernelGGL((k_kv4_partial<3, G, kPartialWaves>), grid, block, 0, st, a); break;
-    default: hipLaunchKernelGGL((k_kv4_partial<4, G, kPartialWaves>), grid, block, 0, st, a); break;
+// Up to kAlone tiles a wavefront one workgroup takes a whole head, and the second kernel is saved (300
+// positions of four heads 7.3 us a call against 10.0, 800 8.7 against 9.9; at five tiles 9.8 either way).
+// From kRingFrom tiles on the ring in LDS gets ahead of its wavefront (131138 positions of eight heads, 17
+// tiles: 42.6 us against 47.8 from registers, and with one query tile a wavefront 51.1; at three
+// tiles 12.9 against 11.7), and two query tiles a wavefront share the unpacking.
+constexpr int kAlone = 4, kRingFrom = 5;
+
+Kv4Shape kv4_shape(int M, int Hq, int Hkv, int P, int T) {
+  const int tiles = (P + T + M + kKv4Tile - 1) / kKv4Tile;
+  const int qt = (Hq / Hkv * M + 15) / 16;
+  const int ranges = (256 + Hkv - 1) / Hkv;  // per head: one workgroup a CU
+  auto cut = [&](int qw) {
+    const int qg = qt <= qw ? 1 : qt <= 2 * qw ? 2 : 4;
+    const int at_once = kWaves / qg;
+    int per_wave = (tiles + ranges * at_once - 1) / (ranges * at_once);
+    const int alone = (tiles + at_once - 1) / at_once;
+    if (alone <= kAlone) per_wave = alone;
+    return Kv4Shape{qw, qg, per_wave, per_wave >= kRingFrom};
+  };
+  if (qt > 1) {
+    const Kv4Shape wide = cut(2);
+    if (wide.ring) return wide;
   }
+  return cut(1);
+}
+
+template <int QW, int QG, bool RING>
+void launch_shape(const Kv4AttnArgs& a, int groups, hipStream_t st) {
+  const dim3 grid(a.splits, a.Hkv), block(kWaves * kWave);
+  if (groups == 1)
+    hipLaunchKernelGGL((k_kv4_partial<QW, QG, 1, RING>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_kv4_partial<QW, QG, 2, RING>), grid, block, 0, st, a);
+}
+
+template <int QG>
+void launch_narrow(const Kv4AttnArgs& a, int groups, bool ring, hipStream_t st) {
+  if (ring)
+    launch_shape<1, QG, true>(a, groups, st);
+  else
+    launch_shape<1, QG, false>(a, groups, st);
 }
 
 }  // namespace
 
 void kv4_attn_plan(int M, int Hq, int Hkv, int P, int T, int* splits, int* tiles_per_split) {
   const int tiles = (P + T + M + kKv4Tile - 1) / kKv4Tile;
-  const int rows_pad = 16 * ((Hq / Hkv * M + 15) / 16);
-  const int at_once = kPartialWaves / (rows_pad > 32 ? 2 : 1);  // tiles a workgroup works on at a time
-  // two workgroups a CU of the 256, every wavefront with a tile
-  const int most = (512 + Hkv - 1) / Hkv;  // ranges per head
-  int tps = (tiles + most - 1) / most;
-  tps = (tps + at_once - 1) / at_once * at_once;
-  *tiles_per_split = tps;
-  *splits = (tiles + tps - 1) / tps;
+  const Kv4Shape sh = kv4_shape(M, Hq, Hkv, P, T);
+  *tiles_per_split = sh.per_wave * (kWaves / sh.qg);
+  *splits = (tiles + *tiles_per_split - 1) / *tiles_per_split;
 }
 
 size_t kv4_attn_workspace_bytes(int M, int Hq, int Hkv, int P, int T) {
@@ -476,13 +696,20 @@ size_t kv4_attn_workspace_bytes(int M, int Hq, int Hkv, int P, int T) {
 }
 
 hipError_t launch_kv4_attention(const Kv4AttnArgs& a, int groups, hipStream_t st) {
-  if (groups == 1)
-    launch_partial<1>(a, st);
+  const Kv4Shape sh = kv4_shape(a.M, a.Hq, a.Hkv, a.P, a.T);
+  if (sh.qw == 2 && sh.qg == 1)
+    launch_shape<2, 1, true>(a, groups, st);
+  else if (sh.qw == 2)
+    launch_shape<2, 2, true>(a, groups, st);
+  else if (sh.qg == 1)
+    launch_narrow<1>(a, groups, sh.ring, st);
+  else if (sh.qg == 2)
+    launch_narrow<2>(a, groups, sh.ring, st);
   else
-    launch_partial<2>(a, st);
+    launch_narrow<4>(a, groups, sh.ring, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL(k_kv4_combine, dim3(a.M * a.Hq), dim3(kKv4D), 0, st, a);
+  hipLaunchKernelGGL(k_kv4_combine, dim3(a.M * a.Hq), dim3(kCombineThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -1,17 +1,17 @@
 """GPU parity of the tree attention over the 4-bit cache against the fp64 oracle on the
 values that the cache holds.
 
-Tolerance, from the arithmetic.  A value is m + s c; the kernel's weight of a position in the
-second product is fp16(p s): 2^-11 relative, on s c alone (the minima are summed with p
-in fp32), so 2^-11 sum_j p_j |v_j - m_j| <= 2^-11 sum_j p_j (|v_j| + |m_j|).  Below fp16's
-normal range the rounding is 2^-25 absolute, in units where the heaviest position of the call
-has at least 2^13 times (its p) times (the scale's share of its power of two): at most
-2^-37 of the largest scale a position, 15 codes: 2^-33 L smax.  Scores: a product of exact
-codes accumulates in fp32 with terms up to 31 s |q|, four chained products, at most four
-roundings each: 2^-20 scale sum_d 31 s |q_d| absolute, plus 2^-21 of the largest score for the
-exponent's argument; either changes a weight by as much relatively, and the output by twice
-that times sum_j p_j |v_j|.  Sums in fp32 over biased codes: 2^-18 of sum_j p_j (31 s_j).  The output is
-rounded to bf16: 2^-8."""
+Tolerance, from the arithmetic.  A value is m + s c.  The kernel rounds a weight p to fp16 for
+the sum of weights and for the minima, and the product of that and s once more for the
+codes: 2^-11 relative each, so 2^-11 (sum_j p_j |v_j| + |o|) for the first and 2^-11 sum_j p_j
+|v_j - m_j| for the second, together at most 2^-11 sum_j p_j (3 |v_j| + |m_j|).  Below fp16's normal
+range either rounding is 2^-25 absolute, where the heaviest weight of the row is at least
+2^(8 - E), 2^E (E >= 0) above the largest scale of a value: L 2^(E - 33) (15 + max |v|).
+Scores: fp32 sums of exact products of codes, 4 chained matrix products of terms up to 15 s |q|, at
+most four roundings each, and the minima's share: 2^-20 scale sum_d (15 s + |m|) |q_d| absolute, plus 2^-21 of the largest
+score for the exponent's argument; either changes a weight by as much relatively, and the
+output by twice that times sum_j p_j |v_j|.  Second products sum in fp32: 2^-18 of sum_j p_j (15 s_j + |m_j|).  The output
+is rounded to bf16: 2^-8."""
 import math
 
 import numpy as np
@@ -85,10 +85,12 @@ def _check(M, Hq, Hkv, P, T, group, seed, q_scale=1.0, mask=None, S=None, scale=
     G = Hq // Hkv
     delta = np.empty((M, Hq, 1))
     for h in range(Hq):
-        delta[:, h, 0] = (2.0 ** -20 * 31 * abs(scale) * (qa[:, h] @ wide(kh[1])[:, h // G].T).max(1) +
+        size = 15 * wide(kh[1]) + np.abs(wide(kh[2]))
+        delta[:, h, 0] = (2.0 ** -20 * abs(scale) * (qa[:, h] @ size[:, h // G].T).max(1) +
                           2.0 ** -21 * np.abs(oracle.bf16_bits_to_f64(q)[:, h] @ K[:, h // G].T * scale).max(1))
-    tol = (2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * (wabs + wmin) + 2.0 ** -33 * n * float(vh[1].max()) +
-           2 * delta * wabs + 2.0 ** -18 * (31 * wstep + wmin))
+    E = max(0, math.frexp(float(vh[1].max()))[1])
+    tol = (2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * (3 * wabs + wmin) + n * 2.0 ** (E - 33) * (15 + np.abs(V).max()) +
+           2 * delta * wabs + 2.0 ** -18 * (15 * wstep + wmin))
     err = np.abs(got - ref)
     assert np.all(err <= tol), (what, float(err.max()), float((err / np.maximum(tol, 1e-300)).max()))
     return got

@@ -255,20 +255,15 @@ def test_binding_refuses_tensors_that_a_kernel_cannot_read():
         _append(k=np.zeros(1 << 16, np.int16))
 
     class Strided:  # on the right device by its word, but not whole
-        nbytes = 1 << 30
-
         def get_device(self):
             return -2
 
         def is_contiguous(self):
             return False
+
+        def data_ptr(self):
+            return A
     with refused("not contiguous"):
         _verify(logits=Strided())
-
-    class Small(Strided):
-        nbytes = 16
-
-        def is_contiguous(self):
-            return True
-    with refused("needs"):
-        _verify(logits=Small())
+    with refused("current device"):
+        _verify(logits=torch.zeros(8))

@@ -1359,14 +1359,7 @@ int subspec_tree_verify(const void* logits, const int* parent, const int* token,
   a.c = a.greedy ? 0.f : c;
   a.inv_t = a.greedy ? 0.0 : 1.0 / static_cast<double>(temperature);
   subspec::verify_plan(N, V, &a.chunks, &a.chunk_len);
-  char* p = static_cast<char*>(ws);
-  a.cnt = reinterpret_cast<unsigned*>(p);
-  p += subspec::kSplitCounterBytes;
-  a.last_row = reinterpret_cast<int*>(p);
-  a.row_stat = reinterpret_cast<float2*>(p + 8);
-  a.slice_sum = reinterpret_cast<double*>(p + 16);
-  const int slices = (V + subspec::kVerifySlice - 1) / subspec::kVerifySlice;
-  a.stat = reinterpret_cast<float2*>(p + 16 + slices * sizeof(double));
+  subspec::verify_workspace(&a, ws);
   a.path = path;
   a.accepted = accepted;
   a.next_token = next_token;

@@ -19,9 +19,12 @@ struct VerifyArgs {
   float c;                 // log2(e) / T
   double inv_t;            // 1 / T
   int chunks, chunk_len;   // workgroups per row and the logits each one covers
-  unsigned* cnt;           // completion counter (zero between launches)
+  // workspace
+  unsigned* cnt;           // completion counters (zero between launches): the residual's slices, rows, slices of each row
   float2* stat;            // [N + 1][chunks] maximum, and sum of 2^(c (l - maximum)) (greedy: the maximum's token)
-  float2* row_stat;        // [1] the last row's maximum and sum
+  float2* row_stat;        // [N + 1] the same of whole rows
+  int* next;               // [N + 1] the drafted token that a row picks, or -1
+  float2* last_stat;       // [1] row_stat of the path's last row
   int* last_row;           // [1]
   double* slice_sum;       // [ceil(V / kVerifySlice)] the last row's sums without its children
   int* path;               // [N]
@@ -31,6 +34,7 @@ struct VerifyArgs {
 
 void verify_plan(int N, int V, int* chunks, int* chunk_len);
 size_t verify_workspace_bytes(int N, int V);
+void verify_workspace(VerifyArgs* a, void* ws);  // fills the workspace's pointers; N, V and chunks are set
 hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t st);
 
 }  // namespace subspec

@@ -11,12 +11,11 @@
 // All rows are read at once, although only those on the path matter, because the path is
 // known only at its end: a row needs its maximum and its sum of exponentials to say which
 // child it picks, not the whole distribution.
-//   k_verify_rows     per (row, slice) workgroup the maximum and the sum, 32 bits
-//   k_verify_walk     one workgroup: every token's interval, then the path
-//   k_verify_residual the last row's other tokens in 64 bits: with V = 152064 tokens the
-//                     borders lie 10^-5 apart, and a sum in 32 bits, 10^-7 off, would pick a
-//                     neighbour in one call of a hundred; the last workgroup to finish finds
-//                     the token.
+//   k_verify_rows      per (row, slice) workgroup the maximum and the sum, in 32 bits; the last
+//                      of a row finds the child that the row picks, the last of all the path
+//   k_verify_residual  the last row's other tokens in 64 bits: with V = 152064 tokens the
+//                      borders lie 10^-5 apart, and a sum in 32 bits, 10^-7 off, would pick a
+//                      neighbour in one call of a hundred; the last workgroup finds the token
 #include <climits>
 #include <cmath>
 
@@ -56,70 +55,143 @@ __device__ __forceinline__ void merge(float c, float& m, float& s, float m2, flo
   m = mx;
 }
 
-__global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
-  __shared__ float wm[kRowWaves], ws[kRowWaves];
-  const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-  const int lo = chunk * a.chunk_len, hi = min(a.V, lo + a.chunk_len);
-  const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
-  float m = -INFINITY, s = 0.f;
-  for (int v0 = lo + 8 * static_cast<int>(threadIdx.x); v0 < hi; v0 += 8 * kRowThreads * kRowLoads) {
-    uint4 w[kRowLoads];
-#pragma unroll
-    for (int j = 0; j < kRowLoads; ++j) {
-      const int v = v0 + 8 * kRowThreads * j;
-      w[j] = v < hi ? *reinterpret_cast<const uint4*>(l + v) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
-    }
-#pragma unroll
-    for (int j = 0; j < kRowLoads; ++j) {
-      float x[8];
-      split8(w[j], x);
-      float mx = m;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
-      if (mx == -INFINITY) {  // nothing but -inf (or NaN, which the sum has to show)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += x[e] == x[e] ? 0.f : x[e];
-        continue;
-      }
-      s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(a.c * (m - mx));
-      m = mx;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(a.c * (x[e] - mx));
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) merge(a.c, m, s, __shfl_xor(m, d), __shfl_xor(s, d));
-  if (threadIdx.x % kWave == 0) {
-    wm[threadIdx.x / kWave] = m;
-    ws[threadIdx.x / kWave] = s;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    m = wm[0];
-    s = ws[0];
-#pragma unroll
-    for (int w = 1; w < kRowWaves; ++w) merge(a.c, m, s, wm[w], ws[w]);
-    a.stat[blockIdx.x] = make_float2(m, s);
-  }
-}
-
-// Greedy: the slice's largest logit and its lowest token; a NaN makes the row have none
-// (stored as NaN).
+// Greedy: the larger logit and of equals the lower token; a NaN (the row has none) stays.
 __device__ __forceinline__ void best_of(float& m, int& i, float m2, int i2) {
   const bool take = m != m ? false : m2 != m2 ? true : m2 > m || (m2 == m && i2 < i);
   m = take ? m2 : m;
   i = take ? i2 : i;
 }
 
-__global__ __launch_bounds__(kRowThreads) void k_verify_best(VerifyArgs a) {
-  __shared__ float wm[kRowWaves];
-  __shared__ int wi[kRowWaves];
+// What is kept of logits seen: (maximum, sum of 2^(c (l - maximum))), or greedy (maximum, token).
+template <bool GREEDY>
+struct Seen {
+  float m = -INFINITY;
+  float s = GREEDY ? __int_as_float(INT_MAX) : 0.f;
+
+  __device__ __forceinline__ void add(float c, const float (&x)[8], int v0) {
+    if constexpr (GREEDY) {
+      int i = __float_as_int(s);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        // a thread's tokens come in order: a later equal one does not replace
+        const bool take = x[e] > m || x[e] != x[e];
+        m = take && m == m ? x[e] : m;
+        i = take ? v0 + e : i;
+      }
+      s = __int_as_float(i);
+    } else {
+      float mx = m;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
+      if (mx == -INFINITY) {  // nothing but -inf (or NaN, which the sum has to show)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s += x[e] == x[e] ? 0.f : x[e];
+        return;
+      }
+      s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - mx));
+      m = mx;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(c * (x[e] - mx));
+    }
+  }
+
+  __device__ __forceinline__ void add(float c, float m2, float s2) {
+    if constexpr (GREEDY) {
+      int i = __float_as_int(s);
+      best_of(m, i, m2, __float_as_int(s2));
+      s = __int_as_float(i);
+    } else {
+      merge(c, m, s, m2, s2);
+    }
+  }
+
+  __device__ __forceinline__ void across_wave(float c) {
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) add(c, __shfl_xor(m, d), __shfl_xor(s, d));
+  }
+};
+
+// Stores that other XCDs' coherent loads see once they are acknowledged.
+__device__ __forceinline__ void put(int* p, int v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void put(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void put(float2* p, float x, float y) {
+  __hip_atomic_store(reinterpret_cast<unsigned long long*>(p),
+                     (static_cast<unsigned long long>(__float_as_uint(y)) << 32) | __float_as_uint(x), __ATOMIC_RELAXED,
+                     __HIP_MEMORY_SCOPE_AGENT);
+}
+template <typename T>
+__device__ __forceinline__ T get(const T* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get(const float2* p) {
+  const unsigned long long w =
+      __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return make_float2(__uint_as_float(static_cast<uint32_t>(w)), __uint_as_float(static_cast<uint32_t>(w >> 32)));
+}
+
+// Whether the calling workgroup is the `of`-th to arrive; it then clears the counter.  Every
+// wavefront's stores are acknowledged before it arrives.  (All threads call it.)
+__device__ __forceinline__ bool last_to_arrive(unsigned* cnt, unsigned of, int* flag) {
+  __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last = __hip_atomic_fetch_add(cnt, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
+    if (last) __hip_atomic_store(cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    *flag = last;
+  }
+  __syncthreads();
+  return *flag != 0;
+}
+
+// Token j continues `row` (a parent that does not come before it, or a token outside the
+// vocabulary, continues nothing).
+__device__ __forceinline__ bool continues(const VerifyArgs& a, int j, int row, int* token) {
+  const int p = a.parent[j], k = a.token[j];
+  *token = k;
+  return p + 1 == row && p >= -1 && p < j && k >= 0 && k < a.V;
+}
+
+struct Children {
+  int j[kVerifyMaxTokens];
+  int token[kVerifyMaxTokens];
+  float p[kVerifyMaxTokens];  // logits
+};
+struct Ordered {  // by index; a repeated token's share is 0
+  int j[kVerifyMaxTokens];
+  float p[kVerifyMaxTokens];
+};
+
+template <bool GREEDY>
+__global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
+  __shared__ Children kids;
+  __shared__ union {
+    Ordered order;
+    int next[kVerifyMaxTokens + 1];
+  } u;
+  __shared__ float wm[kRowWaves], ws[kRowWaves];
+  __shared__ int n, flag, pick;
+  const int t = threadIdx.x;
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
   const int lo = chunk * a.chunk_len, hi = min(a.V, lo + a.chunk_len);
   const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
-  float m = -INFINITY;
-  int i = INT_MAX;
-  for (int v0 = lo + 8 * static_cast<int>(threadIdx.x); v0 < hi; v0 += 8 * kRowThreads * kRowLoads) {
+  if (t == 0) {
+    n = 0;
+    pick = INT_MAX;
+  }
+  __syncthreads();
+  // the row's children, in any order; their logits arrive while the row streams
+  for (int j = t; j < a.N; j += kRowThreads) {
+    int k;
+    if (continues(a, j, row, &k)) {
+      const int at = atomicAdd(&n, 1);
+      kids.j[at] = j;
+      kids.token[at] = k;
+      kids.p[at] = __uint_as_float(static_cast<uint32_t>(l[k]) << 16);
+    }
+  }
+
+  Seen<GREEDY> seen;
+  for (int v0 = lo + 8 * t; v0 < hi; v0 += 8 * kRowThreads * kRowLoads) {
     uint4 w[kRowLoads];
 #pragma unroll
     for (int j = 0; j < kRowLoads; ++j) {
@@ -130,140 +202,103 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_best(VerifyArgs a) {
     for (int j = 0; j < kRowLoads; ++j) {
       float x[8];
       split8(w[j], x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        // within a thread the tokens come in order: a later equal one does not replace
-        const bool take = x[e] > m || x[e] != x[e];
-        m = take && m == m ? x[e] : m;
-        i = take ? v0 + 8 * kRowThreads * j + e : i;
-      }
+      seen.add(a.c, x, v0 + 8 * kRowThreads * j);
     }
   }
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) best_of(m, i, __shfl_xor(m, d), __shfl_xor(i, d));
-  if (threadIdx.x % kWave == 0) {
-    wm[threadIdx.x / kWave] = m;
-    wi[threadIdx.x / kWave] = i;
+  seen.across_wave(a.c);
+  if (t % kWave == 0) {
+    wm[t / kWave] = seen.m;
+    ws[t / kWave] = seen.s;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    m = wm[0];
-    i = wi[0];
+  seen.m = wm[0];
+  seen.s = ws[0];
 #pragma unroll
-    for (int w = 1; w < kRowWaves; ++w) best_of(m, i, wm[w], wi[w]);
-    a.stat[blockIdx.x] = make_float2(m, __int_as_float(i));
-  }
-}
-
-constexpr int kWalkThreads = 1024;
-
-__global__ __launch_bounds__(kWalkThreads) void k_verify_walk(VerifyArgs a) {
-  __shared__ float rm[kVerifyMaxTokens + 1], rs[kVerifyMaxTokens + 1];  // rows' maxima and sums (greedy: tokens)
-  __shared__ float pj[kVerifyMaxTokens];
-  __shared__ int par[kVerifyMaxTokens], tok[kVerifyMaxTokens], next[kVerifyMaxTokens + 1];
-  const int t = threadIdx.x;
-  for (int r = t; r <= a.N; r += kWalkThreads) {
-    float2 st = a.stat[static_cast<size_t>(r) * a.chunks];
-    if (a.greedy) {
-      int i = __float_as_int(st.y);
-      for (int c = 1; c < a.chunks; ++c) {
-        const float2 o = a.stat[static_cast<size_t>(r) * a.chunks + c];
-        best_of(st.x, i, o.x, __float_as_int(o.y));
+  for (int w = 1; w < kRowWaves; ++w) seen.add(a.c, wm[w], ws[w]);
+  if (a.chunks > 1) {
+    if (t == 0) put(a.stat + blockIdx.x, seen.m, seen.s);
+    if (!last_to_arrive(a.cnt + 2 + row, a.chunks, &flag)) return;
+    // every wavefront merges the row's slices, in the same order
+    seen = Seen<GREEDY>();
+    for (int c0 = 0; c0 < a.chunks; c0 += kWave) {
+      const int c = c0 + t % kWave;
+      Seen<GREEDY> part;
+      if (c < a.chunks) {
+        const float2 st = get(a.stat + static_cast<size_t>(row) * a.chunks + c);
+        part.m = st.x;
+        part.s = st.y;
       }
-      // no finite largest logit: nothing is picked
-      rs[r] = __int_as_float(fabsf(st.x) < INFINITY ? i : -1);
-    } else {
-      for (int c = 1; c < a.chunks; ++c) {
-        const float2 o = a.stat[static_cast<size_t>(r) * a.chunks + c];
-        merge(a.c, st.x, st.y, o.x, o.y);
-      }
-      const bool ok = fabsf(st.x) < INFINITY && st.y > 0.f && st.y < INFINITY;
-      rm[r] = st.x;
-      rs[r] = ok ? st.y : 0.f;
+      part.across_wave(a.c);
+      seen.add(a.c, part.m, part.s);
     }
-    next[r] = -1;
   }
-  if (t < a.N) {
-    const int p = a.parent[t], k = a.token[t];
-    // a parent that does not come before its child, or a token outside the vocabulary: never accepted
-    const bool ok = p >= -1 && p < t && k >= 0 && k < a.V;
-    par[t] = ok ? p : -2;
-    tok[t] = k;
-  }
-  __syncthreads();
-  const bool ok = t < a.N && par[t] != -2;
-  const int row = ok ? par[t] + 1 : 0;
-  if (a.greedy) {
-    if (ok && tok[t] == __float_as_int(rs[row])) {
-      bool first = true;  // of equal siblings the first
-      for (int i = 0; i < t; ++i) first &= !(par[i] == par[t] && tok[i] == tok[t]);
-      if (first) next[row] = t;
+
+  // The row's pick among its children.
+  const int nk = n;
+  const int best = GREEDY ? __float_as_int(seen.s) : 0;
+  const bool ok = fabsf(seen.m) < INFINITY && (GREEDY || (seen.s > 0.f && seen.s < INFINITY));
+  if (ok) {
+    for (int k = t; k < nk; k += kRowThreads) {
+      const int j = kids.j[k], token = kids.token[k];
+      if constexpr (GREEDY) {
+        if (token == best) atomicMin(&pick, j);  // of equal siblings the first
+      } else {
+        int rank = 0;
+        bool repeat = false;
+        for (int i = 0; i < nk; ++i) {
+          const bool before = kids.j[i] < j;
+          rank += before;
+          repeat |= before && kids.token[i] == token;
+        }
+        u.order.j[rank] = j;
+        u.order.p[rank] = repeat ? 0.f : __builtin_amdgcn_exp2f(a.c * (kids.p[k] - seen.m)) / seen.s;
+      }
     }
     __syncthreads();
-  } else {
-    float p = 0.f;
-    if (ok && rs[row] > 0.f) {
-      const uint32_t bits = a.logits[static_cast<size_t>(row) * a.V + tok[t]];
-      p = __builtin_amdgcn_exp2f(a.c * (__uint_as_float(bits << 16) - rm[row])) / rs[row];
-    }
-    if (t < a.N) {
-      for (int i = 0; i < t; ++i)
-        if (ok && par[i] == par[t] && tok[i] == tok[t]) p = 0.f;
-      pj[t] = p;
-    }
-    __syncthreads();
-    if (p > 0.f) {
+    if (!GREEDY && t == 0) {
+      const float at = a.uniform[row];
       float f = 0.f;
-      for (int i = 0; i < t; ++i)
-        if (par[i] == par[t]) f += pj[i];
-      const float u = a.uniform[row];
-      if (f <= u && u < f + p) next[row] = t;
+      for (int k = 0; k < nk; ++k) {
+        const float f2 = f + u.order.p[k];
+        if (f <= at && at < f2) {
+          pick = u.order.j[k];
+          break;
+        }
+        f = f2;
+      }
     }
-    __syncthreads();
   }
   if (t == 0) {
-    int r = 0, n = 0;
-    for (int j; (j = next[r]) >= 0; r = j + 1) a.path[n++] = j;  // j >= r: it ends
-    *a.accepted = n;
-    par[0] = n;
-    if (a.greedy) {
-      *a.next_token = __float_as_int(rs[r]);
+    put(a.next + row, pick == INT_MAX ? -1 : pick);
+    // a row without a distribution: no sum, or no token
+    put(a.row_stat + row, seen.m, GREEDY ? __int_as_float(ok ? best : -1) : ok ? seen.s : 0.f);
+  }
+  if (!last_to_arrive(a.cnt + 1, a.N + 1, &flag)) return;
+
+  // The path.
+  for (int r = t; r <= a.N; r += kRowThreads) u.next[r] = get(a.next + r);
+  __syncthreads();
+  if (t == 0) {
+    int r = 0, len = 0;
+    for (int j; (j = u.next[r]) >= 0; r = j + 1) a.path[len++] = j;  // j >= r: it ends
+    *a.accepted = len;
+    n = len;
+    const float2 st = get(a.row_stat + r);
+    if constexpr (GREEDY) {
+      *a.next_token = __float_as_int(st.y);
     } else {
       *a.last_row = r;
-      *a.row_stat = make_float2(rm[r], rs[r]);
+      *a.last_stat = st;
     }
   }
   __syncthreads();
-  for (int i = t; i < a.N; i += kWalkThreads)
-    if (i >= par[0]) a.path[i] = -1;
+  for (int i = n + t; i < a.N; i += kRowThreads) a.path[i] = -1;
 }
 
 constexpr int kResThreads = 256;
+constexpr int kResWaves = kResThreads / kWave;
 static_assert(kVerifySlice == 8 * kResThreads, "eight logits a thread");
-
-struct Residual {
-  int kids[kVerifyMaxTokens];  // the last row's drafted tokens
-  int n, last;
-  double sum[kResThreads / kWave];
-};
-
-// e^((l - m) / T) of this thread's 8 logits of a slice, drafted tokens and logits past the
-// vocabulary zero.
-__device__ __forceinline__ void residual_terms(const VerifyArgs& a, const Residual& sh, const uint16_t* l, float m, int v0,
-                                               double (&e)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = 0.0;
-  if (v0 >= a.V) return;
-  float x[8];
-  split8(*reinterpret_cast<const uint4*>(l + v0), x);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = exp((static_cast<double>(x[i]) - static_cast<double>(m)) * a.inv_t);
-  for (int k = 0; k < sh.n; ++k) {
-    const int d = sh.kids[k] - v0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = d == i ? 0.0 : e[i];
-  }
-}
+constexpr int kSlices = kVerifyMaxV / kVerifySlice / kWave;  // sums of slices a lane
 
 __device__ __forceinline__ double wave_add(double v) {
 #pragma unroll
@@ -271,137 +306,163 @@ __device__ __forceinline__ double wave_add(double v) {
   return v;
 }
 
-// The first of the workgroup's terms (K a thread, in order, the first of thread 0's with
-// number `first`) whose running sum passes `target`; if none does, the last positive one; -1 if
-// no term is positive.  Every thread gets the number, and in *before the sum of the terms in
-// front of it.
+// Within a wavefront whose lanes hold K terms each, in order, the first of which has number
+// `first` in lane 0: the number of the first term whose running sum (on top of `start`)
+// passes `target`, or of the last positive one if none does (-1 if none is); in *before the
+// sum in front of it.  The same in every lane.
 template <int K>
-__device__ int find_term(const double (&e)[K], int first, double target, double* wsum, int* found, double* before) {
-  const int t = threadIdx.x;
+__device__ __forceinline__ int find_term(const double (&e)[K], int first, double start, double target, double* before) {
+  const int lane = threadIdx.x % kWave;
   double own = 0.0;
 #pragma unroll
   for (int i = 0; i < K; ++i) own += e[i];
-  double incl = own;  // inclusive sum over the wavefront's lanes
+  double run = own;
 #pragma unroll
   for (int d = 1; d < kWave; d *= 2) {
-    const double o = __shfl_up(incl, d);
-    if (t % kWave >= d) incl += o;
+    const double o = __shfl_up(run, d);
+    if (lane >= d) run += o;
   }
-  if (t % kWave == kWave - 1) wsum[t / kWave] = incl;
-  if (t < 2) found[t] = t == 0 ? INT_MAX : -1;
-  __syncthreads();
-  double run = incl - own;
-  for (int w = 0; w < t / kWave; ++w) run += wsum[w];
-  const double start = run;
-  int hit = INT_MAX, any = -1;
+  run = start + (run - own);
+  int hit = -1, any = -1;
+  double hit_before = 0.0, any_before = 0.0;
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    run += e[i];
+    const double up = run + e[i];
     if (e[i] > 0.0) {
-      any = first + K * t + i;
-      if (run > target && hit == INT_MAX) hit = any;
+      any = first + K * lane + i;
+      any_before = run;
+      if (up > target && hit < 0) {
+        hit = any;
+        hit_before = run;
+      }
     }
+    run = up;
   }
-  if (hit != INT_MAX) atomicMin(&found[0], hit);
-  if (any >= 0) atomicMax(&found[1], any);
-  __syncthreads();
-  const int r = found[0] != INT_MAX ? found[0] : found[1];
-  const int mine = r - (first + K * t);
-  if (mine >= 0 && mine < K) {
-    run = start;
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-      if (i < mine) run += e[i];
-    wsum[0] = run;
-  }
-  __syncthreads();
-  *before = wsum[0];
-  __syncthreads();
-  return r;
+  const unsigned long long hits = __ballot(hit >= 0), some = __ballot(any >= 0);
+  if (hits == 0 && some == 0) return -1;
+  const int from = hits ? __ffsll(hits) - 1 : 63 - __clzll(static_cast<long long>(some));
+  *before = __shfl(hits ? hit_before : any_before, from);
+  return __shfl(hits ? hit : any, from);
 }
 
-// The threads' sum, in a fixed order, in every thread.
-__device__ double block_add(double v, double* wsum) {
-  v = wave_add(v);
-  if (threadIdx.x % kWave == 0) wsum[threadIdx.x / kWave] = v;
-  __syncthreads();
-  v = wsum[0];
+// e^((l - m) / T) of this thread's 8 logits, drafted tokens and logits past the vocabulary zero.
+__device__ __forceinline__ void residual_terms(const VerifyArgs& a, const int* kids, int n, const uint16_t* l, float m,
+                                               int v0, double (&e)[8]) {
 #pragma unroll
-  for (int w = 1; w < kResThreads / kWave; ++w) v += wsum[w];
-  __syncthreads();
-  return v;
-}
-
-__device__ __forceinline__ bool is_child(const VerifyArgs& a, int j, int row) {
-  const int p = a.parent[j], k = a.token[j];
-  return p + 1 == row && p >= -1 && p < j && k >= 0 && k < a.V;
+  for (int i = 0; i < 8; ++i) e[i] = 0.0;
+  if (v0 >= a.V) return;
+  float x[8];
+  split8(*reinterpret_cast<const uint4*>(l + v0), x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = exp((static_cast<double>(x[i]) - static_cast<double>(m)) * a.inv_t);
+  for (int k = 0; k < n; ++k) {
+    const int d = kids[k] - v0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = d == i ? 0.0 : e[i];
+  }
 }
 
 __global__ __launch_bounds__(kResThreads) void k_verify_residual(VerifyArgs a) {
-  __shared__ Residual sh;
-  __shared__ int found[2];
-  const int t = threadIdx.x;
+  __shared__ int kid_j[kVerifyMaxTokens], kid[kVerifyMaxTokens];  // the row's drafted tokens
+  __shared__ double part[2][kResWaves], share[kVerifyMaxTokens];
+  __shared__ int n, flag;
+  const int t = threadIdx.x, wave = t / kWave;
   const int row = *a.last_row;
-  const float2 st = *a.row_stat;
+  const float2 st = *a.last_stat;
   if (!(st.y > 0.f)) {  // no distribution (the same for every workgroup)
     if (blockIdx.x == 0 && t == 0) *a.next_token = -1;
     return;
   }
-  if (t == 0) sh.n = 0;
+  if (t == 0) n = 0;
   __syncthreads();
-  for (int j = t; j < a.N; j += kResThreads)
-    if (is_child(a, j, row)) sh.kids[atomicAdd(&sh.n, 1)] = a.token[j];  // in any order
+  for (int j = t; j < a.N; j += kResThreads) {
+    int k;
+    if (continues(a, j, row, &k)) {
+      const int at = atomicAdd(&n, 1);
+      kid_j[at] = j;
+      kid[at] = k;
+    }
+  }
   __syncthreads();
   const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
   double e[8];
-  residual_terms(a, sh, l, st.x, blockIdx.x * kVerifySlice + 8 * t, e);
+  residual_terms(a, kid, n, l, st.x, blockIdx.x * kVerifySlice + 8 * t, e);
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) s += e[i];
-  s = block_add(s, sh.sum);
-  if (t == 0) {
-    __hip_atomic_store(a.slice_sum + blockIdx.x, s, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    // the sum is out before the counter says so
-    sh.last = __hip_atomic_fetch_add(a.cnt, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-  }
+  s = wave_add(s);
+  if (t % kWave == 0) part[0][wave] = s;
   __syncthreads();
-  if (!sh.last) return;
-
-  // The last workgroup: the drafted tokens' share (each once), the slice, the token.
-  double drafted = 0.0;
-  for (int j = t; j < a.N; j += kResThreads) {
-    if (!is_child(a, j, row)) continue;
-    const int k = a.token[j];
-    bool once = true;
-    for (int i = 0; i < j && once; ++i) once = !(is_child(a, i, row) && a.token[i] == k);
-    if (once)
-      drafted += exp((static_cast<double>(__uint_as_float(static_cast<uint32_t>(l[k]) << 16)) - static_cast<double>(st.x)) * a.inv_t);
+  if (t == 0) {
+    s = part[0][0];
+#pragma unroll
+    for (int w = 1; w < kResWaves; ++w) s += part[0][w];
+    put(a.slice_sum + blockIdx.x, s);
   }
-  drafted = block_add(drafted, sh.sum);
-  constexpr int kSlices = kVerifyMaxV / kVerifySlice / kResThreads;  // a thread
-  double x[kSlices], mine = 0.0;
+  if (!last_to_arrive(a.cnt, gridDim.x, &flag)) return;
+
+  // The last workgroup: the drafted tokens' share (each token once, summed in index order),
+  // the slice, the token.  Every wavefront finds the slice itself.
+  double x[kSlices], rest = 0.0;
 #pragma unroll
   for (int i = 0; i < kSlices; ++i) {
-    const int at = kSlices * t + i;
-    x[i] = at < static_cast<int>(gridDim.x) ? __hip_atomic_load(a.slice_sum + at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-    mine += x[i];
+    const int at = kSlices * (t % kWave) + i;
+    x[i] = at < static_cast<int>(gridDim.x) ? get(a.slice_sum + at) : 0.0;
+    rest += x[i];
   }
-  const double rest = block_add(mine, sh.sum);
+  rest = wave_add(rest);
+  // in index order, whatever order they were found in
+  for (int k = t; k < n; k += kResThreads) {
+    int rank = 0;
+    bool repeat = false;
+    for (int i = 0; i < n; ++i) {
+      const bool first = kid_j[i] < kid_j[k];
+      rank += first;
+      repeat |= first && kid[i] == kid[k];
+    }
+    share[rank] = repeat ? 0.0
+                         : exp((static_cast<double>(__uint_as_float(static_cast<uint32_t>(l[kid[k]]) << 16)) -
+                                static_cast<double>(st.x)) * a.inv_t);
+  }
+  __syncthreads();
+  double drafted = 0.0;
+  for (int k = t % kWave; k < n; k += kWave) drafted += share[k];
+  drafted = wave_add(drafted);
   int token = -1;
   if (rest > 0.0) {
     const double target = fmax(static_cast<double>(a.uniform[row]) * (rest + drafted) - drafted, 0.0);
     double before = 0.0, unused;
-    const int slice = find_term(x, 0, target, sh.sum, found, &before);
-    residual_terms(a, sh, l, st.x, slice * kVerifySlice + 8 * t, e);
-    token = find_term(e, slice * kVerifySlice, target - before, sh.sum, found, &unused);
-  } else {
-    // the drafted tokens hold everything, and rounding kept u from all of them: the last of them
-    for (int i = 0; i < sh.n; ++i)
-      if (__uint_as_float(static_cast<uint32_t>(l[sh.kids[i]]) << 16) > -INFINITY) token = max(token, sh.kids[i]);
+    const int slice = find_term(x, 0, 0.0, target, &before);
+    residual_terms(a, kid, n, l, st.x, slice * kVerifySlice + 8 * t, e);
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s += e[i];
+    s = wave_add(s);
+    if (t % kWave == 0) part[1][wave] = s;
+    __syncthreads();
+    // The wavefront in whose share the target falls, or the last with a share.
+    double start = before;
+    int owner = -1;
+    double owner_start = 0.0;
+    for (int w = 0; w < kResWaves; ++w) {
+      const double up = start + part[1][w];
+      if (part[1][w] > 0.0) {
+        owner = w;
+        owner_start = start;
+        if (up > target) break;
+      }
+      start = up;
+    }
+    if (wave != owner) return;
+    token = find_term(e, slice * kVerifySlice + 8 * kWave * wave, owner_start, target, &unused);
+    if (t % kWave == 0) *a.next_token = token;
+    return;
   }
+  // The drafted tokens hold everything, and rounding kept u from all of them: the last of them.
   if (t == 0) {
+    for (int i = 0; i < n; ++i)
+      if (__uint_as_float(static_cast<uint32_t>(l[kid[i]]) << 16) > -INFINITY) token = max(token, kid[i]);
     *a.next_token = token;
-    __hip_atomic_store(a.cnt, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
 }
 
@@ -418,24 +479,34 @@ void verify_plan(int N, int V, int* chunks, int* chunk_len) {
 }
 
 // After the completion counters: the last row and its (maximum, sum), the slices' sums,
-// the rows' pairs.
+// the rows' (maximum, sum) pairs, the slices' of rows, the rows' picks.
 size_t verify_workspace_bytes(int N, int V) {
   int chunks = 0, len = 0;
   verify_plan(N, V, &chunks, &len);
   const size_t slices = (V + kVerifySlice - 1) / kVerifySlice;
-  return kSplitCounterBytes + 16 + slices * sizeof(double) + static_cast<size_t>(N + 1) * chunks * sizeof(float2);
+  return kSplitCounterBytes + 16 + slices * sizeof(double) + static_cast<size_t>(N + 1) * (1 + chunks) * sizeof(float2) +
+         static_cast<size_t>(N + 1) * sizeof(int);
+}
+
+void verify_workspace(VerifyArgs* a, void* ws) {
+  char* p = static_cast<char*>(ws);
+  a->cnt = reinterpret_cast<unsigned*>(p);
+  p += kSplitCounterBytes;
+  a->last_row = reinterpret_cast<int*>(p);
+  a->last_stat = reinterpret_cast<float2*>(p + 8);
+  a->slice_sum = reinterpret_cast<double*>(p + 16);
+  a->row_stat = reinterpret_cast<float2*>(a->slice_sum + (a->V + kVerifySlice - 1) / kVerifySlice);
+  a->stat = a->row_stat + (a->N + 1);
+  a->next = reinterpret_cast<int*>(a->stat + static_cast<size_t>(a->N + 1) * a->chunks);
 }
 
 hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t st) {
   const dim3 rows((a.N + 1) * a.chunks);
   if (a.greedy)
-    hipLaunchKernelGGL(k_verify_best, rows, dim3(kRowThreads), 0, st, a);
+    hipLaunchKernelGGL(k_verify_rows<true>, rows, dim3(kRowThreads), 0, st, a);
   else
-    hipLaunchKernelGGL(k_verify_rows, rows, dim3(kRowThreads), 0, st, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_verify_walk, dim3(1), dim3(kWalkThreads), 0, st, a);
-  e = hipGetLastError();
+    hipLaunchKernelGGL(k_verify_rows<false>, rows, dim3(kRowThreads), 0, st, a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.greedy) return e;
   hipLaunchKernelGGL(k_verify_residual, dim3((a.V + kVerifySlice - 1) / kVerifySlice), dim3(kResThreads), 0, st, a);
   return hipGetLastError();

@@ -82,6 +82,17 @@ def test_tree_verify_accepts_long_paths():
     assert len(path) == N
 
 
+@pytest.mark.parametrize("N,V", [(1024, 2048), (700, 152064)])
+def test_tree_verify_one_row_with_many_children(N, V):
+    rng = np.random.default_rng(N)
+    logits = rng.standard_normal((N + 1, V), dtype=np.float32)
+    token = rng.integers(0, min(V, 1500), N)  # many of them drafted twice
+    for seed in range(3):
+        u = np.random.default_rng([N, seed]).random(N + 1, dtype=np.float32)
+        _check(_bf16(logits), np.full(N, -1), token, u, 1.0)
+    _check(_bf16(logits), np.full(N, -1), token, None, 0.0)
+
+
 def test_tree_verify_uniform_numbers_across_a_row():
     """Every pick of a row: numbers over [0, 1) choose drafted tokens, in index order, then the
     others in token order, with the row's probabilities."""

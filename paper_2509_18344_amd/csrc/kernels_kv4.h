@@ -26,10 +26,11 @@ struct Kv4RowsArgs {
   uint8_t* v_cache;
   uint16_t* k_out;    // read: bf16 [n][Hkv][128]
   uint16_t* v_out;
+  bool heads_first;   // grid (heads, tiles); set by the launchers
 };
 
-hipError_t launch_kv4_append(const Kv4RowsArgs& a, int groups, hipStream_t st);
-hipError_t launch_kv4_read(const Kv4RowsArgs& a, int groups, hipStream_t st);
+hipError_t launch_kv4_append(Kv4RowsArgs a, int groups, hipStream_t st);
+hipError_t launch_kv4_read(Kv4RowsArgs a, int groups, hipStream_t st);
 
 struct Kv4AttnArgs {
   const uint16_t* q;       // bf16 [M][Hq][128]

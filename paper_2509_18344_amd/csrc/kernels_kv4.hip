@@ -14,19 +14,18 @@ constexpr int kKv4Threads = 256;
 
 template <int G>
 __global__ __launch_bounds__(kKv4Threads) void k_kv4_append(Kv4RowsArgs a) {
-  __shared__ alignas(16) uint8_t lds[kKv4Tile][kKv4LdsRow];
-  __shared__ uint32_t live;
-  const int tile = a.pos / kKv4Tile + blockIdx.x, g = blockIdx.y;
+  __shared__ Kv4TileLds lds;
+  const int tile = a.pos / kKv4Tile + (a.heads_first ? blockIdx.y : blockIdx.x), g = a.heads_first ? blockIdx.x : blockIdx.y;
   const int n = a.count ? min(max(*a.count, 0), a.n) : a.n;
   if (tile * kKv4Tile - a.pos >= n) return;  // no position of this tile is written
   const size_t at = (static_cast<size_t>(g) * (a.S / kKv4Tile) + tile) * kv4_tile_bytes(G);
-  kv4_store_tile<G>(a.k_cache + at, a.v_cache + at, lds, &live, [&](int w, int col, bool value, float (&x)[8]) {
+  kv4_store_tile<G>(a.k_cache + at, a.v_cache + at, lds, [&](int w, int col, bool value, uint4& x) {
     const int i = tile * kKv4Tile + w - a.pos;
     if (i < 0 || i >= n) return false;
     const int src = a.rows ? a.rows[i] : i;
     if (src < 0 || src >= a.src_rows) return false;
     const uint16_t* row = (value ? a.v : a.k) + (static_cast<size_t>(src) * a.Hkv + g) * kKv4D + 8 * col;
-    unpack8(*reinterpret_cast<const uint4*>(row), x);
+    x = *reinterpret_cast<const uint4*>(row);
     return true;
   });
 }
@@ -40,8 +39,8 @@ __device__ __forceinline__ uint4 kv4_values8(const uint32_t (&code)[8], float s,
 
 template <int G>
 __global__ __launch_bounds__(kKv4Threads) void k_kv4_read(Kv4RowsArgs a) {
-  __shared__ alignas(16) uint8_t lds[kKv4Tile][kKv4LdsRow];
-  const int tile = a.pos / kKv4Tile + blockIdx.x, g = blockIdx.y;
+  __shared__ alignas(16) uint8_t lds[kKv4Tile][kKv4D + 16];
+  const int tile = a.pos / kKv4Tile + (a.heads_first ? blockIdx.y : blockIdx.x), g = a.heads_first ? blockIdx.x : blockIdx.y;
   const size_t at = (static_cast<size_t>(g) * (a.S / kKv4Tile) + tile) * kv4_tile_bytes(G);
   const uint8_t* kt = a.k_cache + at;
   const uint8_t* vt = a.v_cache + at;
@@ -80,26 +79,31 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_read(Kv4RowsArgs a) {
   }
 }
 
-dim3 tiles_of(const Kv4RowsArgs& a) {
-  const int first = a.pos / kKv4Tile, last = (a.pos + a.n - 1) / kKv4Tile;
-  return dim3(last - first + 1, a.Hkv);
+// The heads of a tile next to each other in the order of launch, where the grid allows: their
+// rows of k and v are neighbours in memory.
+dim3 kv4_grid(Kv4RowsArgs* a) {
+  const unsigned tiles = (a->pos + a->n - 1) / kKv4Tile - a->pos / kKv4Tile + 1;
+  a->heads_first = tiles <= 65535;
+  return a->heads_first ? dim3(a->Hkv, tiles) : dim3(tiles, a->Hkv);
 }
 
 }  // namespace
 
-hipError_t launch_kv4_append(const Kv4RowsArgs& a, int groups, hipStream_t st) {
+hipError_t launch_kv4_append(Kv4RowsArgs a, int groups, hipStream_t st) {
+  const dim3 grid = kv4_grid(&a);
   if (groups == 1)
-    hipLaunchKernelGGL(k_kv4_append<1>, tiles_of(a), dim3(kKv4Threads), 0, st, a);
+    hipLaunchKernelGGL(k_kv4_append<1>, grid, dim3(kKv4Threads), 0, st, a);
   else
-    hipLaunchKernelGGL(k_kv4_append<2>, tiles_of(a), dim3(kKv4Threads), 0, st, a);
+    hipLaunchKernelGGL(k_kv4_append<2>, grid, dim3(kKv4Threads), 0, st, a);
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_read(const Kv4RowsArgs& a, int groups, hipStream_t st) {
+hipError_t launch_kv4_read(Kv4RowsArgs a, int groups, hipStream_t st) {
+  const dim3 grid = kv4_grid(&a);
   if (groups == 1)
-    hipLaunchKernelGGL(k_kv4_read<1>, tiles_of(a), dim3(kKv4Threads), 0, st, a);
+    hipLaunchKernelGGL(k_kv4_read<1>, grid, dim3(kKv4Threads), 0, st, a);
   else
-    hipLaunchKernelGGL(k_kv4_read<2>, tiles_of(a), dim3(kKv4Threads), 0, st, a);
+    hipLaunchKernelGGL(k_kv4_read<2>, grid, dim3(kKv4Threads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -54,48 +54,59 @@ __device__ __forceinline__ float2 rope_cos_sin(int position, double inv_freq) {
   return make_float2(c, s);
 }
 
-// One head row, dimensions 8 col .. 8 col + 7 in x (bias already added): x / sqrt(mean x^2
-// + eps) * w if `w` is not null, then the rotation of the first `rot` dimensions (a
-// multiple of 16).  cs: cos and sin of the rot / 2 frequencies.  Every lane of a row's 16 calls
-// it.
-__device__ __forceinline__ void rope_row(float (&x)[8], int col, const uint16_t* w, float eps, int rot, int interleaved,
-                                         const float2* cs) {
-  if (w) {
-    float sq = 0.f;
+// What a lane needs of its token's angles: for its 8 dimensions x the rotated value is
+// x cos + partner sin, where the partner's sign is in sin.
+struct RopeTurn {
+  float c[8], s[8];
+};
+
+// cs: cos and sin of the rot / 2 frequencies.  Pairs are (d, d + rot / 2), the partner rot / 16
+// lanes away, or (interleaved) neighbours in the lane.  Past `rot` the turn is none.
+__device__ __forceinline__ RopeTurn rope_turn(int col, int rot, int interleaved, const float2* cs) {
+  RopeTurn t;
+  const int chunks = rot / 8, h = chunks / 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sq += x[i] * x[i];
-    const float r = 1.f / sqrtf(row_sum16(sq) * (1.f / kRopeD) + eps);
-    float wf[8];
-    unpack8(*reinterpret_cast<const uint4*>(w + 8 * col), wf);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = x[i] * r * wf[i];
+  for (int i = 0; i < 8; ++i) {
+    const bool turned = col < chunks;
+    const bool first = interleaved ? i % 2 == 0 : col < h;
+    const int f = interleaved ? 4 * col + i / 2 : 8 * (first ? col : col - h) + i;
+    const float2 v = cs[turned ? f : 0];
+    t.c[i] = turned ? v.x : 1.f;
+    t.s[i] = turned ? (first ? -v.y : v.y) : 0.f;
   }
-  const int chunks = rot / 8;  // lanes that hold rotated dimensions
-  if (interleaved) {
-    if (col < chunks) {
+  return t;
+}
+
+// x / sqrt(mean x^2 + eps) * w over a head row, 16 lanes of 8 dimensions; w: this lane's weights.
+__device__ __forceinline__ void rope_norm(float (&x)[8], const float (&w)[8], float eps) {
+  float sq = 0.f;
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        const float2 t = cs[4 * col + p];
-        const float a = x[2 * p], b = x[2 * p + 1];
-        x[2 * p] = a * t.x - b * t.y;
-        x[2 * p + 1] = b * t.x + a * t.y;
-      }
-    }
-  } else if (rot) {
-    // pairs (d, d + rot / 2): the partner's dimensions are rot / 16 lanes away
-    const int h = chunks / 2;
-    const bool first = col < h;
-    const int lane = threadIdx.x % kWave;
-    const int from = col < chunks ? (first ? lane + h : lane - h) : lane;
+  for (int i = 0; i < 8; ++i) sq = __builtin_fmaf(x[i], x[i], sq);
+  const float r = rsqrtf(row_sum16(sq) * (1.f / kRopeD) + eps);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float other = __shfl(x[i], from);
-      if (col < chunks) {
-        const float2 t = cs[8 * (first ? col : col - h) + i];
-        x[i] = first ? x[i] * t.x - other * t.y : x[i] * t.x + other * t.y;
-      }
-    }
+  for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
+}
+
+// The rotation of a head row.  FULL: all 128 dimensions in pairs (d, d + 64), whose partner
+// is eight lanes away in the row of 16 (a DPP move instead of one through LDS).
+template <bool FULL>
+__device__ __forceinline__ void rope_rotate(float (&x)[8], int col, int rot, int interleaved, const RopeTurn& t) {
+  float other[8];
+  if constexpr (FULL) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      other[i] = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x[i]), 0x128, 0xF, 0xF, true));  // row_ror:8
+  } else if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) other[i] = x[i ^ 1];
+  } else {
+    const int chunks = rot / 8, h = chunks / 2, lane = threadIdx.x % kWave;
+    const int from = col < chunks ? (col < h ? lane + h : lane - h) : lane;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) other[i] = __shfl(x[i], from);
   }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], t.c[i], other[i] * t.s[i]);
 }
 
 }  // namespace subspec

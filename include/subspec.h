@@ -511,7 +511,7 @@ int subspec_prefetch_acquire(subspec_prefetch* pf, long long ticket, hipStream_t
 int subspec_prefetch_release(subspec_prefetch* pf, long long ticket, hipStream_t compute);
 
 /* The per-device workspace.  subspec_qlinear, subspec_tree_expand and
- * subspec_tree_attention share one device buffer per device: its first 64 KiB are
+ * subspec_tree_attention (and the calls named below) share one device buffer per device: its first 64 KiB are
  * split-K completion counters (zero between calls), the rest is scratch for the call
  * in flight.  A call that needs more than the buffer holds grows it: hipMalloc of a
  * buffer at least twice as large, its counters zeroed on the call's stream, and a
@@ -521,7 +521,10 @@ int subspec_prefetch_release(subspec_prefetch* pf, long long ticket, hipStream_t
  * subspec_reserve while no captured graph is alive on the device, and when the
  * device's last captured graph is destroyed; both synchronise the device first.  A
  * call made after subspec_reserve(bytes) with a need of at most `bytes` neither
- * allocates, frees nor synchronises.
+ * allocates, frees nor synchronises.  subspec_tree_attention_kv4 and subspec_tree_verify
+ * use the same buffer; called while the caller captures the stream into a graph of its own,
+ * they keep it allocated until the process ends, and replays of such graphs must not overlap
+ * in time with each other or with other calls that use the workspace.
  *
  * subspec_reserve: grow the calling device's workspace to at least `bytes` now
  * (synchronous; may call hipMalloc) and free retired buffers as above, so that later

@@ -676,7 +676,8 @@ struct Workspace {
   void* ptr = nullptr;
   size_t bytes = 0;
   int graphs = 0;                // live captured graphs made on this device
-  bool foreign = false;          // a graph that the caller captures holds one of the buffers
+  bool foreign = false;          // a graph that the caller captured holds `ptr`
+  std::vector<void*> kept;       // earlier buffers that such graphs hold: never freed
   std::vector<void*> retired;    // earlier buffers: queued kernels or graphs may still use them
   unsigned long long allocations = 0;
 };
@@ -696,7 +697,6 @@ Workspace& workspace_of(int dev) {  // caller holds g_ws_mutex
 
 // Frees the retired buffers of `w`; the caller has synchronised the device.
 int free_retired(Workspace& w) {
-  if (w.foreign) return SUBSPEC_OK;
   int rc = SUBSPEC_OK;
   for (void* p : w.retired) {
     const hipError_t e = hipFree(p);
@@ -711,8 +711,8 @@ int free_retired(Workspace& w) {
 // one), zeroes its completion counters on `st` and waits for that stream only.  The
 // old buffer is retired, not freed: kernels queued on other streams and captured
 // graphs may still use it.  Growth is refused while `st` is being captured.  note_capture:
-// a call inside the caller's own stream capture (the library never learns when that graph
-// ends) keeps every buffer of the device until the process ends.
+// a call inside the caller's own stream capture keeps its buffer until the process ends (the
+// library never learns when that graph does).
 int get_workspace(size_t bytes, hipStream_t st, void** out, bool note_capture = false) {
   int dev = 0;
   int rc = current_device(&dev);
@@ -749,7 +749,8 @@ int get_workspace(size_t bytes, hipStream_t st, void** out, bool note_capture = 
     (void)hipFree(p);
     return hip_fail(e, "zeroing the workspace counters");
   }
-  if (w.ptr) w.retired.push_back(w.ptr);
+  if (w.ptr) (w.foreign ? w.kept : w.retired).push_back(w.ptr);
+  w.foreign = false;
   w.ptr = p;
   w.bytes = nb;
   ++w.allocations;
@@ -1442,7 +1443,7 @@ int subspec_workspace_info(size_t* bytes, int* retired, unsigned long long* allo
   std::lock_guard<std::mutex> lock(g_ws_mutex);
   const Workspace& w = workspace_of(dev);
   if (bytes) *bytes = w.bytes;
-  if (retired) *retired = static_cast<int>(w.retired.size());
+  if (retired) *retired = static_cast<int>(w.retired.size() + w.kept.size());
   if (allocations) *allocations = w.allocations;
   return SUBSPEC_OK;
 }

@@ -1316,6 +1316,8 @@ int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v
   a.P = P;
   a.T = T;
   a.W = (T + M + 31) / 32;
+  a.Gq = Hq / Hkv;
+  a.inv_m = 1.f / static_cast<float>(M);
   // The kernel takes a positive factor: a negative scale flips q, and 2^-100 for 0 leaves
   // every score at 0 for any finite product.
   a.scale_log2 = std::max(c, 0x1p-100f);

@@ -38,6 +38,8 @@ struct Kv4AttnArgs {
   const uint8_t* v_cache;
   const uint32_t* mask;    // [M][W] bit rows over the tree positions
   int M, Hq, Hkv, S, P, T, W;
+  int Gq;                  // Hq / Hkv
+  float inv_m;             // 1 / M
   float scale_log2;        // |scale| * log2(e), positive
   uint32_t q_sign;         // 0x80008000 where the scale is negative: flips q's signs
   int splits;              // key ranges per key/value head

@@ -187,6 +187,10 @@ __device__ __forceinline__ void kv4_wave_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// row / M for a row below 64, from 1 / M: the quotient's distance to a whole number is at least
+// half of 1 / M before the 32-bit product's rounding.
+__device__ __forceinline__ int kv4_row_head(int row, float inv_m) { return static_cast<int>((static_cast<float>(row) + 0.5f) * inv_m); }
+
 // Query rows of one wavefront (QW tiles of 16) and what it has summed for them.
 template <int QW, int G>
 struct Kv4Rows {
@@ -202,14 +206,13 @@ struct Kv4Rows {
   u32x4_t raw[QW][4];
 
   __device__ __forceinline__ void request(const Kv4AttnArgs& a, int g, int row0, int lane) {
-    const int Gq = a.Hq / a.Hkv;
 #pragma unroll
     for (int t = 0; t < QW; ++t) {
       const int row = row0 + 16 * t + (lane & 15);
-      live[t] = row < Gq * a.M;
-      qi[t] = live[t] ? row % a.M : 0;
-      const int hl = live[t] ? row / a.M : 0;  // (a row past the last repeats the first)
-      const uint16_t* q = a.q + (static_cast<size_t>(qi[t]) * a.Hq + g * Gq + hl) * kKv4D + 8 * (lane >> 4);
+      live[t] = row < a.Gq * a.M;
+      const int hl = live[t] ? kv4_row_head(row, a.inv_m) : 0;  // (a row past the last repeats the first)
+      qi[t] = live[t] ? row - hl * a.M : 0;
+      const uint16_t* q = a.q + (static_cast<size_t>(qi[t]) * a.Hq + g * a.Gq + hl) * kKv4D + 8 * (lane >> 4);
 #pragma unroll
       for (int j = 0; j < 4; ++j) raw[t][j] = *reinterpret_cast<const u32x4_t*>(q + 32 * j);
     }
@@ -279,10 +282,11 @@ struct Kv4Rows {
     }
   }
 
-  __device__ __forceinline__ void mask(const Kv4AttnArgs& a, int key0, int total, int quarter, f32x4_t (&x)[QW][2]) const {
+  __device__ __forceinline__ void mask(const Kv4AttnArgs& a, const uint32_t* words, int key0, int total, int quarter,
+                                       f32x4_t (&x)[QW][2]) const {
 #pragma unroll
     for (int t = 0; t < QW; ++t) {
-      const uint32_t vis = live[t] ? kv4_visibility(a.mask + static_cast<size_t>(qi[t]) * a.W, a.W, a.P, key0, total) : 0u;
+      const uint32_t vis = live[t] ? kv4_visibility(words + qi[t] * a.W, a.W, a.P, key0, total) : 0u;
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -378,11 +382,12 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
   constexpr int KW = kWaves / QG;  // tiles of positions at a time
   constexpr int kThreads = kWaves * kWave;
   constexpr int kSlot = (2 * kv4_tile_bytes(G)) / 16;  // of a wavefront, in 16 bytes: key codes, value codes, their scales and minima
-  constexpr int kHalfRow = kKv4D / 2 + 4;               // floats of a merged half row of outputs
-  constexpr int kBuffer = kWaves * 16 * kHalfRow / 4;  // the wavefronts' half rows
-  static_assert(kRing * kWaves * kSlot >= 2 * kBuffer, "the merge fits the ring");
-  __shared__ u32x4_t lds[RING ? kRing * kWaves * kSlot : 2 * kBuffer];
-  __shared__ float Lm[kWaves][16 * QW], Ll[kWaves][16 * QW];
+  constexpr int kMergeRow = kKv4D + 4;                 // floats of an output row in the merge
+  constexpr int kMerge = kWaves * 16 * kMergeRow / 4;  // the wavefronts' outputs of a query tile, in 16 bytes
+  static_assert(kRing * kWaves * kSlot >= kMerge, "the merge fits the ring");
+  __shared__ u32x4_t lds[RING ? kRing * kWaves * kSlot : kMerge];
+  __shared__ float2 stat[kWaves][16 * QW];  // reference and sum of weights
+  __shared__ uint32_t words[kKv4MaskWords];
   const int s = blockIdx.x, g = blockIdx.y;
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x / kWave));
@@ -397,8 +402,27 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
   // the auxiliary product's first row is ones
   const uint32_t keep = col == 0 ? 0u : ~0u, ones = col == 0 ? 0x3C003C00u : 0u;
   Kv4Rows<QW, G> rows;
-  rows.request(a, g, 16 * QW * qg, lane);
   int n = first + kw;
+  // The masks, where the range has a tile that they have a say in: in LDS, since a load from
+  // memory in the loop would wait for every load before it.
+  const bool any_masked = last * kKv4Tile > a.P;  // the same for the whole workgroup
+  constexpr int kWords = kKv4MaskWords / kThreads;  // a thread
+  uint32_t own_words[kWords];
+  auto request_masks = [&]() __attribute__((always_inline)) {
+    if (any_masked)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        const int w = static_cast<int>(threadIdx.x) + i * kThreads;
+        own_words[i] = w < a.M * a.W ? a.mask[w] : 0u;
+      }
+  };
+  auto keep_masks = [&]() __attribute__((always_inline)) {
+    if (any_masked) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) words[threadIdx.x + i * kThreads] = own_words[i];
+      __syncthreads();
+    }
+  };
 
   if constexpr (RING) {
     constexpr int VM = 4 + G;  // vector memory operations of a tile's loads
@@ -425,9 +449,12 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       kv4_to_lds<16>(vt + l16, to + 2048);
       kv4_to_lds<16>(vt + next + l16, to + 2048 + 1024);
     };
+    rows.request(a, g, 16 * QW * qg, lane);
+    request_masks();
 #pragma unroll
     for (int i = 0; i < kRing - 1; ++i) request(i, n + i * KW);
     rows.begin(a);
+    keep_masks();
     for (int slot = 0; n < last; n += KW, slot = (slot + 1) % kRing) {
       // Into the slot whose tile the last step was done with, once that step's reads are back.
       __builtin_amdgcn_s_waitcnt(kKv4WaitLds);
@@ -461,7 +488,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       v.m = meta[8 * G + (col == 2 ? 2 * (G - 1) : 0) + 1];
       f32x4_t x[QW][2];
       rows.scores(k, x);
-      if (masked) rows.mask(a, key0, total, quarter, x);
+      if (masked) rows.mask(a, words, key0, total, quarter, x);
       rows.values(v, x, keep, ones);
     }
     asm volatile("" ::: "memory");
@@ -474,7 +501,10 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       kv4_load<G>(kbase + static_cast<size_t>(n) * kv4_tile_bytes(G), lane, k);
       kv4_load<G>(vbase + static_cast<size_t>(n) * kv4_tile_bytes(G), lane, v);
     }
+    rows.request(a, g, 16 * QW * qg, lane);
+    request_masks();
     rows.begin(a);
+    keep_masks();
     auto one_tile = [&](auto masked) __attribute__((always_inline)) {
       f32x4_t x[QW][2];
       rows.scores(k, x);
@@ -484,7 +514,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       else
         kv4_keep(k);
       if constexpr (decltype(masked)::value) {
-        rows.mask(a, n * kKv4Tile, total, quarter, x);
+        rows.mask(a, words, n * kKv4Tile, total, quarter, x);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
 #pragma unroll
@@ -504,63 +534,67 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
     while (n < last) one_tile(std::true_type{});
   }
 
-  // The workgroup's largest reference per row; every wavefront scales its outputs to it.
+  // The wavefronts' outputs, references and sums in LDS; then the workgroup scales and adds them in
+  // wavefront order, four dimensions of a row a thread.
   rows.finish(col);
-  if (quarter == 0)
-#pragma unroll
-    for (int t = 0; t < QW; ++t) Lm[wave][16 * t + col] = rows.ref[t];
-  __syncthreads();
+  float* merge = reinterpret_cast<float*>(lds);
+  const int nrows = a.Gq * a.M;
 #pragma unroll
   for (int t = 0; t < QW; ++t) {
-    float mall = -INFINITY;
+    if (t > 0) __syncthreads();
+    if (quarter == 0) stat[wave][16 * t + col] = make_float2(rows.ref[t], rows.aux[t][0]);
 #pragma unroll
-    for (int w = 0; w < KW; ++w) mall = fmaxf(mall, Lm[w * QG + qg][16 * t + col]);
-    const float sc = rows.ref[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(rows.ref[t] - mall);
+    for (int dt = 0; dt < 8; ++dt)
+      *reinterpret_cast<f32x4_t*>(merge + (wave * 16 + col) * kMergeRow + 16 * dt + 4 * quarter) = rows.o[t][dt];
+    __syncthreads();
+    for (int i = threadIdx.x; i < QG * 16 * (kKv4D / 4); i += kThreads) {
+      const int qw = i / (16 * (kKv4D / 4)), rr = i / (kKv4D / 4) % 16, d4 = 4 * (i % (kKv4D / 4));
+      const int row = 16 * (QW * qw + t) + rr;
+      if (row >= nrows) continue;  // padding rows are never read
+      float2 st[KW];
+      f32x4_t v[KW];
+      float top = -INFINITY, ls = 0.f;
 #pragma unroll
-    for (int dt = 0; dt < 8; ++dt) rows.o[t][dt] *= sc;
-    if (quarter == 0) Ll[wave][16 * t + col] = rows.aux[t][0] * sc;
-  }
-  // Half a query tile of every wavefront at a time (64 dimensions), in two buffers in turn: outputs
-  // [row][dimension] in LDS, then the workgroup adds the wavefronts' in order, four dimensions a thread.
-  const int nrows = a.Hq / a.Hkv * a.M;
-#pragma unroll
-  for (int t = 0; t < QW; ++t)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float* buf = reinterpret_cast<float*>(lds + h * kBuffer);
-#pragma unroll
-      for (int dt = 0; dt < 4; ++dt)
-        *reinterpret_cast<f32x4_t*>(buf + (wave * 16 + col) * kHalfRow + 16 * dt + 4 * quarter) = rows.o[t][4 * h + dt];
-      __syncthreads();
-      for (int i = threadIdx.x; i < QG * 16 * 16; i += kThreads) {
-        const int qw = i / 256, rr = i / 16 % 16, d4 = 4 * (i % 16);
-        const int row = 16 * (QW * qw + t) + rr;
-        if (row >= nrows) continue;  // padding rows are never read
-        f32x4_t sum = *reinterpret_cast<const f32x4_t*>(buf + (qw * 16 + rr) * kHalfRow + d4);
-        float ls = Ll[qw][16 * t + rr];
-#pragma unroll
-        for (int w = 1; w < KW; ++w) {
-          sum += *reinterpret_cast<const f32x4_t*>(buf + ((w * QG + qw) * 16 + rr) * kHalfRow + d4);
-          ls += Ll[w * QG + qw][16 * t + rr];
-        }
-        if (a.splits == 1) {
-          const float inv = ls == 0.f ? 0.f : 1.f / ls;
-          const int token = row % a.M, hq = g * (a.Hq / a.Hkv) + row / a.M;
-          *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(token) * a.Hq + hq) * kKv4D + 64 * h + d4) =
-              make_uint2(kv4_pack(sum[0] * inv, sum[1] * inv), kv4_pack(sum[2] * inv, sum[3] * inv));
-          continue;
-        }
-        const size_t base = (static_cast<size_t>(g) * a.splits + s) * a.rows_pad + row;
-        *reinterpret_cast<f32x4_t*>(a.part_o + base * kKv4D + 64 * h + d4) = sum;
-        if (d4 == 0 && h == 0) {
-          float mm = -INFINITY;
-#pragma unroll
-          for (int w = 0; w < KW; ++w) mm = fmaxf(mm, Lm[w * QG + qw][16 * t + rr]);
-          a.part_ml[2 * base] = mm;
-          a.part_ml[2 * base + 1] = ls;
-        }
+      for (int w = 0; w < KW; ++w) {
+        st[w] = stat[w * QG + qw][16 * t + rr];
+        v[w] = *reinterpret_cast<const f32x4_t*>(merge + ((w * QG + qw) * 16 + rr) * kMergeRow + d4);
+        top = fmaxf(top, st[w].x);
       }
+      const float base = top == -INFINITY ? 0.f : top;
+      f32x4_t sum{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float f = __builtin_amdgcn_exp2f(st[w].x - base);
+        sum += v[w] * f;
+        ls += st[w].y * f;
+      }
+      if (a.splits == 1) {
+        const float inv = ls == 0.f ? 0.f : 1.f / ls;
+        const int hl = kv4_row_head(row, a.inv_m), token = row - hl * a.M;
+        *reinterpret_cast<uint2*>(a.out + (static_cast<size_t>(token) * a.Hq + g * a.Gq + hl) * kKv4D + d4) =
+            make_uint2(kv4_pack(sum[0] * inv, sum[1] * inv), kv4_pack(sum[2] * inv, sum[3] * inv));
+        continue;
+      }
+      const size_t at = (static_cast<size_t>(g) * a.splits + s) * a.rows_pad + row;
+      *reinterpret_cast<f32x4_t*>(a.part_o + at * kKv4D + d4) = sum;
+      if (d4 == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(top, ls);
     }
+  }
+}
+
+// The wavefront's largest value, in every lane: within rows of 16 lanes by DPP moves, then across
+// them.
+template <int CTRL>
+__device__ __forceinline__ float kv4_dpp_max(float v) {
+  const int b = __float_as_int(v);
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, 0xF, 0xF, false)));
+}
+__device__ __forceinline__ float kv4_wave_max(float v) {
+  v = kv4_dpp_max<0xB1>(v);   // quad_perm [1,0,3,2]
+  v = kv4_dpp_max<0x4E>(v);   // quad_perm [2,3,0,1]
+  v = kv4_dpp_max<0x141>(v);  // row_half_mirror
+  v = kv4_dpp_max<0x140>(v);  // row_mirror
+  return kv4_cross_max(v);
 }
 
 constexpr int kCombineThreads = 256;
@@ -573,11 +607,10 @@ __global__ __launch_bounds__(kCombineThreads) void k_kv4_combine(Kv4AttnArgs a) 
   constexpr int kTeams = kCombineThreads / 32, kBatch = 8;
   __shared__ f32x4_t num[kTeams][32];
   __shared__ float den[kTeams];
-  const int i = blockIdx.x / a.Hq, h = blockIdx.x % a.Hq;
+  const int i = blockIdx.y, h = blockIdx.x;
   const int team = threadIdx.x / 32, d4 = 4 * (threadIdx.x % 32);
   const int lane = threadIdx.x % kWave;
-  const int Gq = a.Hq / a.Hkv;
-  const int g = h / Gq, row = h % Gq * a.M + i;
+  const int g = h / a.Gq, row = (h - g * a.Gq) * a.M + i;
   const int ns = a.splits;
   const size_t base = static_cast<size_t>(g) * ns * a.rows_pad + row;
   const float* po = a.part_o + base * kKv4D + d4;
@@ -593,12 +626,9 @@ __global__ __launch_bounds__(kCombineThreads) void k_kv4_combine(Kv4AttnArgs a) 
       v[u] = s < ns ? *reinterpret_cast<const f32x4_t*>(po + s * step * kKv4D) : f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     const float2 own = s0 + lane < ns ? ml[(s0 + lane) * step] : make_float2(-INFINITY, 0.f);
-    float mx = own.x;
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
-    mx = fmaxf(mmax, mx);
-    const float w = own.x == -INFINITY ? 0.f : exp2f(own.x - mx);
-    const float keep = mmax == -INFINITY ? 0.f : exp2f(mmax - mx);
+    const float mx = fmaxf(mmax, kv4_wave_max(own.x));
+    const float w = own.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(own.x - mx);
+    const float keep = mmax == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mmax - mx);
     mmax = mx;
     sum *= keep;
     total *= keep;
@@ -709,7 +739,7 @@ hipError_t launch_kv4_attention(const Kv4AttnArgs& a, int groups, hipStream_t st
     launch_narrow<4>(a, groups, sh.ring, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  hipLaunchKernelGGL(k_kv4_combine, dim3(a.M * a.Hq), dim3(kCombineThreads), 0, st, a);
+  hipLaunchKernelGGL(k_kv4_combine, dim3(a.Hq, a.M), dim3(kCombineThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -11,11 +11,18 @@
 // All rows are read at once, although only those on the path matter, because the path is
 // known only at its end: a row needs its maximum and its sum of exponentials to say which
 // child it picks, not the whole distribution.
+// Up to kVerifySmall slices of 2048 logits in all one kernel does everything in 64 bits
+// (k_verify_small: a slice its maximum and its sum without the row's children, the last workgroup of a
+// row the row's pick, the last of all path and token: a chain of 4 at V = 32000 11.5 us a call
+// against 15.1 with two kernels, 20 tokens at V = 152064, 1575 slices, 14.9 against 17.4; 99 at
+// 32000, 1600, 15.4 against 15.7).  Beyond, two, since 64-bit exponentials of all logits would bound
+// them:
 //   k_verify_rows      per (row, slice) workgroup the maximum and the sum, in 32 bits; the last
 //                      of a row finds the child that the row picks, the last of all the path
 //   k_verify_residual  the last row's other tokens in 64 bits: with V = 152064 tokens the
 //                      borders lie 10^-5 apart, and a sum in 32 bits, 10^-7 off, would pick a
 //                      neighbour in one call of a hundred; the last workgroup finds the token
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -28,7 +35,11 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / kWave;
-constexpr int kRowLoads = 4;  // 16-byte loads in flight per thread
+// Rows' completion counters lie a cache line apart: arrivals at one line take turns, 17 ns each.
+constexpr int kCounterStep = 15;
+static_assert(kCounterStep * (kVerifyMaxTokens + 2) <= kSplitCounters, "the workspace's counters");
+
+constexpr int kRowLoads = 2;  // 16-byte loads in flight per thread
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -113,6 +124,7 @@ struct Seen {
 
 // Stores that other XCDs' coherent loads see once they are acknowledged.
 __device__ __forceinline__ void put(int* p, int v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void put(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void put(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void put(float2* p, float x, float y) {
   __hip_atomic_store(reinterpret_cast<unsigned long long*>(p),
@@ -217,7 +229,7 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
   for (int w = 1; w < kRowWaves; ++w) seen.add(a.c, wm[w], ws[w]);
   if (a.chunks > 1) {
     if (t == 0) put(a.stat + blockIdx.x, seen.m, seen.s);
-    if (!last_to_arrive(a.cnt + 2 + row, a.chunks, &flag)) return;
+    if (!last_to_arrive(a.cnt + kCounterStep * (1 + row), a.chunks, &flag)) return;
     // every wavefront merges the row's slices, in the same order
     seen = Seen<GREEDY>();
     for (int c0 = 0; c0 < a.chunks; c0 += kWave) {
@@ -273,7 +285,7 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
     // a row without a distribution: no sum, or no token
     put(a.row_stat + row, seen.m, GREEDY ? __int_as_float(ok ? best : -1) : ok ? seen.s : 0.f);
   }
-  if (!last_to_arrive(a.cnt + 1, a.N + 1, &flag)) return;
+  if (!last_to_arrive(a.cnt, a.N + 1, &flag)) return;
 
   // The path.
   for (int r = t; r <= a.N; r += kRowThreads) u.next[r] = get(a.next + r);
@@ -299,6 +311,13 @@ constexpr int kResThreads = 256;
 constexpr int kResWaves = kResThreads / kWave;
 static_assert(kVerifySlice == 8 * kResThreads, "eight logits a thread");
 constexpr int kSlices = kVerifyMaxV / kVerifySlice / kWave;  // sums of slices a lane
+constexpr int kRowSlices = (kVerifyMaxV / kVerifySlice + kResThreads - 1) / kResThreads;  // and a thread
+
+__device__ __forceinline__ float wave_top(float v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
 
 __device__ __forceinline__ double wave_add(double v) {
 #pragma unroll
@@ -345,6 +364,15 @@ __device__ __forceinline__ int find_term(const double (&e)[K], int first, double
   return __shfl(hits ? hit : any, from);
 }
 
+// Zeroes the terms of tokens v0 .. v0 + 7 that are among `kids`.
+__device__ __forceinline__ void drop_tokens(const int* kids, int n, int v0, double (&e)[8]) {
+  for (int k = 0; k < n; ++k) {
+    const int d = kids[k] - v0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e[i] = d == i ? 0.0 : e[i];
+  }
+}
+
 // e^((l - m) / T) of this thread's 8 logits, drafted tokens and logits past the vocabulary zero.
 __device__ __forceinline__ void residual_terms(const VerifyArgs& a, const int* kids, int n, const uint16_t* l, float m,
                                                int v0, double (&e)[8]) {
@@ -355,10 +383,51 @@ __device__ __forceinline__ void residual_terms(const VerifyArgs& a, const int* k
   split8(*reinterpret_cast<const uint4*>(l + v0), x);
 #pragma unroll
   for (int i = 0; i < 8; ++i) e[i] = exp((static_cast<double>(x[i]) - static_cast<double>(m)) * a.inv_t);
-  for (int k = 0; k < n; ++k) {
-    const int d = kids[k] - v0;
+  drop_tokens(kids, n, v0, e);
+}
+
+// The token that the residual of `row` gives to its uniform number, written by the calling (last)
+// workgroup.  x: a lane's kSlices slice sums (the same in every wavefront), `rest` their sum,
+// `drafted` the drafted tokens' share, all relative to the maximum m; kid: the drafted tokens.
+__device__ __forceinline__ void pick_residual(const VerifyArgs& a, int row, float m, const double (&x)[kSlices], double rest,
+                                              double drafted, const int* kid, int n, double* part) {
+  const int t = threadIdx.x, wave = t / kWave;
+  const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
+  int token = -1;
+  if (rest > 0.0) {
+    const double target = fmax(static_cast<double>(a.uniform[row]) * (rest + drafted) - drafted, 0.0);
+    double before = 0.0, unused, e[8];
+    const int slice = find_term(x, 0, 0.0, target, &before);
+    residual_terms(a, kid, n, l, m, slice * kVerifySlice + 8 * t, e);
+    double s = 0.0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e[i] = d == i ? 0.0 : e[i];
+    for (int i = 0; i < 8; ++i) s += e[i];
+    s = wave_add(s);
+    if (t % kWave == 0) part[wave] = s;
+    __syncthreads();
+    // The wavefront in whose share the target falls, or the last with a share.
+    double start = before;
+    int owner = -1;
+    double owner_start = 0.0;
+    for (int w = 0; w < kResWaves; ++w) {
+      const double up = start + part[w];
+      if (part[w] > 0.0) {
+        owner = w;
+        owner_start = start;
+        if (up > target) break;
+      }
+      start = up;
+    }
+    if (wave != owner) return;
+    token = find_term(e, slice * kVerifySlice + 8 * kWave * wave, owner_start, target, &unused);
+    if (t % kWave == 0) *a.next_token = token;
+    return;
+  }
+  // The drafted tokens hold everything, and rounding kept u from all of them: the last of them.
+  if (t == 0) {
+    for (int i = 0; i < n; ++i)
+      if (__uint_as_float(static_cast<uint32_t>(l[kid[i]]) << 16) > -INFINITY) token = max(token, kid[i]);
+    *a.next_token = token;
   }
 }
 
@@ -428,49 +497,169 @@ __global__ __launch_bounds__(kResThreads) void k_verify_residual(VerifyArgs a) {
   double drafted = 0.0;
   for (int k = t % kWave; k < n; k += kWave) drafted += share[k];
   drafted = wave_add(drafted);
-  int token = -1;
-  if (rest > 0.0) {
-    const double target = fmax(static_cast<double>(a.uniform[row]) * (rest + drafted) - drafted, 0.0);
-    double before = 0.0, unused;
-    const int slice = find_term(x, 0, 0.0, target, &before);
-    residual_terms(a, kid, n, l, st.x, slice * kVerifySlice + 8 * t, e);
-    s = 0.0;
+  pick_residual(a, row, st.x, x, rest, drafted, kid, n, part[1]);
+}
+
+// Everything in one kernel, workgroup (row, slice of 2048 logits); the last workgroup of a row finds
+// the row's pick, the last of all the path and the token.
+__global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
+  __shared__ double share[kResThreads], part[2][kResWaves];
+  __shared__ float wm[2][kResWaves];
+  __shared__ int kid_j[kResThreads], kid[kResThreads], order[kResThreads], next[kResThreads];
+  __shared__ float kid_l[kResThreads];
+  __shared__ int n, flag;
+  const int t = threadIdx.x, wave = t / kWave, lane = t % kWave;
+  const int slices = (a.V + kVerifySlice - 1) / kVerifySlice;
+  const int row = blockIdx.x / slices, slice = blockIdx.x % slices;
+  const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
+  const int v0 = slice * kVerifySlice + 8 * t;
+  uint4 raw = make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);  // -inf
+  if (v0 < a.V) raw = *reinterpret_cast<const uint4*>(l + v0);
+  if (t == 0) n = 0;
+  __syncthreads();
+  int token;
+  if (t < a.N && continues(a, t, row, &token)) {  // the row's children, in any order
+    const int at = atomicAdd(&n, 1);
+    kid_j[at] = t;
+    kid[at] = token;
+    kid_l[at] = __uint_as_float(static_cast<uint32_t>(l[token]) << 16);
+  }
+  // the slice's maximum; a NaN or +inf in it makes the sum NaN
+  float x[8], m = -INFINITY;
+  split8(raw, x);
+  bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += e[i];
-    s = wave_add(s);
-    if (t % kWave == 0) part[1][wave] = s;
-    __syncthreads();
-    // The wavefront in whose share the target falls, or the last with a share.
-    double start = before;
-    int owner = -1;
-    double owner_start = 0.0;
-    for (int w = 0; w < kResWaves; ++w) {
-      const double up = start + part[1][w];
-      if (part[1][w] > 0.0) {
-        owner = w;
-        owner_start = start;
-        if (up > target) break;
-      }
-      start = up;
+  for (int i = 0; i < 8; ++i) {
+    m = fmaxf(m, x[i]);
+    bad |= !(x[i] < INFINITY);
+  }
+  m = wave_top(m);
+  if (lane == 0) wm[0][wave] = m;
+  const int any_bad = __syncthreads_or(bad);
+#pragma unroll
+  for (int w = 0; w < kResWaves; ++w) m = fmaxf(m, wm[0][w]);
+  double e[8], s = 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e[i] = x[i] == -INFINITY ? 0.0 : exp((static_cast<double>(x[i]) - static_cast<double>(m)) * a.inv_t);
+  drop_tokens(kid, n, v0, e);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s += e[i];
+  s = wave_add(s);
+  if (lane == 0) part[0][wave] = s;
+  __syncthreads();
+  if (t == 0) {
+    s = part[0][0];
+#pragma unroll
+    for (int w = 1; w < kResWaves; ++w) s += part[0][w];
+    put(a.slice_sum + blockIdx.x, any_bad ? __longlong_as_double(0x7FF8000000000000ll) : s);
+    put(a.slice_max + blockIdx.x, m);
+  }
+  if (!last_to_arrive(a.cnt + kCounterStep * (1 + row), slices, &flag)) return;
+
+  // The row: its maximum, its slices' sums relative to it, and their sum.
+  double v[kRowSlices];
+  float vm[kRowSlices], rm = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kRowSlices; ++i) {
+    const int c = t + i * kResThreads;
+    v[i] = c < slices ? get(a.slice_sum + row * slices + c) : 0.0;
+    vm[i] = c < slices ? get(a.slice_max + row * slices + c) : -INFINITY;
+    rm = fmaxf(rm, vm[i]);
+  }
+  rm = wave_top(rm);
+  if (lane == 0) wm[1][wave] = rm;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kResWaves; ++w) rm = fmaxf(rm, wm[1][w]);
+  double rest = 0.0;
+#pragma unroll
+  for (int i = 0; i < kRowSlices; ++i) {
+    // (a slice of -inf alone has nothing; a NaN stays one)
+    if (v[i] != 0.0) v[i] *= exp((static_cast<double>(vm[i]) - static_cast<double>(rm)) * a.inv_t);
+    if (t + i * kResThreads < slices) put(a.slice_sum + row * slices + t + i * kResThreads, v[i]);
+    rest += v[i];
+  }
+  rest = wave_add(rest);
+  if (lane == 0) part[1][wave] = rest;
+  // its children's shares in index order, a repeated token's 0
+  const int nk = n;
+  if (t < nk) {
+    int rank = 0;
+    bool repeat = false;
+    for (int i = 0; i < nk; ++i) {
+      const bool before = kid_j[i] < kid_j[t];
+      rank += before;
+      repeat |= before && kid[i] == kid[t];
     }
-    if (wave != owner) return;
-    token = find_term(e, slice * kVerifySlice + 8 * kWave * wave, owner_start, target, &unused);
-    if (t % kWave == 0) *a.next_token = token;
+    order[rank] = kid_j[t];
+    share[rank] = repeat || kid_l[t] == -INFINITY ? 0.0 : exp((static_cast<double>(kid_l[t]) - static_cast<double>(rm)) * a.inv_t);
+  }
+  __syncthreads();
+  if (t == 0) {
+    rest = 0.0;
+#pragma unroll
+    for (int w = 0; w < kResWaves; ++w) rest += part[1][w];
+    const bool ok = fabsf(rm) < INFINITY && rest == rest;
+    double drafted = 0.0;
+    for (int k = 0; k < nk; ++k) drafted += share[k];
+    int pick = -1;
+    if (ok) {
+      const double target = static_cast<double>(a.uniform[row]) * (rest + drafted);
+      double f = 0.0;
+      for (int k = 0; k < nk; ++k) {
+        const double f2 = f + share[k];
+        if (f <= target && target < f2) {
+          pick = order[k];
+          break;
+        }
+        f = f2;
+      }
+    }
+    put(a.next + row, pick);
+    put(a.row_rest + 2 * row, ok ? rest : __longlong_as_double(0x7FF8000000000000ll));
+    put(a.row_rest + 2 * row + 1, drafted);
+    put(a.row_max + row, rm);
+  }
+  if (!last_to_arrive(a.cnt, a.N + 1, &flag)) return;
+
+  // The path, and the token after it.
+  for (int r = t; r <= a.N; r += kResThreads) next[r] = get(a.next + r);
+  __syncthreads();
+  if (t == 0) {
+    int r = 0, len = 0;
+    for (int j; (j = next[r]) >= 0; r = j + 1) a.path[len++] = j;  // j >= r: it ends
+    *a.accepted = len;
+    flag = r;
+    order[0] = len;
+    n = 0;
+  }
+  __syncthreads();
+  const int end = flag;
+  for (int i = order[0] + t; i < a.N; i += kResThreads) a.path[i] = -1;
+  rest = get(a.row_rest + 2 * end);
+  const double drafted = get(a.row_rest + 2 * end + 1);
+  rm = get(a.row_max + end);
+  double y[kSlices];
+#pragma unroll
+  for (int i = 0; i < kSlices; ++i) {
+    const int at = kSlices * lane + i;
+    y[i] = at < slices ? get(a.slice_sum + end * slices + at) : 0.0;
+  }
+  if (t < a.N && continues(a, t, end, &token)) kid[atomicAdd(&n, 1)] = token;
+  __syncthreads();
+  if (rest != rest) {  // no distribution
+    if (t == 0) *a.next_token = -1;
     return;
   }
-  // The drafted tokens hold everything, and rounding kept u from all of them: the last of them.
-  if (t == 0) {
-    for (int i = 0; i < n; ++i)
-      if (__uint_as_float(static_cast<uint32_t>(l[kid[i]]) << 16) > -INFINITY) token = max(token, kid[i]);
-    *a.next_token = token;
-  }
+  pick_residual(a, end, rm, y, rest, drafted, kid, n, part[0]);
 }
 
 }  // namespace
 
 void verify_plan(int N, int V, int* chunks, int* chunk_len) {
-  // about 1024 workgroups, each with at least one round of loads
-  int c = (1024 + N) / (N + 1);
+  // about 640 workgroups (three slices of 289 rows: 30.8 us; one 38, eight 36), each with at least one
+  // round of loads
+  int c = (640 + N) / (N + 1);
   const int most = (V + 8 * kRowThreads * kRowLoads - 1) / (8 * kRowThreads * kRowLoads);
   if (c > most) c = most;
   if (c < 1) c = 1;
@@ -478,29 +667,50 @@ void verify_plan(int N, int V, int* chunks, int* chunk_len) {
   *chunks = (V + *chunk_len - 1) / *chunk_len;
 }
 
-// After the completion counters: the last row and its (maximum, sum), the slices' sums,
-// the rows' (maximum, sum) pairs, the slices' of rows, the rows' picks.
+bool verify_small(int N, int V) {
+  return N < kResThreads && static_cast<long long>(N + 1) * ((V + kVerifySlice - 1) / kVerifySlice) <= kVerifySmall;
+}
+
+// After the completion counters, small calls: the slices' sums, the rows' (sum, drafted share), the
+// slices' and rows' maxima, the rows' picks.  Others: the last row
+// and its (maximum, sum), its slices' sums, the rows' (maximum, sum) pairs, the slices' of
+// rows, the rows' picks.
 size_t verify_workspace_bytes(int N, int V) {
   int chunks = 0, len = 0;
   verify_plan(N, V, &chunks, &len);
-  const size_t slices = (V + kVerifySlice - 1) / kVerifySlice;
-  return kSplitCounterBytes + 16 + slices * sizeof(double) + static_cast<size_t>(N + 1) * (1 + chunks) * sizeof(float2) +
-         static_cast<size_t>(N + 1) * sizeof(int);
+  const size_t slices = (V + kVerifySlice - 1) / kVerifySlice, rows = N + 1;
+  const size_t small = verify_small(N, V) ? rows * (slices * (sizeof(double) + sizeof(float)) + 2 * sizeof(double) + 2 * sizeof(float)) : 0;
+  const size_t large = 16 + slices * sizeof(double) + rows * (1 + chunks) * sizeof(float2) + rows * sizeof(int);
+  return kSplitCounterBytes + std::max(small, large);
 }
 
 void verify_workspace(VerifyArgs* a, void* ws) {
   char* p = static_cast<char*>(ws);
   a->cnt = reinterpret_cast<unsigned*>(p);
   p += kSplitCounterBytes;
+  const int slices = (a->V + kVerifySlice - 1) / kVerifySlice;
+  if (!a->greedy && verify_small(a->N, a->V)) {
+    a->slice_sum = reinterpret_cast<double*>(p);
+    a->row_rest = a->slice_sum + static_cast<size_t>(a->N + 1) * slices;
+    a->slice_max = reinterpret_cast<float*>(a->row_rest + 2 * (a->N + 1));
+    a->row_max = a->slice_max + static_cast<size_t>(a->N + 1) * slices;
+    a->next = reinterpret_cast<int*>(a->row_max + (a->N + 1));
+    return;
+  }
   a->last_row = reinterpret_cast<int*>(p);
   a->last_stat = reinterpret_cast<float2*>(p + 8);
   a->slice_sum = reinterpret_cast<double*>(p + 16);
-  a->row_stat = reinterpret_cast<float2*>(a->slice_sum + (a->V + kVerifySlice - 1) / kVerifySlice);
+  a->row_stat = reinterpret_cast<float2*>(a->slice_sum + slices);
   a->stat = a->row_stat + (a->N + 1);
   a->next = reinterpret_cast<int*>(a->stat + static_cast<size_t>(a->N + 1) * a->chunks);
 }
 
 hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t st) {
+  const int slices = (a.V + kVerifySlice - 1) / kVerifySlice;
+  if (!a.greedy && verify_small(a.N, a.V)) {
+    hipLaunchKernelGGL(k_verify_small, dim3((a.N + 1) * slices), dim3(kResThreads), 0, st, a);
+    return hipGetLastError();
+  }
   const dim3 rows((a.N + 1) * a.chunks);
   if (a.greedy)
     hipLaunchKernelGGL(k_verify_rows<true>, rows, dim3(kRowThreads), 0, st, a);
@@ -508,7 +718,7 @@ hipError_t launch_tree_verify(const VerifyArgs& a, hipStream_t st) {
     hipLaunchKernelGGL(k_verify_rows<false>, rows, dim3(kRowThreads), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.greedy) return e;
-  hipLaunchKernelGGL(k_verify_residual, dim3((a.V + kVerifySlice - 1) / kVerifySlice), dim3(kResThreads), 0, st, a);
+  hipLaunchKernelGGL(k_verify_residual, dim3(slices), dim3(kResThreads), 0, st, a);
   return hipGetLastError();
 }
 

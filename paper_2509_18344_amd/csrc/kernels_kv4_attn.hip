@@ -120,23 +120,25 @@ __device__ __forceinline__ uint32_t kv4_pack(float lo, float hi) {
   return static_cast<uint32_t>(float_to_bf16_bits(lo)) | (static_cast<uint32_t>(float_to_bf16_bits(hi)) << 16);
 }
 
-// Eight codes of a word, in order, as the fp16 numbers 2^-24 c: a code is the mantissa of a
-// subnormal, which the matrix instruction takes as it is.
+// Eight codes of a word as fp16 numbers: a code is the mantissa of a subnormal, which the matrix
+// instruction takes as it is.  Codes 0, 1, 4 and 5 come as 2^-24 c and codes 2, 3, 6 and 7, left a
+// nibble higher, as 2^-20 c (two shifts fewer a word); the other operand is 2^-4 times as
+// large there.
 __device__ __forceinline__ f16x8_t kv4_codes(uint32_t d) {
-  const uint32_t mask = 0x000F000Fu;
-  return __builtin_bit_cast(f16x8_t, u32x4_t{d & mask, (d >> 4) & mask, (d >> 8) & mask, (d >> 12) & mask});
+  const uint32_t low = 0x000F000Fu, high = 0x00F000F0u, e = d >> 8;
+  return __builtin_bit_cast(f16x8_t, u32x4_t{d & low, d & high, e & low, e & high});
 }
 
-// One load straight into LDS: lane l's SIZE bytes at p land at byte dst + SIZE * l.  Written as
+// One load straight into LDS: lane l's SIZE bytes at base + offset (the lane's) land at byte dst + SIZE * l.  Written as
 // assembly because the compiler, where it sees such loads, waits for all of them before it reads
 // the ring again; it has no register result, and the ring's own waits order it (a wait state after
 // the write of m0 included).
 template <int SIZE>
-__device__ __forceinline__ void kv4_to_lds(const uint8_t* p, uint32_t dst) {
+__device__ __forceinline__ void kv4_to_lds(const uint8_t* base, uint32_t offset, uint32_t dst) {
   if constexpr (SIZE == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(p) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(p) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory");
 }
 
 // Infinite and NaN halves become zero (rows that nothing has written, seen by no query).
@@ -195,8 +197,9 @@ __device__ __forceinline__ int kv4_row_head(int row, float inv_m) { return stati
 template <int QW, int G>
 struct Kv4Rows {
   // Per lane the query row's fragments of q times 2^(15 - e), where the row's largest value
-  // lies below 2^e, as fp16 (bf16's 8 bits fit, down to 2^-29 of the largest), their sums per
-  // group times 2^-24, and the factor that takes a score to log2.
+  // lies below 2^e, as fp16 (bf16's 8 bits fit, down to 2^-25 of the largest; those that meet codes
+  // 16 times as large 2^-4 times that), their sums per group times 2^-24, and the factor that takes
+  // a score to log2.
   f16x8_t qf[QW][4];
   float qs[QW][G], factor[QW];
   bool live[QW];
@@ -233,17 +236,18 @@ struct Kv4Rows {
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          qf[t][j][2 * i] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] << 16), 15 - e));
-          qf[t][j][2 * i + 1] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] & 0xFFFF0000u), 15 - e));
+          const int up = i % 2 == 0 ? 15 - e : 11 - e;  // codes 2, 3, 6 and 7 are 16 times as large
+          qf[t][j][2 * i] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] << 16), up));
+          qf[t][j][2 * i + 1] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] & 0xFFFF0000u), up));
         }
 #pragma unroll
       for (int gg = 0; gg < G; ++gg) {
-        float sum = 0.f;
+        float sum = 0.f, sum16 = 0.f;
 #pragma unroll
         for (int j = gg * (4 / G); j < (gg + 1) * (4 / G); ++j)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum += static_cast<float>(qf[t][j][i]);
-        qs[t][gg] = kv4_cross_sum(sum) * 0x1p-24f;
+          for (int i = 0; i < 8; ++i) (i / 2 % 2 == 0 ? sum : sum16) += static_cast<float>(qf[t][j][i]);
+        qs[t][gg] = kv4_cross_sum(__builtin_fmaf(16.f, sum16, sum)) * 0x1p-24f;
       }
       factor[t] = fminf(fmaxf(ldexpf(a.scale_log2, 9 + e), 0x1p-126f), 0x1p126f);
       ref[t] = -INFINITY;
@@ -330,8 +334,14 @@ struct Kv4Rows {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           ps[t][4 * u + e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(x[t][u][e], factor[t], -base)));
+      // times the scales, and 2^-4 where the codes are 16 times as large (positions 2 and 3 of each
+      // four: before the scale, which may be a subnormal already)
+      f16x8_t pq = ps[t];
 #pragma unroll
-      for (int gg = 0; gg < G; ++gg) pf[t][gg] = ps[t] * __builtin_bit_cast(f16x8_t, v.s[gg]);
+      for (int e = 2; e < 8; ++e)
+        if (e % 4 >= 2) pq[e] = ps[t][e] * static_cast<_Float16>(0.0625f);
+#pragma unroll
+      for (int gg = 0; gg < G; ++gg) pf[t][gg] = pq * __builtin_bit_cast(f16x8_t, v.s[gg]);
     }
     u32x4_t w;
 #pragma unroll
@@ -425,29 +435,32 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
   };
 
   if constexpr (RING) {
-    constexpr int VM = 4 + G;  // vector memory operations of a tile's loads
+    constexpr int VM = 6;  // vector memory operations of a tile's loads
     u32x4_t* ring = lds + wave * (kRing * kSlot);
     const uint32_t ring_at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) void*)ring));
-    // Tile `tile` into slot `slot`.  A tile past the range's last is one 16-byte piece of that
-    // one over and over: the count of loads in flight stays what the waits assume, and memory
-    // sees one line.
+    // Tile `tile` into slot `slot`.  A tile past the range's last is one word of that one over
+    // and over: the count of loads in flight stays what the waits assume, and memory sees one
+    // line.
+    const uint32_t l16 = 16 * lane, l4 = 4 * lane;
     auto request = [&](int slot, int tile) __attribute__((always_inline)) {
-      const bool real = tile < last;
-      const size_t at = static_cast<size_t>(real ? tile : last - 1) * kv4_tile_bytes(G);
-      const int l16 = real ? 16 * lane : 0, l4 = real ? 4 * lane : 0, next = real ? 1024 : 0;
-      const uint8_t* kt = kbase + at;
-      const uint8_t* vt = vbase + at;
       const uint32_t to = __builtin_amdgcn_readfirstlane(ring_at + slot * (16 * kSlot));
-      kv4_to_lds<16>(kt + l16, to);
-      kv4_to_lds<16>(kt + next + l16, to + 1024);
-      if constexpr (G == 1) {
-        kv4_to_lds<4>((lane < 32 ? kt : vt) + kKv4CodeBytes + (real ? 4 * (lane % 32) : 0), to + 4096);
+      if (tile < last) {
+        const size_t at = static_cast<size_t>(tile) * kv4_tile_bytes(G);
+        const uint8_t* kt = kbase + at;
+        const uint8_t* vt = vbase + at;
+        kv4_to_lds<16>(kt, l16, to);
+        kv4_to_lds<16>(kt + 1024, l16, to + 1024);
+        if (G == 2 || lane < 32) {  // scales and minima: 128 G bytes a side
+          kv4_to_lds<4>(kt + kKv4CodeBytes, l4, to + 4096);
+          kv4_to_lds<4>(vt + kKv4CodeBytes, l4, to + 4096 + 128 * G);
+        }
+        kv4_to_lds<16>(vt, l16, to + 2048);
+        kv4_to_lds<16>(vt + 1024, l16, to + 3072);
       } else {
-        kv4_to_lds<4>(kt + kKv4CodeBytes + l4, to + 4096);
-        kv4_to_lds<4>(vt + kKv4CodeBytes + l4, to + 4096 + 256);
+        const uint8_t* kt = kbase + static_cast<size_t>(last - 1) * kv4_tile_bytes(G);
+#pragma unroll
+        for (int i = 0; i < VM; ++i) kv4_to_lds<4>(kt, 0, to);
       }
-      kv4_to_lds<16>(vt + l16, to + 2048);
-      kv4_to_lds<16>(vt + next + l16, to + 2048 + 1024);
     };
     rows.request(a, g, 16 * QW * qg, lane);
     request_masks();

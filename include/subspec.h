@@ -433,8 +433,10 @@ int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, i
  *            no mask row allows may hold anything
  *   mask     device uint32 [M][W], W = ceil((T + M) / 32), as subspec_tree_attention's
  *   out      device bf16 [M][Hq][128]; a query with no visible position gets zeros
- * Scores are fp32 sums over exact codes; a position's weight times its value's scale is
- * rounded to fp16 (11 bits) before the second product, which sums in fp32.  Limits as
+ * Scores are fp32 sums over exact codes.  A position's weight is rounded to fp16, and its product
+ * with the value's scale once more, before the second product, which sums in fp32: 11 bits,
+ * fewer for weights below 2^(E - 20) of the heaviest (2^E, at least 1, the largest scale of a
+ * value seen), none below 2^(E - 29).  What positions hold that no query sees changes no bit of the result.  Limits as
  * subspec_tree_attention's (Hkv at most 65535, S a multiple of 32); q, caches and out
  * 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one where
  * a single range covers the positions); workspace as for subspec_qlinear

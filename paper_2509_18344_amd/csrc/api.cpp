@@ -1318,9 +1318,7 @@ int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v
   a.W = (T + M + 31) / 32;
   a.Gq = Hq / Hkv;
   a.inv_m = 1.f / static_cast<float>(M);
-  // The kernel takes a positive factor: a negative scale flips q, and 2^-100 for 0 leaves
-  // every score at 0 for any finite product.
-  a.scale_log2 = std::max(c, 0x1p-100f);
+  a.scale_log2 = c;  // the kernel takes a factor that is not negative: a negative scale flips q
   a.q_sign = scale < 0.f ? 0x80008000u : 0u;
   a.out = static_cast<uint16_t*>(out);
   const hipError_t e = subspec::launch_kv4_attention(a, 128 / group, stream);

@@ -11,7 +11,6 @@ constexpr int kKv4Tile = 32;         // positions per tile
 constexpr int kKv4CodeBytes = kKv4Tile * kKv4D / 2;
 constexpr int kKv4MaxRows = 64;      // attention: query rows per key/value head
 constexpr int kKv4MaskWords = 2048;  // attention: M * ceil((T + M) / 32)
-constexpr int kKv4MaxSplits = 512;   // attention: key ranges per head
 
 // Bytes of a tile: the codes, and per 64 or 128 dimensions a scale and a minimum of each position.
 constexpr int kv4_tile_bytes(int groups) { return kKv4CodeBytes + kKv4Tile * 4 * groups; }
@@ -40,7 +39,7 @@ struct Kv4AttnArgs {
   int M, Hq, Hkv, S, P, T, W;
   int Gq;                  // Hq / Hkv
   float inv_m;             // 1 / M
-  float scale_log2;        // |scale| * log2(e), positive
+  float scale_log2;        // |scale| * log2(e)
   uint32_t q_sign;         // 0x80008000 where the scale is negative: flips q's signs
   int splits;              // key ranges per key/value head
   int tiles_per_split;

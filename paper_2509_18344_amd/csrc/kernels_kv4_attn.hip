@@ -5,31 +5,42 @@
 // P + j (j < T + M) that their mask rows allow.  A position's key is m_g + s_g c per group g
 // of dimensions (fp16 minimum m, scale s, codes c of 4 bits), its value the same with its own.
 //
-// Neither product forms those numbers.  With codes as exact 16-bit floats (16 + c: the code
-// or-ed into the mantissa of 16),
-//   q.k = sum_g s_g (q.(16 + c))_g + (m_g - 16 s_g) (sum q)_g
-//       = sum_g s_g ((q.(16 + c))_g - 16 (sum q)_g) + m_g (sum q)_g
-// where the bracket is a bf16 matrix product whose accumulator starts at -16 (sum q)_g, and
-//   sum_j p_j v_j = sum_j (p_j s_jg) (16 + c_j) - 16 sum_j (p_j s_jg) + sum_j p_j m_jg
-// where the first term is an fp16 matrix product, the second the same weights against a row
-// of 16s, and the third stays in 32-bit lanes.  The weight p s is rounded to fp16 (2^-12
-// relative: a sixteenth of what rounding the bf16 output costs, and the roundings of
-// different positions are independent); everything else is exact or in 32 bits.  fp16
-// spans 2^-24 .. 65504, so the running maximum is that of score + log2 of the tile's
-// largest scale: then p s is at most 2^14 for the heaviest position and keeps its
-// 11 bits down to 2^-28 of it.
+// Neither product forms those numbers.  With x the sum over a group g of dimensions,
+//   q.k = sum_g s_g (q.c)_g + m_g (sum q)_g
+//   sum_j p_j v_j = sum_j (p_j s_jg) c_j + sum_j p_j m_jg
+// where q.c and (p s) c are fp16 matrix products that take the 4-bit codes as they lie: a code is the
+// mantissa of an fp16 subnormal, so unpacking a word of eight is four ands and a shift.  bf16 q fits
+// fp16 once its row is scaled by a power of two.  The sum of the weights and the minima's share come
+// from one more product against rows of ones and of minima, so that the numerator's and the
+// denominator's weights are the same numbers.
+//
+// Roundings: a weight p to fp16, its product with the scale to fp16 again (2^-11 relative at most, an
+// eighth of what rounding the output to bf16 may cost, and independent from position to
+// position); everything else is exact or in 32 bits.  fp16 spans 2^-24 .. 65504, so weights are
+// relative to a reference that covers score + log2 of the tile's largest scale: p and p s stay
+// below 2^15, and the heaviest position's p is at least 2^8 while scales lie below 1.  The
+// reference moves only when a weight would pass 2^14 (a few times in a row's life), so most
+// tiles scale nothing.
 //
 // Kernel 1 (k_kv4_partial): workgroup (range s, key/value head g); its wavefronts take the
 // range's tiles of 32 positions in turn, each for up to two tiles of 16 query rows (row =
-// local head * M + token; with more than 32 rows two wavefronts share a tile of positions).
-// The cache holds both operands in register order: a lane's share of a tile is five or six
-// 16-byte loads a side, no code passes through LDS and no wavefront waits for another until
-// the end, when their outputs are scaled to a common maximum and added in wavefront order.
-//   S^T = K Q^T     16x16x32 bf16, 2 blocks of 16 positions x 4 steps of 32 dimensions
+// local head * M + token; with more rows two or four wavefronts share a tile of positions).
+// The cache holds both operands in register order: no code moves between lanes, and no wavefront
+// waits for another until the end, when their outputs are scaled to a common reference and added in
+// wavefront order.
+//   S^T = K Q^T     16x16x32 fp16, 2 blocks of 16 positions x 4 steps of 32 dimensions
 //   O^T += V^T P^T  16x16x32 fp16, 8 tiles of 16 dimensions; P is in the operand layout
 //                   where the scores are
 // Kernel 2 (k_kv4_combine) combines the ranges in a fixed order; a single range writes the
 // output itself.
+//
+// Measured (a call, both kernels): 131138 positions of 8 heads in groups of 64, 30 query rows a head:
+// 302 MB in 40 to 43 us, 7.0 to 7.6 TB/s (part of the cache stays in the last-level cache between
+// calls); the first kernel's vector ALUs are busy two thirds of its time, so unpacking and the
+// softmax bound it, not loads.  8407 positions of 8 heads in groups of 128, 64 rows a head: 18 MB in
+// 17 us, a chain of the launch with the first loads (3.4 us), two or three tiles a wavefront (1.2 to
+// 2 each), the merge (1 to 2.5) and the second kernel (2.5 to 3.3).  2336 positions of 4 heads,
+// 42 rows: 10.5 us, the same chain with one or two tiles.
 #include <cmath>
 #include <type_traits>
 
@@ -129,10 +140,10 @@ __device__ __forceinline__ f16x8_t kv4_codes(uint32_t d) {
   return __builtin_bit_cast(f16x8_t, u32x4_t{d & low, d & high, e & low, e & high});
 }
 
-// One load straight into LDS: lane l's SIZE bytes at base + offset (the lane's) land at byte dst + SIZE * l.  Written as
-// assembly because the compiler, where it sees such loads, waits for all of them before it reads
-// the ring again; it has no register result, and the ring's own waits order it (a wait state after
-// the write of m0 included).
+// One load straight into LDS: lane l's SIZE bytes at base + offset (the lane's) land at byte
+// dst + SIZE * l.  Written as assembly because the compiler, where it sees such loads, waits for all
+// of them before it reads the ring again; it has no register result, and the ring's own waits order
+// it (a wait state after the write of m0 included).
 template <int SIZE>
 __device__ __forceinline__ void kv4_to_lds(const uint8_t* base, uint32_t offset, uint32_t dst) {
   if constexpr (SIZE == 16)
@@ -141,12 +152,22 @@ __device__ __forceinline__ void kv4_to_lds(const uint8_t* base, uint32_t offset,
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory");
 }
 
-// Infinite and NaN halves become zero (rows that nothing has written, seen by no query).
-__device__ __forceinline__ uint32_t kv4_finite(uint32_t w) {
-  uint32_t r = w;
-  if ((w & 0x7C00u) == 0x7C00u) r &= 0xFFFF0000u;
-  if ((w & 0x7C000000u) == 0x7C000000u) r &= 0x0000FFFFu;
-  return r;
+// The halves of a metadata word, two positions', of which bits 0 and 1 of `seen` say which stay; the
+// others become zero.
+__device__ __forceinline__ uint32_t kv4_seen_halves(uint32_t seen) {
+  return (seen & 1u ? 0xFFFFu : 0u) | (seen & 2u ? 0xFFFF0000u : 0u);
+}
+
+// OR over the 16 lanes of a DPP row, in every lane.
+template <int CTRL>
+__device__ __forceinline__ uint32_t kv4_dpp_or(uint32_t v) {
+  return v | static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, 0xF, 0xF, false));
+}
+__device__ __forceinline__ uint32_t kv4_row_or(uint32_t v) {
+  v = kv4_dpp_or<0xB1>(v);     // quad_perm [1,0,3,2]
+  v = kv4_dpp_or<0x4E>(v);     // quad_perm [2,3,0,1]
+  v = kv4_dpp_or<0x141>(v);    // row_half_mirror
+  return kv4_dpp_or<0x140>(v); // row_mirror
 }
 
 // A lane and its partners 16, 32 and 48 lanes away (the four quarters that share a query):
@@ -286,17 +307,25 @@ struct Kv4Rows {
     }
   }
 
-  __device__ __forceinline__ void mask(const Kv4AttnArgs& a, const uint32_t* words, int key0, int total, int quarter,
-                                       f32x4_t (&x)[QW][2]) const {
+  // The tile's positions that each row sees, and (returned) that any of the wavefront's rows does.
+  __device__ __forceinline__ uint32_t look(const Kv4AttnArgs& a, const uint32_t* words, int key0, int total, uint32_t (&vis)[QW]) const {
+    uint32_t any = 0;
 #pragma unroll
     for (int t = 0; t < QW; ++t) {
-      const uint32_t vis = live[t] ? kv4_visibility(words + qi[t] * a.W, a.W, a.P, key0, total) : 0u;
+      vis[t] = live[t] ? kv4_visibility(words + qi[t] * a.W, a.W, a.P, key0, total) : 0u;
+      any |= vis[t];
+    }
+    return kv4_row_or(any);
+  }
+
+  __device__ __forceinline__ void mask(const uint32_t (&vis)[QW], int quarter, f32x4_t (&x)[QW][2]) const {
+#pragma unroll
+    for (int t = 0; t < QW; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (!((vis >> (16 * u + 4 * quarter + e)) & 1u)) x[t][u][e] = -INFINITY;
-    }
+          if (!((vis[t] >> (16 * u + 4 * quarter + e)) & 1u)) x[t][u][e] = -INFINITY;
   }
 
   // Weights of the tile's positions, and their products with the values.  keep, ones: the
@@ -479,9 +508,15 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       const int key0 = n * kKv4Tile;
       const bool masked = key0 + kKv4Tile > a.P;  // the same for the whole wavefront
       u32x4_t* p = ring + slot * kSlot;
-      if (masked && lane < 32 * G) {  // scales and minima of values that nothing has written
-        uint32_t* w = reinterpret_cast<uint32_t*>(p + 256) + 32 * G + lane;
-        *w = kv4_finite(*w);
+      uint32_t vis[QW] = {};
+      if (masked) {
+        // Scales and minima of values that no row sees become zero: they may be anything, and a large
+        // scale among them would cost the others' weights bits.
+        const uint32_t any = rows.look(a, words, key0, total, vis);
+        if (lane < 32 * G) {
+          const int e = lane % 4, at = 4 * (lane / (8 * G)) + 16 * (e / 2) + 2 * (e % 2);  // the word's first position
+          reinterpret_cast<uint32_t*>(p + 256)[32 * G + lane] &= kv4_seen_halves(any >> at);
+        }
       }
       if (masked) kv4_wave_fence();
       Kv4Keys<G> k;
@@ -501,7 +536,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       v.m = meta[8 * G + (col == 2 ? 2 * (G - 1) : 0) + 1];
       f32x4_t x[QW][2];
       rows.scores(k, x);
-      if (masked) rows.mask(a, words, key0, total, quarter, x);
+      if (masked) rows.mask(vis, quarter, x);
       rows.values(v, x, keep, ones);
     }
     asm volatile("" ::: "memory");
@@ -527,12 +562,15 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
       else
         kv4_keep(k);
       if constexpr (decltype(masked)::value) {
-        rows.mask(a, words, n * kKv4Tile, total, quarter, x);
+        uint32_t vis[QW];
+        const uint32_t any = rows.look(a, words, n * kKv4Tile, total, vis);
+        rows.mask(vis, quarter, x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 4; ++e) {  // scales and minima of values that no row sees become zero, as in the ring
+          const uint32_t stay = kv4_seen_halves(any >> (4 * quarter + 16 * (e / 2) + 2 * (e % 2)));
 #pragma unroll
-          for (int gg = 0; gg < G; ++gg) v.s[gg][e] = kv4_finite(v.s[gg][e]);
-          v.m[e] = kv4_finite(v.m[e]);
+          for (int gg = 0; gg < G; ++gg) v.s[gg][e] &= stay;
+          v.m[e] &= stay;
         }
       }
       rows.values(v, x, keep, ones);

@@ -5,8 +5,10 @@ Tolerance, from the arithmetic.  A value is m + s c.  The kernel rounds a weight
 the sum of weights and for the minima, and the product of that and s once more for the
 codes: 2^-11 relative each, so 2^-11 (sum_j p_j |v_j| + |o|) for the first and 2^-11 sum_j p_j
 |v_j - m_j| for the second, together at most 2^-11 sum_j p_j (3 |v_j| + |m_j|).  Below fp16's normal
-range either rounding is 2^-25 absolute, where the heaviest weight of the row is at least
-2^(8 - E), 2^E (E >= 0) above the largest scale of a value: L 2^(E - 33) (15 + max |v|).
+range a rounding is 2^-25 absolute, where the heaviest weight of the row is at least 2^(8 - E), 2^E
+(E >= 0) above the largest scale of a value.  Half of the positions' weights are scaled by 2^-4 before the
+product with s (their codes are 16 times as large), so there three roundings add up: of p for the
+minima, of p / 16, and of its product with s: L 2^(E - 33) (max |v| + 16 * 15 (max s + 1)).
 Scores: fp32 sums of exact products of codes, 4 chained matrix products of terms up to 15 s |q|, at
 most four roundings each, and the minima's share: 2^-20 scale sum_d (15 s + |m|) |q_d| absolute, plus 2^-21 of the largest
 score for the exponent's argument; either changes a weight by as much relatively, and the
@@ -89,7 +91,7 @@ def _check(M, Hq, Hkv, P, T, group, seed, q_scale=1.0, mask=None, S=None, scale=
         delta[:, h, 0] = (2.0 ** -20 * abs(scale) * (qa[:, h] @ size[:, h // G].T).max(1) +
                           2.0 ** -21 * np.abs(oracle.bf16_bits_to_f64(q)[:, h] @ K[:, h // G].T * scale).max(1))
     E = max(0, math.frexp(float(vh[1].max()))[1])
-    tol = (2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * (3 * wabs + wmin) + n * 2.0 ** (E - 33) * (15 + np.abs(V).max()) +
+    tol = (2.0 ** -8 * np.abs(ref) + 2.0 ** -11 * (3 * wabs + wmin) + n * 2.0 ** (E - 33) * (np.abs(V).max() + 240 * (1 + float(vh[1].max()))) +
            2 * delta * wabs + 2.0 ** -18 * (15 * wstep + wmin))
     err = np.abs(got - ref)
     assert np.all(err <= tol), (what, float(err.max()), float((err / np.maximum(tol, 1e-300)).max()))
@@ -182,6 +184,37 @@ def test_kv4_attention_positions_that_nothing_wrote(group, junk):
     clean = _fill(k, v, S, group)
     same = _run(q, *clean, mask, M, Hq, Hkv, S, P, T, group, 0.1)
     assert np.isfinite(got).all() and np.array_equal(got, same)
+
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("M,Hq,Hkv,P,T", [(4, 8, 2, 37, 61), (6, 28, 4, 2048, 282), (8, 16, 2, 70000, 90)])
+def test_kv4_attention_large_scales_where_nothing_is_seen(M, Hq, Hkv, P, T, group):
+    """The same bits whatever finite scales and minima lie past the last position and at tree
+    positions that no row allows: 0x7777 is 30576, beside values of 2^-7 whose weights would
+    lose their bits to it."""
+    n = P + T + M
+    S = (n + 31) // 32 * 32 + 64
+    rng = np.random.default_rng([group, P])
+    q = _bf16(rng.standard_normal((M, Hq, D)))
+    k, v = _bf16(rng.standard_normal((n, Hkv, D))), _bf16(rng.standard_normal((n, Hkv, D)) * 2.0 ** -7)
+    hidden = rng.choice(T, T // 3, replace=False)
+    mask = rng.integers(0, 2 ** 32, (M, (T + M + 31) // 32), dtype=np.uint64).astype(np.uint32)
+    for j in hidden:
+        mask[:, j // 32] &= ~np.uint32(1 << (j % 32))
+    rows = np.arange(n, dtype=np.int32)
+    rows[P + hidden] = -1
+    got = []
+    for junk in (0, 0x77):
+        dk = torch.full((ss.subspec_kv4_bytes(Hkv, S, group),), junk, dtype=torch.uint8, device=DEV)
+        dv = torch.full_like(dk, junk)
+        ss.subspec_kv4_append(_dev(k), _dev(v), n, torch.from_numpy(rows).to(DEV), None, n, Hkv, S, 0, group, dk, dv)
+        got.append(_run(q, dk, dv, mask, M, Hq, Hkv, S, P, T, group, 0.1))
+    assert np.array_equal(*got)
+
+
+@pytest.mark.parametrize("q_scale", [1e-38, 5e37])
+def test_kv4_attention_scale_zero_for_any_q(q_scale):
+    _check(3, 8, 2, 200, 9, 64, 13, q_scale=q_scale, scale=0.0, what=f"q of {q_scale}, scale 0")
 
 
 @pytest.mark.parametrize("scale", [-0.05, 0.0, 1.0])

@@ -382,8 +382,8 @@ int subspec_qkv_rope(const void* qkv, int ld, const void* bias, const void* q_we
  * with a scale and a minimum each:
  *     m = fp16(min x),  s = fp16((max x - min x) / 15),
  *     c = clamp(rint((x - m) / s), 0, 15)  (s = 0: c = 0),      x stands as m + s c,
- * in fp32, ties to even; m and s round to nearest-even.  NaN counts as 0 and values past
- * +-65504 as that.  (The minimum and not a zero-point: it is exact for bf16 values of fp16's
+ * in fp32, ties to even; m and s round to nearest-even.  -0 lies below 0, NaN counts as 0 and
+ * values past +-65504 as that.  (The minimum and not a zero-point: it is exact for bf16 values of fp16's
  * range, also where a group's values all lie far from 0.)
  *
  * Layout ("kv4"): one buffer for keys and one for values, each [Hkv][S / 32] tiles of 32
@@ -434,9 +434,9 @@ int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, i
  *   mask     device uint32 [M][W], W = ceil((T + M) / 32), as subspec_tree_attention's
  *   out      device bf16 [M][Hq][128]; a query with no visible position gets zeros
  * Scores are fp32 sums over exact codes.  A position's weight is rounded to fp16, and its product
- * with the value's scale once more, before the second product, which sums in fp32: 11 bits,
- * fewer for weights below 2^(E - 20) of the heaviest (2^E, at least 1, the largest scale of a
- * value seen), none below 2^(E - 29).  What positions hold that no query sees changes no bit of the result.  Limits as
+ * with the value's scale once more, before the second product, which sums in fp32: 11 bits each, or
+ * 2^(E - 29) of the heaviest weight in absolute terms (2^E, at least 1, the largest scale of a
+ * value seen).  What positions hold that no query sees changes no bit of the result.  Limits as
  * subspec_tree_attention's (Hkv at most 65535, S a multiple of 32); q, caches and out
  * 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one where
  * a single range covers the positions); workspace as for subspec_qlinear

@@ -21,6 +21,7 @@ def kv4_quantize(x, group: int):
     x = np.nan_to_num(np.asarray(x, dtype=np.float32), nan=0.0, posinf=65504.0, neginf=-65504.0)
     x = np.clip(x, np.float32(-65504), np.float32(65504)).reshape(*x.shape[:-1], 128 // group, group)
     lo, hi = x.min(-1), x.max(-1)
+    lo = np.where((lo == 0) & ((x == 0) & np.signbit(x)).any(-1), np.float32(-0.0), lo)  # -0 lies below 0
     m = lo.astype(np.float16)
     s = ((hi - lo) / np.float32(15)).astype(np.float16)
     d = x - m.astype(np.float32)[..., None]

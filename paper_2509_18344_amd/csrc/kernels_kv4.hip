@@ -19,14 +19,12 @@ __global__ __launch_bounds__(kKv4Threads) void k_kv4_append(Kv4RowsArgs a) {
   const int n = a.count ? min(max(*a.count, 0), a.n) : a.n;
   if (tile * kKv4Tile - a.pos >= n) return;  // no position of this tile is written
   const size_t at = (static_cast<size_t>(g) * (a.S / kKv4Tile) + tile) * kv4_tile_bytes(G);
-  kv4_store_tile<G>(a.k_cache + at, a.v_cache + at, lds, [&](int w, int col, bool value, uint4& x) {
+  kv4_store_tile<G>(a.k_cache + at, a.v_cache + at, a.k, a.v, lds, [&](int w) {
     const int i = tile * kKv4Tile + w - a.pos;
-    if (i < 0 || i >= n) return false;
+    if (i < 0 || i >= n) return -1ll;
     const int src = a.rows ? a.rows[i] : i;
-    if (src < 0 || src >= a.src_rows) return false;
-    const uint16_t* row = (value ? a.v : a.k) + (static_cast<size_t>(src) * a.Hkv + g) * kKv4D + 8 * col;
-    x = *reinterpret_cast<const uint4*>(row);
-    return true;
+    if (src < 0 || src >= a.src_rows) return -1ll;
+    return (static_cast<long long>(src) * a.Hkv + g) * kKv4D;
   });
 }
 

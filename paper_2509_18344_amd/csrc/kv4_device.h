@@ -15,20 +15,18 @@
 
 namespace subspec {
 
-// 1 / s correctly rounded: the hardware's reciprocal (1 ulp) and one Newton step; checked for every
-// significand of an fp16 s.
-__device__ __forceinline__ float kv4_reciprocal(float s) {
-  const float y = __builtin_amdgcn_rcpf(s);
-  return __builtin_fmaf(__builtin_fmaf(-s, y, 1.f), y, y);
+// a / s correctly rounded, so that a tie of the rounding to a code falls as in exact arithmetic, given
+// 1 / s as the sum of two numbers: the hardware's reciprocal and what it leaves.  With a of 24 bits
+// and s of 11 no quotient lies nearer to the middle of two numbers than 2^-36 of itself, the
+// sum is within 2^-45 of 1 / s and the fma rounds once.
+struct Kv4Reciprocal {
+  float hi, lo;
+};
+__device__ __forceinline__ Kv4Reciprocal kv4_reciprocal(float s) {
+  const float hi = __builtin_amdgcn_rcpf(s);
+  return {hi, __builtin_fmaf(-s, hi, 1.f) * hi};
 }
-
-// a / s correctly rounded, given 1 / s, so that a tie of the rounding to a code falls as in
-// exact arithmetic: the product is off by an ulp or two, one step with its residual (exact
-// in an fma) corrects it.
-__device__ __forceinline__ float kv4_quotient(float a, float s, float inv) {
-  const float q = a * inv;
-  return __builtin_fmaf(__builtin_fmaf(-q, s, a), inv, q);
-}
+__device__ __forceinline__ float kv4_quotient(float a, Kv4Reciprocal r) { return __builtin_fmaf(a, r.hi, a * r.lo); }
 
 // min and max over the 8 or 16 lanes that hold a group of dimensions, in every lane
 template <int CTRL>
@@ -52,8 +50,6 @@ __device__ __forceinline__ void kv4_range(int& lo, int& hi) {
 // Numbers in an integer form that orders them (-0 below 0); the same function turns it back.
 __device__ __forceinline__ int kv4_order(int bits) { return bits ^ ((bits >> 31) & 0x7FFFFFFF); }
 
-typedef int16_t i16x2_t __attribute__((ext_vector_type(2)));
-
 struct Kv4Meta {
   _Float16 s, m;
 };
@@ -64,42 +60,46 @@ template <int G>
 __device__ __forceinline__ uint2 kv4_quantize(uint4 raw, Kv4Meta& meta) {
   float x[8];
   unpack8(raw, x);
-  // the range of pairs of bf16 values in their ordered 16-bit form (half the instructions of floats')
-  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-  i16x2_t plo, phi;
+  float lo = x[0], hi = x[0];  // NaN wins, -0 lies below 0
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const i16x2_t v = __builtin_bit_cast(i16x2_t, w[i]);
-    const i16x2_t k = v ^ ((v >> 15) & static_cast<int16_t>(0x7FFF));
-    plo = i == 0 ? k : __builtin_elementwise_min(plo, k);
-    phi = i == 0 ? k : __builtin_elementwise_max(phi, k);
+  for (int i = 1; i < 8; ++i) {
+    lo = __builtin_elementwise_minimum(lo, x[i]);
+    hi = __builtin_elementwise_maximum(hi, x[i]);
   }
-  int ilo = min(static_cast<int>(plo[0]), static_cast<int>(plo[1])), ihi = max(static_cast<int>(phi[0]), static_cast<int>(phi[1]));
+  int ilo = kv4_order(__float_as_int(lo)), ihi = kv4_order(__float_as_int(hi));
   kv4_range<G>(ilo, ihi);
-  float lo = __uint_as_float(static_cast<uint32_t>(ilo ^ ((ilo >> 31) & 0x7FFF)) << 16);
-  float hi = __uint_as_float(static_cast<uint32_t>(ihi ^ ((ihi >> 31) & 0x7FFF)) << 16);
-  // 0x477F is the largest bf16 within fp16's range; larger ones, infinities and NaN lie past it
-  if (__builtin_amdgcn_ballot_w64(ihi > 0x477F || ilo < -0x4780)) {
-    int flo = 0x7FFFFFFF, fhi = -0x7FFFFFFF;
+  // past fp16's range (as the bounds' next bf16 values are), infinities and NaN
+  if (__builtin_amdgcn_ballot_w64(ihi >= 0x47800000 || ilo <= kv4_order(static_cast<int>(0xC7800000u)))) {
+    ilo = 0x7FFFFFFF;
+    ihi = -0x7FFFFFFF;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -65504.f), 65504.f) : 0.f;
       const int k = kv4_order(__float_as_int(x[i]));
-      flo = min(flo, k);
-      fhi = max(fhi, k);
+      ilo = min(ilo, k);
+      ihi = max(ihi, k);
     }
-    kv4_range<G>(flo, fhi);
-    lo = __int_as_float(kv4_order(flo));
-    hi = __int_as_float(kv4_order(fhi));
+    kv4_range<G>(ilo, ihi);
   }
+  lo = __int_as_float(kv4_order(ilo));
+  hi = __int_as_float(kv4_order(ihi));
   meta.m = static_cast<_Float16>(lo);
-  meta.s = static_cast<_Float16>(kv4_quotient(hi - lo, 15.f, 0x1.111112p-4f));  // 1 / 15 rounded
+  constexpr Kv4Reciprocal kFifteenth{0x1.111112p-4f, -0x1.dddddep-29f};
+  meta.s = static_cast<_Float16>(kv4_quotient(hi - lo, kFifteenth));
   const float m = static_cast<float>(meta.m), s = static_cast<float>(meta.s);
-  const float inv = s > 0.f ? kv4_reciprocal(s) : 0.f;
+  const Kv4Reciprocal r = kv4_reciprocal(s);
+  float q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = kv4_quotient(x[i] - m, r);
+  // A scale that fp16 holds to 11 bits keeps every quotient below 15.5; below, and for 0, they may be anything.
+  if (__builtin_amdgcn_ballot_w64(s < 0x1p-14f)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = s == 0.f ? 0.f : fminf(q[i], 15.f);
+  }
   uint32_t code[2] = {0, 0};
 #pragma unroll
-  for (int i = 0; i < 8; ++i)  // (the conversion takes negative numbers to 0)
-    code[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(fminf(rintf(kv4_quotient(x[i] - m, s, inv)), 15.f), i % 4, code[i / 4]);
+  for (int i = 0; i < 8; ++i)  // (the conversion rounds to nearest-even and takes negative numbers to 0)
+    code[i / 4] = __builtin_amdgcn_cvt_pk_u8_f32(q[i], i % 4, code[i / 4]);
   return make_uint2(code[0], code[1]);
 }
 
@@ -120,22 +120,26 @@ struct Kv4TileLds {
   uint32_t live;                                 // positions that are written
 };
 
-// One tile of one head: 256 threads write the positions that are live.  `load(w, col, value, x)`
-// puts dimensions 8 col .. of position w's key or value (bf16) into x and says whether the
-// position is written; the 16 lanes of a row agree.  The tile is put together in LDS and written
+// One tile of one head: 256 threads write the positions that are live.  `source(w)` is where
+// position w's row of 128 starts in k and v (bf16), or negative where the position is not written.  The tile is put together in LDS and written
 // 16 bytes a thread; where only some positions are live, their parts of it, and words that
 // hold codes of other positions too (a value's hold 8) are merged with what they held: a
 // tile belongs to one workgroup and a word to one thread.
-template <int G, typename Load>
-__device__ __forceinline__ void kv4_store_tile(uint8_t* kt, uint8_t* vt, Kv4TileLds& L, Load load) {
+template <int G, typename Source>
+__device__ __forceinline__ void kv4_store_tile(uint8_t* kt, uint8_t* vt, const uint16_t* k, const uint16_t* v, Kv4TileLds& L,
+                                               Source source) {
   const int t = threadIdx.x, col = t % 16, r = t / 16;
   if (t == 0) L.live = 0;
   uint4 x[2][2];
   bool live[2];
+  const long long at[2] = {source(r), source(16 + r)};
 #pragma unroll
   for (int b = 0; b < 2; ++b) {  // all of the workgroup's rows in flight
-    live[b] = load(16 * b + r, col, false, x[b][0]);
-    (void)load(16 * b + r, col, true, x[b][1]);
+    live[b] = at[b] >= 0;
+    if (live[b]) {
+      x[b][0] = *reinterpret_cast<const uint4*>(k + at[b] + 8 * col);
+      x[b][1] = *reinterpret_cast<const uint4*>(v + at[b] + 8 * col);
+    }
   }
   __syncthreads();
 #pragma unroll

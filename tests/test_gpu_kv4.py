@@ -124,6 +124,33 @@ def test_kv4_read_rounds_the_held_values_once(group, n, Hkv, S, pos):
         assert np.all(err <= step * (0.5 + 15 * 2.0 ** -11) + 2.0 ** -11 * np.abs(x).max(-1) + 2.0 ** -24)
 
 
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("kind", ["halves", "wide", "tiny", "zeros"])
+def test_kv4_append_rounds_codes_to_nearest_even(kind, group):
+    """Quotients that are ties (whole and half numbers over scales of 2^j (1 + i / 32)), rows whose numbers
+    span many exponents, scales that fp16 holds to few bits, zeros of either sign."""
+    rng = np.random.default_rng([len(kind), group])
+    n, Hkv, S = 500, 2, 512
+    shape = (n, Hkv, 128)
+    if kind == "halves":
+        x = rng.integers(0, 31, shape) * 0.5
+        x[..., 0::64], x[..., 1::64] = 0.0, 15.0  # a scale of 1 times the row's factor
+        x = x * (2.0 ** rng.integers(-9, 10, (n, Hkv, 1))) * rng.choice([1.0, -1.0], (n, Hkv, 1))
+    elif kind == "wide":
+        x = rng.standard_normal(shape) * 2.0 ** rng.integers(-30, 16, shape)
+    elif kind == "tiny":
+        x = rng.standard_normal(shape) * 2.0 ** rng.integers(-28, -8, (n, Hkv, 1))
+    else:
+        x = rng.choice([0.0, -0.0], shape) * np.where(rng.random((n, Hkv, 1)) < 0.5, 0.0, 1.0)
+        x[::3, :, 5] = 2.0 ** -20
+    bits = synth.bf16_bits(torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16))
+    cache = np.zeros((Hkv, oracle.kv4_bytes(1, S, group)), np.uint8)
+    dk, dv = torch.from_numpy(cache).to(DEV), torch.from_numpy(cache).to(DEV)
+    ss.subspec_kv4_append(_dev(bits), _dev(bits), n, None, None, n, Hkv, S, 0, group, dk, dv)
+    assert np.array_equal(dk.cpu().numpy(), _expect(cache, bits, range(n), group, False))
+    assert np.array_equal(dv.cpu().numpy(), _expect(cache, bits, range(n), group, True))
+
+
 def test_kv4_append_zero_rows_and_many_tiles():
     rng = np.random.default_rng(5)
     Hkv, group, n = 2, 64, 3000

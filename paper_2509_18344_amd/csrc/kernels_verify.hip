@@ -155,11 +155,9 @@ __device__ __forceinline__ bool last_to_arrive(unsigned* cnt, unsigned of, int* 
   return *flag != 0;
 }
 
-// Token j continues `row` (a parent that does not come before it, or a token outside the
+// Token j continues `row` (a parent p that does not come before it, or a token k outside the
 // vocabulary, continues nothing).
-__device__ __forceinline__ bool continues(const VerifyArgs& a, int j, int row, int* token) {
-  const int p = a.parent[j], k = a.token[j];
-  *token = k;
+__device__ __forceinline__ bool continues(const VerifyArgs& a, int j, int p, int k, int row) {
   return p + 1 == row && p >= -1 && p < j && k >= 0 && k < a.V;
 }
 
@@ -193,8 +191,8 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
   __syncthreads();
   // the row's children, in any order; their logits arrive while the row streams
   for (int j = t; j < a.N; j += kRowThreads) {
-    int k;
-    if (continues(a, j, row, &k)) {
+    const int k = a.token[j];
+    if (continues(a, j, a.parent[j], k, row)) {
       const int at = atomicAdd(&n, 1);
       kids.j[at] = j;
       kids.token[at] = k;
@@ -373,14 +371,16 @@ __device__ __forceinline__ void drop_tokens(const int* kids, int n, int v0, doub
   }
 }
 
-// e^((l - m) / T) of this thread's 8 logits, drafted tokens and logits past the vocabulary zero.
-__device__ __forceinline__ void residual_terms(const VerifyArgs& a, const int* kids, int n, const uint16_t* l, float m,
-                                               int v0, double (&e)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) e[i] = 0.0;
-  if (v0 >= a.V) return;
+// 8 logits at v0, or -inf past the vocabulary.
+__device__ __forceinline__ uint4 load_logits(const VerifyArgs& a, const uint16_t* l, int v0) {
+  return v0 < a.V ? *reinterpret_cast<const uint4*>(l + v0) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+}
+
+// e^((l - m) / T) of 8 logits at v0, drafted tokens zero.
+__device__ __forceinline__ void residual_terms(const VerifyArgs& a, const int* kids, int n, uint4 raw, float m, int v0,
+                                               double (&e)[8]) {
   float x[8];
-  split8(*reinterpret_cast<const uint4*>(l + v0), x);
+  split8(raw, x);
 #pragma unroll
   for (int i = 0; i < 8; ++i) e[i] = exp((static_cast<double>(x[i]) - static_cast<double>(m)) * a.inv_t);
   drop_tokens(kids, n, v0, e);
@@ -398,7 +398,8 @@ __device__ __forceinline__ void pick_residual(const VerifyArgs& a, int row, floa
     const double target = fmax(static_cast<double>(a.uniform[row]) * (rest + drafted) - drafted, 0.0);
     double before = 0.0, unused, e[8];
     const int slice = find_term(x, 0, 0.0, target, &before);
-    residual_terms(a, kid, n, l, m, slice * kVerifySlice + 8 * t, e);
+    const int v0 = slice * kVerifySlice + 8 * t;
+    residual_terms(a, kid, n, load_logits(a, l, v0), m, v0, e);
     double s = 0.0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += e[i];
@@ -432,30 +433,44 @@ __device__ __forceinline__ void pick_residual(const VerifyArgs& a, int row, floa
 }
 
 __global__ __launch_bounds__(kResThreads) void k_verify_residual(VerifyArgs a) {
+  constexpr int kOwn = kVerifyMaxTokens / kResThreads;  // drafted tokens a thread looks at
   __shared__ int kid_j[kVerifyMaxTokens], kid[kVerifyMaxTokens];  // the row's drafted tokens
+  __shared__ float kid_l[kVerifyMaxTokens];                       // and their logits
   __shared__ double part[2][kResWaves], share[kVerifyMaxTokens];
   __shared__ int n, flag;
   const int t = threadIdx.x, wave = t / kWave;
+  // The tree's loads before the row's, which wait for the path's end.
+  int parent[kOwn], token[kOwn];
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int j = t + i * kResThreads;
+    parent[i] = j < a.N ? a.parent[j] : INT_MAX - 1;
+    token[i] = j < a.N ? a.token[j] : 0;
+  }
   const int row = *a.last_row;
   const float2 st = *a.last_stat;
   if (!(st.y > 0.f)) {  // no distribution (the same for every workgroup)
     if (blockIdx.x == 0 && t == 0) *a.next_token = -1;
     return;
   }
+  const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
+  const int v0 = blockIdx.x * kVerifySlice + 8 * t;
+  const uint4 raw = load_logits(a, l, v0);
   if (t == 0) n = 0;
   __syncthreads();
-  for (int j = t; j < a.N; j += kResThreads) {
-    int k;
-    if (continues(a, j, row, &k)) {
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const int j = t + i * kResThreads;
+    if (continues(a, j, parent[i], token[i], row)) {
       const int at = atomicAdd(&n, 1);
       kid_j[at] = j;
-      kid[at] = k;
+      kid[at] = token[i];
+      kid_l[at] = __uint_as_float(static_cast<uint32_t>(l[token[i]]) << 16);
     }
   }
   __syncthreads();
-  const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
   double e[8];
-  residual_terms(a, kid, n, l, st.x, blockIdx.x * kVerifySlice + 8 * t, e);
+  residual_terms(a, kid, n, raw, st.x, v0, e);
   double s = 0.0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) s += e[i];
@@ -490,8 +505,7 @@ __global__ __launch_bounds__(kResThreads) void k_verify_residual(VerifyArgs a) {
       repeat |= first && kid[i] == kid[k];
     }
     share[rank] = repeat ? 0.0
-                         : exp((static_cast<double>(__uint_as_float(static_cast<uint32_t>(l[kid[k]]) << 16)) -
-                                static_cast<double>(st.x)) * a.inv_t);
+                         : exp((static_cast<double>(kid_l[k]) - static_cast<double>(st.x)) * a.inv_t);
   }
   __syncthreads();
   double drafted = 0.0;
@@ -517,8 +531,8 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
   if (v0 < a.V) raw = *reinterpret_cast<const uint4*>(l + v0);
   if (t == 0) n = 0;
   __syncthreads();
-  int token;
-  if (t < a.N && continues(a, t, row, &token)) {  // the row's children, in any order
+  const int token = t < a.N ? a.token[t] : -1, parent = t < a.N ? a.parent[t] : -1;
+  if (continues(a, t, parent, token, row)) {  // the row's children, in any order
     const int at = atomicAdd(&n, 1);
     kid_j[at] = t;
     kid[at] = token;
@@ -645,7 +659,7 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
     const int at = kSlices * lane + i;
     y[i] = at < slices ? get(a.slice_sum + end * slices + at) : 0.0;
   }
-  if (t < a.N && continues(a, t, end, &token)) kid[atomicAdd(&n, 1)] = token;
+  if (continues(a, t, parent, token, end)) kid[atomicAdd(&n, 1)] = token;
   __syncthreads();
   if (rest != rest) {  // no distribution
     if (t == 0) *a.next_token = -1;

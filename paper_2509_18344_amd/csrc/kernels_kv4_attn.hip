@@ -35,12 +35,13 @@
 // output itself.
 //
 // Measured (a call, both kernels): 131138 positions of 8 heads in groups of 64, 30 query rows a head:
-// 302 MB in 40 to 43 us, 7.0 to 7.6 TB/s (part of the cache stays in the last-level cache between
-// calls); the first kernel's vector ALUs are busy two thirds of its time, so unpacking and the
-// softmax bound it, not loads.  8407 positions of 8 heads in groups of 128, 64 rows a head: 18 MB in
-// 17 us, a chain of the launch with the first loads (3.4 us), two or three tiles a wavefront (1.2 to
-// 2 each), the merge (1 to 2.5) and the second kernel (2.5 to 3.3).  2336 positions of 4 heads,
-// 42 rows: 10.5 us, the same chain with one or two tiles.
+// 151 MB of cache in 40 us, 3.8 TB/s, where a sum over as much memory reads 4.0; the first kernel's
+// vector ALUs are busy two thirds of its time, so unpacking and the softmax come next.  8407
+// positions of 8 heads in groups of 128, 64 rows a head: 9 MB in 16.6 us, a chain of the launch with
+// the first loads (3.4 us), four or five tiles a wavefront (1.2 to 2 each), the merge (1 to 2.5) and the
+// second kernel (2.5 to 3.3).  2336 positions of 4 heads, 42 rows: 10.3 us, the same chain with one
+// tile; 16385 of 8 heads with 5 rows 9.9 us.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -707,18 +708,21 @@ __global__ __launch_bounds__(kCombineThreads) void k_kv4_combine(Kv4AttnArgs a) 
   }
 }
 
-// How a call is cut: wavefronts of QW query tiles, QG of them on a tile of positions, each
-// taking `per_wave` tiles of a range.
+// How a call is cut: wavefronts of QW query tiles, QG of them on a tile of positions, and ranges of
+// `tiles` tiles.
 struct Kv4Shape {
-  int qw, qg, per_wave;
+  int qw, qg, tiles;
   bool ring;
 };
 
+// A range has a workgroup, and there are as many as CUs (16385 positions of eight heads with 5 rows
+// 9.9 us; with ranges of whole turns of a workgroup's wavefronts, 171 workgroups, 10.4), but no
+// wavefront goes without a tile.
 // Up to kAlone tiles a wavefront one workgroup takes a whole head, and the second kernel is saved (300
 // positions of four heads 7.3 us a call against 10.0, 800 8.7 against 9.9; at five tiles 9.8 either way).
 // From kRingFrom tiles on the ring in LDS gets ahead of its wavefront (131138 positions of eight heads, 17
 // tiles: 42.6 us against 47.8 from registers, and with one query tile a wavefront 51.1; at three
-// tiles 12.9 against 11.7), and two query tiles a wavefront share the unpacking.
+// tiles 11.3 against 9.9), and two query tiles a wavefront share the unpacking.
 constexpr int kAlone = 4, kRingFrom = 5;
 
 Kv4Shape kv4_shape(int M, int Hq, int Hkv, int P, int T) {
@@ -728,10 +732,9 @@ Kv4Shape kv4_shape(int M, int Hq, int Hkv, int P, int T) {
   auto cut = [&](int qw) {
     const int qg = qt <= qw ? 1 : qt <= 2 * qw ? 2 : 4;
     const int at_once = kWaves / qg;
-    int per_wave = (tiles + ranges * at_once - 1) / (ranges * at_once);
-    const int alone = (tiles + at_once - 1) / at_once;
-    if (alone <= kAlone) per_wave = alone;
-    return Kv4Shape{qw, qg, per_wave, per_wave >= kRingFrom};
+    int tiles_a_split = std::max((tiles + ranges - 1) / ranges, at_once);
+    if (tiles <= kAlone * at_once) tiles_a_split = tiles;
+    return Kv4Shape{qw, qg, tiles_a_split, (tiles_a_split + at_once - 1) / at_once >= kRingFrom};
   };
   if (qt > 1) {
     const Kv4Shape wide = cut(2);
@@ -762,7 +765,7 @@ void launch_narrow(const Kv4AttnArgs& a, int groups, bool ring, hipStream_t st) 
 void kv4_attn_plan(int M, int Hq, int Hkv, int P, int T, int* splits, int* tiles_per_split) {
   const int tiles = (P + T + M + kKv4Tile - 1) / kKv4Tile;
   const Kv4Shape sh = kv4_shape(M, Hq, Hkv, P, T);
-  *tiles_per_split = sh.per_wave * (kWaves / sh.qg);
+  *tiles_per_split = sh.tiles;
   *splits = (tiles + *tiles_per_split - 1) / *tiles_per_split;
 }
 

@@ -671,8 +671,8 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
 }  // namespace
 
 void verify_plan(int N, int V, int* chunks, int* chunk_len) {
-  // about 640 workgroups (three slices of 289 rows: 30.8 us; one 38, eight 36), each with at least one
-  // round of loads
+  // about 640 workgroups (289 rows in three to seven slices 30.8 us alike, in one 38), each with at
+  // least one round of loads
   int c = (640 + N) / (N + 1);
   const int most = (V + 8 * kRowThreads * kRowLoads - 1) / (8 * kRowThreads * kRowLoads);
   if (c > most) c = most;

@@ -1134,52 +1134,41 @@ namespace {
 
 bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Checks shared by the entry points that prepare queries and keys; fills *a but for its outputs.
-int rope_args(const char* fn, const void* qkv, int ld, const void* bias, const void* q_weight, const void* k_weight,
-              float eps, const int* positions, const double* inv_freq, int rot, int interleaved, int M, int Hq,
-              int Hkv, const void* q, subspec::RopeArgs* a) {
-  if (!qkv || !q) return fail(SUBSPEC_EINVAL, "%s: null pointer argument", fn);
-  if (rot < 0 || rot > 128 || rot % 16) return fail(SUBSPEC_EUNSUPPORTED, "%s: rot=%d: must be a multiple of 16 in 0..128", fn, rot);
-  if (rot && (!positions || !inv_freq)) return fail(SUBSPEC_EINVAL, "%s: null positions or inv_freq", fn);
-  if (!aligned16(qkv) || !aligned16(bias) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(q))
-    return fail(SUBSPEC_EINVAL, "%s: rows, bias, weights and outputs must be 16-byte aligned", fn);
-  if (!aligned_to(positions, 4) || !aligned_to(inv_freq, 8))
-    return fail(SUBSPEC_EINVAL, "%s: positions must be 4-byte and inv_freq 8-byte aligned", fn);
-  if (interleaved != 0 && interleaved != 1) return fail(SUBSPEC_EINVAL, "%s: interleaved must be 0 or 1", fn);
-  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SUBSPEC_EINVAL, "%s: eps must be finite and not negative", fn);
-  if (M < 1 || M > (1 << 20)) return fail(SUBSPEC_EUNSUPPORTED, "%s: M=%d: must be in 1..2^20", fn, M);
-  if (Hq < 1 || Hkv < 1 || static_cast<long long>(Hq) + 2ll * Hkv > 65536)
-    return fail(SUBSPEC_EUNSUPPORTED, "%s: Hq=%d, Hkv=%d: must be positive, Hq + 2 Hkv at most 65536", fn, Hq, Hkv);
-  if (ld % 8 || ld < (Hq + 2 * Hkv) * 128)
-    return fail(SUBSPEC_EINVAL, "%s: ld=%d: must be a multiple of 8 and at least (Hq + 2 Hkv) * 128", fn, ld);
-  a->qkv = static_cast<const uint16_t*>(qkv);
-  a->bias = static_cast<const uint16_t*>(bias);
-  a->q_weight = static_cast<const uint16_t*>(q_weight);
-  a->k_weight = static_cast<const uint16_t*>(k_weight);
-  a->positions = positions;
-  a->inv_freq = inv_freq;
-  a->ld = ld;
-  a->rot = rot;
-  a->interleaved = interleaved;
-  a->M = M;
-  a->Hq = Hq;
-  a->Hkv = Hkv;
-  a->eps = eps;
-  a->q = static_cast<uint16_t*>(const_cast<void*>(q));
-  return SUBSPEC_OK;
-}
-
 }  // namespace
 
 int subspec_qkv_rope(const void* qkv, int ld, const void* bias, const void* q_weight, const void* k_weight, float eps,
                      const int* positions, const double* inv_freq, int rot, int interleaved, int M, int Hq, int Hkv,
                      void* q, void* k_new, void* v_new, hipStream_t stream) {
+  if (!qkv || !q || !k_new || !v_new) return fail(SUBSPEC_EINVAL, "qkv_rope: null pointer argument");
+  if (rot < 0 || rot > 128 || rot % 16) return fail(SUBSPEC_EUNSUPPORTED, "qkv_rope: rot=%d: must be a multiple of 16 in 0..128", rot);
+  if (rot && (!positions || !inv_freq)) return fail(SUBSPEC_EINVAL, "qkv_rope: null positions or inv_freq");
+  if (!aligned16(qkv) || !aligned16(bias) || !aligned16(q_weight) || !aligned16(k_weight) || !aligned16(q) ||
+      !aligned16(k_new) || !aligned16(v_new))
+    return fail(SUBSPEC_EINVAL, "qkv_rope: rows, bias, weights and outputs must be 16-byte aligned");
+  if (!aligned_to(positions, 4) || !aligned_to(inv_freq, 8))
+    return fail(SUBSPEC_EINVAL, "qkv_rope: positions must be 4-byte and inv_freq 8-byte aligned");
+  if (interleaved != 0 && interleaved != 1) return fail(SUBSPEC_EINVAL, "qkv_rope: interleaved must be 0 or 1");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SUBSPEC_EINVAL, "qkv_rope: eps must be finite and not negative");
+  if (M < 1 || M > (1 << 20)) return fail(SUBSPEC_EUNSUPPORTED, "qkv_rope: M=%d: must be in 1..2^20", M);
+  if (Hq < 1 || Hkv < 1 || static_cast<long long>(Hq) + 2ll * Hkv > 65536)
+    return fail(SUBSPEC_EUNSUPPORTED, "qkv_rope: Hq=%d, Hkv=%d: must be positive, Hq + 2 Hkv at most 65536", Hq, Hkv);
+  if (ld % 8 || ld < (Hq + 2 * Hkv) * 128)
+    return fail(SUBSPEC_EINVAL, "qkv_rope: ld=%d: must be a multiple of 8 and at least (Hq + 2 Hkv) * 128", ld);
   subspec::RopeArgs a{};
-  const int rc = rope_args("qkv_rope", qkv, ld, bias, q_weight, k_weight, eps, positions, inv_freq, rot, interleaved, M,
-                           Hq, Hkv, q, &a);
-  if (rc) return rc;
-  if (!k_new || !v_new) return fail(SUBSPEC_EINVAL, "qkv_rope: null pointer argument");
-  if (!aligned16(k_new) || !aligned16(v_new)) return fail(SUBSPEC_EINVAL, "qkv_rope: outputs must be 16-byte aligned");
+  a.qkv = static_cast<const uint16_t*>(qkv);
+  a.bias = static_cast<const uint16_t*>(bias);
+  a.q_weight = static_cast<const uint16_t*>(q_weight);
+  a.k_weight = static_cast<const uint16_t*>(k_weight);
+  a.positions = positions;
+  a.inv_freq = inv_freq;
+  a.ld = ld;
+  a.rot = rot;
+  a.interleaved = interleaved;
+  a.M = M;
+  a.Hq = Hq;
+  a.Hkv = Hkv;
+  a.eps = eps;
+  a.q = static_cast<uint16_t*>(q);
   a.k = static_cast<uint16_t*>(k_new);
   a.v = static_cast<uint16_t*>(v_new);
   const hipError_t e = subspec::launch_qkv_rope(a, stream);

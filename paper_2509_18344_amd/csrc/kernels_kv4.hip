@@ -4,6 +4,11 @@
 // A workgroup takes one tile of 32 positions of one key/value head, 16 lanes of 8 dimensions
 // a row: a row's range is three or four DPP steps, a key's 8 codes are one word, and the
 // values' codes turn in LDS into words of 8 positions each.
+//
+// Measured, 16384 positions of 8 heads in groups of 128: append 22.8 us for 67 MB read and 18 written,
+// 3.7 TB/s (about 110 vector instructions a row of 8 dimensions come next to the memory's
+// 15.6 us at a large copy's rate), read 15.7 us for the same bytes, 5.4 TB/s: bound by memory.  A few
+// rows 4.0 and 3.3 us, the launch and one chain of loads.
 #include "kv4_device.h"
 
 namespace subspec {

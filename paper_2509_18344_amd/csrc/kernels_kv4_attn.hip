@@ -481,11 +481,11 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2
         kv4_to_lds<16>(kt, l16, to);
         kv4_to_lds<16>(kt + 1024, l16, to + 1024);
         if (G == 2 || lane < 32) {  // scales and minima: 128 G bytes a side
-          kv4_to_lds<4>(kt + kKv4CodeBytes, l4, to + 4096);
-          kv4_to_lds<4>(vt + kKv4CodeBytes, l4, to + 4096 + 128 * G);
+          kv4_to_lds<4>(kt + kKv4CodeBytes, l4, to + 4 * 1024);
+          kv4_to_lds<4>(vt + kKv4CodeBytes, l4, to + 4 * 1024 + 128 * G);
         }
-        kv4_to_lds<16>(vt, l16, to + 2048);
-        kv4_to_lds<16>(vt + 1024, l16, to + 3072);
+        kv4_to_lds<16>(vt, l16, to + 2 * 1024);
+        kv4_to_lds<16>(vt + 1024, l16, to + 3 * 1024);
       } else {
         const uint8_t* kt = kbase + static_cast<size_t>(last - 1) * kv4_tile_bytes(G);
 #pragma unroll

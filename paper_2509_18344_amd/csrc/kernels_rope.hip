@@ -11,6 +11,10 @@
 // same row.  Its first rot / 2 threads compute the token's angles once, in LDS, and a lane holds
 // those of its dimensions for all heads.  Few tokens: a workgroup for every 16 heads
 // instead, so that their loads are all in flight.
+//
+// Measured: 4096 tokens of 56 heads with bias and norms 25.2 us, 117 MB at 4.7 TB/s, where a large
+// copy moves 5.5: bound by memory.  One token 2.4 us, of which a launch that does nothing is about
+// 2; a call from Python costs 7.
 #include "rope_device.h"
 
 namespace subspec {
@@ -19,7 +23,9 @@ namespace {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeHeads = kRopeThreads / 16;
-constexpr int kRopeWhole = 512;  // tokens from which a workgroup takes all heads of its token
+// Tokens from which a workgroup takes all heads of its token (56 heads: 128 tokens 3.6 us against 3.1 in
+// workgroups of 16 heads, 256 4.1 against 4.0, 400 5.0 against 5.5, 4096 24 against 40).
+constexpr int kRopeWhole = 320;
 constexpr int kRopeAhead = 4;  // head rows of a thread in flight
 
 template <bool FULL>

@@ -22,6 +22,9 @@
 //   k_verify_residual  the last row's other tokens in 64 bits: with V = 152064 tokens the
 //                      borders lie 10^-5 apart, and a sum in 32 bits, 10^-7 off, would pick a
 //                      neighbour in one call of a hundred; the last workgroup finds the token
+// Measured, 288 tokens at V = 152064: 88 MB, k_verify_rows 23.7 us (3.7 TB/s, where a sum over as much
+// memory reads 4.0: bound by memory; greedy 21.7), k_verify_residual 8.4, a chain of dependent
+// loads and two reductions; 31 us a call, greedy 21.5.
 #include <algorithm>
 #include <climits>
 #include <cmath>

@@ -1,5 +1,5 @@
-// Bias, norm and position rotation of one head row, 16 lanes of 8 dimensions each: shared
-// by the kernels that prepare queries, keys and values.
+// Norm and position rotation of one head row, 16 lanes of 8 dimensions, and the rows'
+// packing that the 4-bit cache's kernels use too.
 #pragma once
 
 #include "device_common.h"

@@ -1,5 +1,6 @@
-"""MI355X (gfx950) low-bit substitute layers of SubSpec (Sec. 4.1), and the draft-tree
-expansion step that follows every draft pass (Sec. 4.2).
+"""MI355X (gfx950) low-bit substitute layers of SubSpec (Sec. 4.1), the draft pass around them
+(queries, keys and values from the fused projection, tree attention over a 16-bit or a 4-bit
+cache, the draft-tree expansion of Sec. 4.2) and the verification of the drafted tree.
 
 The compute path is the native library ``libsubspec.so`` (hand-written HIP,
 C ABI in ``include/subspec.h``); this package only marshals arguments to it.

@@ -9,7 +9,7 @@ namespace subspec {
 constexpr int kVerifyMaxTokens = 1024;
 constexpr int kVerifyMaxV = 1 << 20;
 constexpr int kVerifySlice = 2048;  // logits per workgroup of the kernels in 64 bits
-constexpr int kVerifySmall = 1600;   // slices in all up to which one kernel does everything
+constexpr int kVerifySmall = 2200;   // slices in all up to which one kernel does everything
 
 struct VerifyArgs {
   const uint16_t* logits;  // bf16 [N + 1][V]
@@ -28,9 +28,8 @@ struct VerifyArgs {
   float2* last_stat;       // [1] row_stat of the path's last row
   int* last_row;           // [1]
   double* slice_sum;       // [ceil(V / kVerifySlice)] the last row's sums without its children (small calls: every row's)
-  double* row_rest;        // small calls: [N + 1] a row's sum without its children, and theirs
-  float* row_max;          // small calls: [N + 1]
   float* slice_max;        // small calls: [N + 1][ceil(V / kVerifySlice)] the slices' maxima
+  int* row_token;          // small calls: [N + 1] the token of a row that ends the path
   int* path;               // [N]
   int* accepted;           // [1]
   int* next_token;         // [1]

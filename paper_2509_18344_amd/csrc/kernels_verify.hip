@@ -13,10 +13,10 @@
 // child it picks, not the whole distribution.
 // Up to kVerifySmall slices of 2048 logits in all one kernel does everything in 64 bits
 // (k_verify_small: a slice its maximum and its sum without the row's children, the last workgroup of a
-// row the row's pick, the last of all path and token: a chain of 4 at V = 32000 11.5 us a call
-// against 15.1 with two kernels, 20 tokens at V = 152064, 1575 slices, 14.9 against 17.4; 99 at
-// 32000, 1600, 15.4 against 15.7).  Beyond, two, since 64-bit exponentials of all logits would bound
-// them:
+// row the row's pick and, where that ends the path, its token, the last of all the path: a chain of 4 at
+// V = 32000 9.9 us a call against 15.2 with two kernels, 26 tokens at V = 152064, 2025 slices, 15.3
+// against 18.2; 130 at 32000, 2096, 16.9 against 16.8).  Beyond, two, since 64-bit exponentials of all
+// logits would bound them:
 //   k_verify_rows      per (row, slice) workgroup the maximum and the sum, in 32 bits; the last
 //                      of a row finds the child that the row picks, the last of all the path
 //   k_verify_residual  the last row's other tokens in 64 bits: with V = 152064 tokens the
@@ -389,11 +389,11 @@ __device__ __forceinline__ void residual_terms(const VerifyArgs& a, const int* k
   drop_tokens(kids, n, v0, e);
 }
 
-// The token that the residual of `row` gives to its uniform number, written by the calling (last)
+// The token that the residual of `row` gives to its uniform number, into *out by the calling
 // workgroup.  x: a lane's kSlices slice sums (the same in every wavefront), `rest` their sum,
 // `drafted` the drafted tokens' share, all relative to the maximum m; kid: the drafted tokens.
 __device__ __forceinline__ void pick_residual(const VerifyArgs& a, int row, float m, const double (&x)[kSlices], double rest,
-                                              double drafted, const int* kid, int n, double* part) {
+                                              double drafted, const int* kid, int n, double* part, int* out) {
   const int t = threadIdx.x, wave = t / kWave;
   const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
   int token = -1;
@@ -411,7 +411,7 @@ __device__ __forceinline__ void pick_residual(const VerifyArgs& a, int row, floa
     __syncthreads();
     // The wavefront in whose share the target falls, or the last with a share.
     double start = before;
-    int owner = -1;
+    int owner = 0;  // (with no share anywhere find_term gives -1)
     double owner_start = 0.0;
     for (int w = 0; w < kResWaves; ++w) {
       const double up = start + part[w];
@@ -424,14 +424,14 @@ __device__ __forceinline__ void pick_residual(const VerifyArgs& a, int row, floa
     }
     if (wave != owner) return;
     token = find_term(e, slice * kVerifySlice + 8 * kWave * wave, owner_start, target, &unused);
-    if (t % kWave == 0) *a.next_token = token;
+    if (t % kWave == 0) put(out, token);
     return;
   }
   // The drafted tokens hold everything, and rounding kept u from all of them: the last of them.
   if (t == 0) {
     for (int i = 0; i < n; ++i)
       if (__uint_as_float(static_cast<uint32_t>(l[kid[i]]) << 16) > -INFINITY) token = max(token, kid[i]);
-    *a.next_token = token;
+    put(out, token);
   }
 }
 
@@ -514,15 +514,15 @@ __global__ __launch_bounds__(kResThreads) void k_verify_residual(VerifyArgs a) {
   double drafted = 0.0;
   for (int k = t % kWave; k < n; k += kWave) drafted += share[k];
   drafted = wave_add(drafted);
-  pick_residual(a, row, st.x, x, rest, drafted, kid, n, part[1]);
+  pick_residual(a, row, st.x, x, rest, drafted, kid, n, part[1], a.next_token);
 }
 
 // Everything in one kernel, workgroup (row, slice of 2048 logits); the last workgroup of a row finds
-// the row's pick, the last of all the path and the token.
+// the row's pick, its residual's too, the last of all the path.
 __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
-  __shared__ double share[kResThreads], part[2][kResWaves];
+  __shared__ double sums[kSlices * kWave], share[kResThreads], part[2][kResWaves];
   __shared__ float wm[2][kResWaves];
-  __shared__ int kid_j[kResThreads], kid[kResThreads], order[kResThreads], next[kResThreads];
+  __shared__ int kid_j[kResThreads], kid[kResThreads], order[kResThreads], next[kResThreads], end_token[kResThreads];
   __shared__ float kid_l[kResThreads];
   __shared__ int n, flag;
   const int t = threadIdx.x, wave = t / kWave, lane = t % kWave;
@@ -588,16 +588,12 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kResWaves; ++w) rm = fmaxf(rm, wm[1][w]);
-  double rest = 0.0;
 #pragma unroll
   for (int i = 0; i < kRowSlices; ++i) {
     // (a slice of -inf alone has nothing; a NaN stays one)
     if (v[i] != 0.0) v[i] *= exp((static_cast<double>(vm[i]) - static_cast<double>(rm)) * a.inv_t);
-    if (t + i * kResThreads < slices) put(a.slice_sum + row * slices + t + i * kResThreads, v[i]);
-    rest += v[i];
+    sums[t + i * kResThreads] = v[i];
   }
-  rest = wave_add(rest);
-  if (lane == 0) part[1][wave] = rest;
   // its children's shares in index order, a repeated token's 0
   const int nk = n;
   if (t < nk) {
@@ -612,63 +608,48 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
     share[rank] = repeat || kid_l[t] == -INFINITY ? 0.0 : exp((static_cast<double>(kid_l[t]) - static_cast<double>(rm)) * a.inv_t);
   }
   __syncthreads();
-  if (t == 0) {
-    rest = 0.0;
+  // Every thread's own, in the same order: the sums, and the first child whose interval holds u.
+  double y[kSlices], rest = 0.0, drafted = 0.0;
 #pragma unroll
-    for (int w = 0; w < kResWaves; ++w) rest += part[1][w];
-    const bool ok = fabsf(rm) < INFINITY && rest == rest;
-    double drafted = 0.0;
-    for (int k = 0; k < nk; ++k) drafted += share[k];
-    int pick = -1;
-    if (ok) {
-      const double target = static_cast<double>(a.uniform[row]) * (rest + drafted);
-      double f = 0.0;
-      for (int k = 0; k < nk; ++k) {
-        const double f2 = f + share[k];
-        if (f <= target && target < f2) {
-          pick = order[k];
-          break;
-        }
-        f = f2;
-      }
-    }
-    put(a.next + row, pick);
-    put(a.row_rest + 2 * row, ok ? rest : __longlong_as_double(0x7FF8000000000000ll));
-    put(a.row_rest + 2 * row + 1, drafted);
-    put(a.row_max + row, rm);
+  for (int i = 0; i < kSlices; ++i) {
+    y[i] = sums[kSlices * lane + i];
+    rest += y[i];
   }
+  rest = wave_add(rest);
+  for (int k = 0; k < nk; ++k) drafted += share[k];
+  const bool ok = fabsf(rm) < INFINITY && rest == rest;
+  int own = -1;
+  if (ok) {
+    const double target = static_cast<double>(a.uniform[row]) * (rest + drafted);
+    double f = 0.0;
+    for (int k = 0; k < nk && own < 0; ++k) {
+      const double f2 = f + share[k];
+      if (f <= target && target < f2) own = order[k];
+      f = f2;
+    }
+  }
+  if (t == 0) {
+    put(a.next + row, own);
+    if (!ok) put(a.row_token + row, -1);  // no distribution
+  }
+  if (ok && own < 0) pick_residual(a, row, rm, y, rest, drafted, kid, nk, part[1], a.row_token + row);
   if (!last_to_arrive(a.cnt, a.N + 1, &flag)) return;
 
-  // The path, and the token after it.
-  for (int r = t; r <= a.N; r += kResThreads) next[r] = get(a.next + r);
+  // The path.
+  for (int r = t; r <= a.N; r += kResThreads) {
+    next[r] = get(a.next + r);
+    end_token[r] = get(a.row_token + r);  // (of a row that goes on, whatever was there)
+  }
   __syncthreads();
   if (t == 0) {
     int r = 0, len = 0;
     for (int j; (j = next[r]) >= 0; r = j + 1) a.path[len++] = j;  // j >= r: it ends
     *a.accepted = len;
-    flag = r;
-    order[0] = len;
-    n = 0;
+    *a.next_token = end_token[r];
+    n = len;
   }
   __syncthreads();
-  const int end = flag;
-  for (int i = order[0] + t; i < a.N; i += kResThreads) a.path[i] = -1;
-  rest = get(a.row_rest + 2 * end);
-  const double drafted = get(a.row_rest + 2 * end + 1);
-  rm = get(a.row_max + end);
-  double y[kSlices];
-#pragma unroll
-  for (int i = 0; i < kSlices; ++i) {
-    const int at = kSlices * lane + i;
-    y[i] = at < slices ? get(a.slice_sum + end * slices + at) : 0.0;
-  }
-  if (continues(a, t, parent, token, end)) kid[atomicAdd(&n, 1)] = token;
-  __syncthreads();
-  if (rest != rest) {  // no distribution
-    if (t == 0) *a.next_token = -1;
-    return;
-  }
-  pick_residual(a, end, rm, y, rest, drafted, kid, n, part[0]);
+  for (int i = n + t; i < a.N; i += kResThreads) a.path[i] = -1;
 }
 
 }  // namespace
@@ -688,15 +669,15 @@ bool verify_small(int N, int V) {
   return N < kResThreads && static_cast<long long>(N + 1) * ((V + kVerifySlice - 1) / kVerifySlice) <= kVerifySmall;
 }
 
-// After the completion counters, small calls: the slices' sums, the rows' (sum, drafted share), the
-// slices' and rows' maxima, the rows' picks.  Others: the last row
+// After the completion counters, small calls: the slices' sums and maxima, the rows' picks and the
+// tokens of those that end the path.  Others: the last row
 // and its (maximum, sum), its slices' sums, the rows' (maximum, sum) pairs, the slices' of
 // rows, the rows' picks.
 size_t verify_workspace_bytes(int N, int V) {
   int chunks = 0, len = 0;
   verify_plan(N, V, &chunks, &len);
   const size_t slices = (V + kVerifySlice - 1) / kVerifySlice, rows = N + 1;
-  const size_t small = verify_small(N, V) ? rows * (slices * (sizeof(double) + sizeof(float)) + 2 * sizeof(double) + 2 * sizeof(float)) : 0;
+  const size_t small = verify_small(N, V) ? rows * (slices * (sizeof(double) + sizeof(float)) + 2 * sizeof(int)) : 0;
   const size_t large = 16 + slices * sizeof(double) + rows * (1 + chunks) * sizeof(float2) + rows * sizeof(int);
   return kSplitCounterBytes + std::max(small, large);
 }
@@ -708,10 +689,9 @@ void verify_workspace(VerifyArgs* a, void* ws) {
   const int slices = (a->V + kVerifySlice - 1) / kVerifySlice;
   if (!a->greedy && verify_small(a->N, a->V)) {
     a->slice_sum = reinterpret_cast<double*>(p);
-    a->row_rest = a->slice_sum + static_cast<size_t>(a->N + 1) * slices;
-    a->slice_max = reinterpret_cast<float*>(a->row_rest + 2 * (a->N + 1));
-    a->row_max = a->slice_max + static_cast<size_t>(a->N + 1) * slices;
-    a->next = reinterpret_cast<int*>(a->row_max + (a->N + 1));
+    a->slice_max = reinterpret_cast<float*>(a->slice_sum + static_cast<size_t>(a->N + 1) * slices);
+    a->next = reinterpret_cast<int*>(a->slice_max + static_cast<size_t>(a->N + 1) * slices);
+    a->row_token = a->next + (a->N + 1);
     return;
   }
   a->last_row = reinterpret_cast<int*>(p);

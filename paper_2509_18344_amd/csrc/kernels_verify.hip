@@ -22,9 +22,9 @@
 //   k_verify_residual  the last row's other tokens in 64 bits: with V = 152064 tokens the
 //                      borders lie 10^-5 apart, and a sum in 32 bits, 10^-7 off, would pick a
 //                      neighbour in one call of a hundred; the last workgroup finds the token
-// Measured, 288 tokens at V = 152064: 88 MB, k_verify_rows 23.7 us (3.7 TB/s, where a sum over as much
-// memory reads 4.0: bound by memory; greedy 21.7), k_verify_residual 8.4, a chain of dependent
-// loads and two reductions; 31 us a call, greedy 21.5.
+// Measured, 288 tokens at V = 152064, 88 MB: k_verify_rows 21.2 us (greedy 20.6), of which reading
+// alone takes 15 (5.9 TB/s) and the chain from a row's sum over its pick to the path 4.5;
+// k_verify_residual 7.8, a chain of dependent loads and two reductions; 29 us a call, greedy 20.5.
 #include <algorithm>
 #include <climits>
 #include <cmath>
@@ -38,11 +38,13 @@ namespace {
 
 constexpr int kRowThreads = 256;
 constexpr int kRowWaves = kRowThreads / kWave;
+constexpr int kRowOwn = kVerifyMaxTokens / kRowThreads;  // drafted tokens a thread looks at
 // Rows' completion counters lie a cache line apart: arrivals at one line take turns, 17 ns each.
 constexpr int kCounterStep = 15;
 static_assert(kCounterStep * (kVerifyMaxTokens + 2) <= kSplitCounters, "the workspace's counters");
 
-constexpr int kRowLoads = 2;  // 16-byte loads in flight per thread
+constexpr int kRowLoads = 2;               // 16-byte loads in flight per thread (four: 22.8 us against 21.2)
+constexpr int kRowTile = 8 * kRowThreads;  // logits that the workgroup's threads load at a time
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
@@ -56,17 +58,10 @@ __device__ __forceinline__ void split8(uint4 w, float (&x)[8]) {
   }
 }
 
-// A row's (m, s): s = sum of 2^(c (l - m)); -inf (nothing seen yet, or masked logits) adds
-// nothing.  NaN and +inf in a row leave m or s not finite.
-__device__ __forceinline__ void merge(float c, float& m, float& s, float m2, float s2) {
-  const float mx = fmaxf(m, m2);
-  if (mx == -INFINITY) {
-    s += s2;  // zeros, or a NaN to be shown
-    return;
-  }
-  s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - mx))) +
-      (m2 == -INFINITY ? s2 : s2 * __builtin_amdgcn_exp2f(c * (m2 - mx)));
-  m = mx;
+__device__ __forceinline__ float wave_top(float v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
 }
 
 // Greedy: the larger logit and of equals the lower token; a NaN (the row has none) stays.
@@ -76,7 +71,8 @@ __device__ __forceinline__ void best_of(float& m, int& i, float m2, int i2) {
   i = take ? i2 : i;
 }
 
-// What is kept of logits seen: (maximum, sum of 2^(c (l - maximum))), or greedy (maximum, token).
+// What is kept of logits seen: (maximum, sum of 2^(c (l - maximum))), or greedy (maximum, the first
+// token of the eight that it was found in).
 template <bool GREEDY>
 struct Seen {
   float m = -INFINITY;
@@ -84,44 +80,62 @@ struct Seen {
 
   __device__ __forceinline__ void add(float c, const float (&x)[8], int v0) {
     if constexpr (GREEDY) {
-      int i = __float_as_int(s);
+      float mx = x[0];  // a NaN stays
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        // a thread's tokens come in order: a later equal one does not replace
-        const bool take = x[e] > m || x[e] != x[e];
-        m = take && m == m ? x[e] : m;
-        i = take ? v0 + e : i;
-      }
-      s = __int_as_float(i);
+      for (int e = 1; e < 8; ++e) mx = __builtin_elementwise_maximum(mx, x[e]);
+      // a thread's tokens come in order: later equal ones do not replace
+      const bool take = m == m && !(mx <= m);
+      m = take ? mx : m;
+      s = take ? __int_as_float(v0) : s;
     } else {
       float mx = m;
 #pragma unroll
       for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
-      if (mx == -INFINITY) {  // nothing but -inf (or NaN, which the sum has to show)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += x[e] == x[e] ? 0.f : x[e];
-        return;
+      if (__builtin_amdgcn_ballot_w64(mx > m)) {
+        s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - mx));
+        m = mx;
       }
-      s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - mx));
-      m = mx;
+      const float base = m == -INFINITY ? 0.f : m;  // (2^-inf of -inf, and a NaN that the sum has to show)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(c * (x[e] - mx));
+      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(c * (x[e] - base));
     }
   }
 
-  __device__ __forceinline__ void add(float c, float m2, float s2) {
+  // What the wavefront's lanes have seen, in every lane.
+  __device__ __forceinline__ void across_wave(float c) {
     if constexpr (GREEDY) {
       int i = __float_as_int(s);
-      best_of(m, i, m2, __float_as_int(s2));
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) best_of(m, i, __shfl_xor(m, d), __shfl_xor(i, d));
       s = __int_as_float(i);
     } else {
-      merge(c, m, s, m2, s2);
+      const float top = wave_top(m);
+      s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - top));  // (a sum of nothing, or a NaN, stays)
+      m = top;
+#pragma unroll
+      for (int d = 1; d < kWave; d *= 2) s += __shfl_xor(s, d);
     }
   }
 
-  __device__ __forceinline__ void across_wave(float c) {
-#pragma unroll
-    for (int d = 1; d < kWave; d *= 2) add(c, __shfl_xor(m, d), __shfl_xor(s, d));
+  // What `n` wavefronts or slices have seen, the pairs from `at`.
+  template <typename At>
+  __device__ __forceinline__ static Seen all(float c, int n, At at) {
+    Seen own;
+    for (int i = threadIdx.x % kWave; i < n; i += kWave) own.join(c, at(i));
+    own.across_wave(c);
+    return own;
+  }
+  __device__ __forceinline__ void join(float c, float2 o) {
+    if constexpr (GREEDY) {
+      int i = __float_as_int(s);
+      best_of(m, i, o.x, __float_as_int(o.y));
+      s = __int_as_float(i);
+    } else {
+      const float top = fmaxf(m, o.x);
+      s = (m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - top))) +
+          (o.x == -INFINITY ? o.y : o.y * __builtin_amdgcn_exp2f(c * (o.x - top)));
+      m = top;
+    }
   }
 };
 
@@ -181,75 +195,93 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
     Ordered order;
     int next[kVerifyMaxTokens + 1];
   } u;
-  __shared__ float wm[kRowWaves], ws[kRowWaves];
+  __shared__ float2 waves[kRowWaves];
   __shared__ int n, flag, pick;
   const int t = threadIdx.x;
   const int row = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
   const int lo = chunk * a.chunk_len, hi = min(a.V, lo + a.chunk_len);
   const uint16_t* l = a.logits + static_cast<size_t>(row) * a.V;
+  // A thread's drafted tokens, then the slice's whole tiles, kRowLoads of them in flight; the row's
+  // children's logits come among them.
+  int token[kRowOwn], parent[kRowOwn];
+#pragma unroll
+  for (int k = 0; k < kRowOwn; ++k) {
+    const int j = t + k * kRowThreads;
+    token[k] = j < a.N ? a.token[j] : -1;
+    parent[k] = j < a.N ? a.parent[j] : -1;
+  }
+  const int tiles = (hi - lo) / kRowTile;
+  auto tile = [&](int i) __attribute__((always_inline)) {
+    return *reinterpret_cast<const uint4*>(l + lo + i * kRowTile + 8 * t);
+  };
+  Seen<GREEDY> seen;
+  auto take = [&](uint4 w, int i) __attribute__((always_inline)) {
+    float x[8];
+    split8(w, x);
+    seen.add(a.c, x, lo + i * kRowTile + 8 * t);
+  };
+  uint4 w[kRowLoads] = {};
+#pragma unroll
+  for (int j = 0; j < kRowLoads; ++j)
+    if (j < tiles) w[j] = tile(j);
   if (t == 0) {
     n = 0;
     pick = INT_MAX;
   }
-  __syncthreads();
-  // the row's children, in any order; their logits arrive while the row streams
-  for (int j = t; j < a.N; j += kRowThreads) {
-    const int k = a.token[j];
-    if (continues(a, j, a.parent[j], k, row)) {
-      const int at = atomicAdd(&n, 1);
-      kids.j[at] = j;
-      kids.token[at] = k;
-      kids.p[at] = __uint_as_float(static_cast<uint32_t>(l[k]) << 16);
-    }
+  bool child[kRowOwn];
+  uint16_t own[kRowOwn];
+#pragma unroll
+  for (int k = 0; k < kRowOwn; ++k) {
+    child[k] = continues(a, t + k * kRowThreads, parent[k], token[k], row);
+    own[k] = child[k] ? l[token[k]] : 0;
   }
-
-  Seen<GREEDY> seen;
-  for (int v0 = lo + 8 * t; v0 < hi; v0 += 8 * kRowThreads * kRowLoads) {
-    uint4 w[kRowLoads];
+  int i = 0;
+  for (; i + 2 * kRowLoads <= tiles; i += kRowLoads)
 #pragma unroll
     for (int j = 0; j < kRowLoads; ++j) {
-      const int v = v0 + 8 * kRowThreads * j;
-      w[j] = v < hi ? *reinterpret_cast<const uint4*>(l + v) : make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+      const uint4 now = w[j];
+      w[j] = tile(i + kRowLoads + j);
+      take(now, i + j);
     }
+  for (; i < tiles; i += kRowLoads)
 #pragma unroll
-    for (int j = 0; j < kRowLoads; ++j) {
-      float x[8];
-      split8(w[j], x);
-      seen.add(a.c, x, v0 + 8 * kRowThreads * j);
-    }
-  }
+    for (int j = 0; j < kRowLoads; ++j)
+      if (i + j < tiles) {
+        const uint4 now = w[j];
+        if (i + kRowLoads + j < tiles) w[j] = tile(i + kRowLoads + j);
+        take(now, i + j);
+      }
+  if (lo + tiles * kRowTile + 8 * t < hi) take(tile(tiles), tiles);  // its last, partial tile
   seen.across_wave(a.c);
-  if (t % kWave == 0) {
-    wm[t / kWave] = seen.m;
-    ws[t / kWave] = seen.s;
-  }
+  if (t % kWave == 0) waves[t / kWave] = make_float2(seen.m, seen.s);
   __syncthreads();
-  seen.m = wm[0];
-  seen.s = ws[0];
 #pragma unroll
-  for (int w = 1; w < kRowWaves; ++w) seen.add(a.c, wm[w], ws[w]);
+  for (int k = 0; k < kRowOwn; ++k)
+    if (child[k]) {  // the row's children, in any order
+      const int at = atomicAdd(&n, 1);
+      kids.j[at] = t + k * kRowThreads;
+      kids.token[at] = token[k];
+      kids.p[at] = __uint_as_float(static_cast<uint32_t>(own[k]) << 16);
+    }
+  seen = Seen<GREEDY>::all(a.c, kRowWaves, [&](int k) { return waves[k]; });
+  __syncthreads();
   if (a.chunks > 1) {
     if (t == 0) put(a.stat + blockIdx.x, seen.m, seen.s);
     if (!last_to_arrive(a.cnt + kCounterStep * (1 + row), a.chunks, &flag)) return;
     // every wavefront merges the row's slices, in the same order
-    seen = Seen<GREEDY>();
-    for (int c0 = 0; c0 < a.chunks; c0 += kWave) {
-      const int c = c0 + t % kWave;
-      Seen<GREEDY> part;
-      if (c < a.chunks) {
-        const float2 st = get(a.stat + static_cast<size_t>(row) * a.chunks + c);
-        part.m = st.x;
-        part.s = st.y;
-      }
-      part.across_wave(a.c);
-      seen.add(a.c, part.m, part.s);
-    }
+    seen = Seen<GREEDY>::all(a.c, a.chunks, [&](int k) { return get(a.stat + static_cast<size_t>(row) * a.chunks + k); });
   }
 
   // The row's pick among its children.
   const int nk = n;
-  const int best = GREEDY ? __float_as_int(seen.s) : 0;
   const bool ok = fabsf(seen.m) < INFINITY && (GREEDY || (seen.s > 0.f && seen.s < INFINITY));
+  int best = -1;  // greedy: the first of its eight
+  if (GREEDY && ok) {
+    float x[8];
+    split8(*reinterpret_cast<const uint4*>(l + __float_as_int(seen.s)), x);
+#pragma unroll
+    for (int e = 7; e >= 0; --e) best = x[e] == seen.m ? __float_as_int(seen.s) + e : best;
+  }
   if (ok) {
     for (int k = t; k < nk; k += kRowThreads) {
       const int j = kids.j[k], token = kids.token[k];
@@ -284,7 +316,7 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
   if (t == 0) {
     put(a.next + row, pick == INT_MAX ? -1 : pick);
     // a row without a distribution: no sum, or no token
-    put(a.row_stat + row, seen.m, GREEDY ? __int_as_float(ok ? best : -1) : ok ? seen.s : 0.f);
+    put(a.row_stat + row, seen.m, GREEDY ? __int_as_float(best) : ok ? seen.s : 0.f);
   }
   if (!last_to_arrive(a.cnt, a.N + 1, &flag)) return;
 
@@ -313,12 +345,6 @@ constexpr int kResWaves = kResThreads / kWave;
 static_assert(kVerifySlice == 8 * kResThreads, "eight logits a thread");
 constexpr int kSlices = kVerifyMaxV / kVerifySlice / kWave;  // sums of slices a lane
 constexpr int kRowSlices = (kVerifyMaxV / kVerifySlice + kResThreads - 1) / kResThreads;  // and a thread
-
-__device__ __forceinline__ float wave_top(float v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
 
 __device__ __forceinline__ double wave_add(double v) {
 #pragma unroll
@@ -655,10 +681,10 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
 }  // namespace
 
 void verify_plan(int N, int V, int* chunks, int* chunk_len) {
-  // about 640 workgroups (289 rows in three to seven slices 30.8 us alike, in one 38), each with at
-  // least one round of loads
+  // about 640 workgroups (289 rows in three slices 21.2 us, in four 23.7, in seven 24.4), each with at
+  // least two tiles
   int c = (640 + N) / (N + 1);
-  const int most = (V + 8 * kRowThreads * kRowLoads - 1) / (8 * kRowThreads * kRowLoads);
+  const int most = (V + 2 * kRowTile - 1) / (2 * kRowTile);
   if (c > most) c = most;
   if (c < 1) c = 1;
   *chunk_len = ((V + c - 1) / c + 7) / 8 * 8;

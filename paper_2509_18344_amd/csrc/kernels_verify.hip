@@ -14,8 +14,8 @@
 // Up to kVerifySmall slices of 2048 logits in all one kernel does everything in 64 bits
 // (k_verify_small: a slice its maximum and its sum without the row's children, the last workgroup of a
 // row the row's pick and, where that ends the path, its token, the last of all the path: a chain of 4 at
-// V = 32000 9.9 us a call against 15.2 with two kernels, 26 tokens at V = 152064, 2025 slices, 15.3
-// against 18.2; 130 at 32000, 2096, 16.9 against 16.8).  Beyond, two, since 64-bit exponentials of all
+// V = 32000 9.8 us a call against 15.3 with two kernels, 26 tokens at V = 152064, 2025 slices, 15.3
+// against 17.7; 130 at 32000, 2096, 17.0 against 16.5).  Beyond, two, since 64-bit exponentials of all
 // logits would bound them:
 //   k_verify_rows      per (row, slice) workgroup the maximum and the sum, in 32 bits; the last
 //                      of a row finds the child that the row picks, the last of all the path

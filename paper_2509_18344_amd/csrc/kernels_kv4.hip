@@ -5,10 +5,10 @@
 // a row: a row's range is three or four DPP steps, a key's 8 codes are one word, and the
 // values' codes turn in LDS into words of 8 positions each.
 //
-// Measured, 16384 positions of 8 heads in groups of 128: append 22.8 us for 67 MB read and 18 written,
-// 3.7 TB/s (about 110 vector instructions a row of 8 dimensions come next to the memory's
-// 15.6 us at a large copy's rate), read 15.7 us for the same bytes, 5.4 TB/s: bound by memory.  A few
-// rows 4.0 and 3.3 us, the launch and one chain of loads.
+// Measured, 16384 positions of 8 heads in groups of 128: append 22.7 us for 67 MB read and 18 written,
+// 3.7 TB/s, issuing vector instructions 70 % of the time (455 a wavefront, 95 of them for a lane's 8
+// values); read 15.5 us for the same bytes, 5.5 TB/s, as a large copy: bound by memory.  A few rows
+// 3.9 and 3.4 us, the launch and one chain of loads.
 #include "kv4_device.h"
 
 namespace subspec {

@@ -35,8 +35,8 @@
 // output itself.
 //
 // Measured (a call, both kernels): 131138 positions of 8 heads in groups of 64, 30 query rows a head:
-// 151 MB of cache in 40 us, 3.8 TB/s, where a sum over as much memory reads 4.0; the first kernel's
-// vector ALUs are busy two thirds of its time, so unpacking and the softmax come next.  8407
+// 151 MB of cache in 40 us, 3.8 TB/s.  The first kernel takes 37 us, 28 with nothing but its loads:
+// unpacking, softmax and products bound it (vector ALUs busy two thirds of the time).  8407
 // positions of 8 heads in groups of 128, 64 rows a head: 9 MB in 16.6 us, a chain of the launch with
 // the first loads (3.4 us), four or five tiles a wavefront (1.2 to 2 each), the merge (1 to 2.5) and the
 // second kernel (2.5 to 3.3).  2336 positions of 4 heads, 42 rows: 10.3 us, the same chain with one

@@ -117,7 +117,7 @@ struct Kv4TileLds {
   alignas(16) uint8_t key[kv4_tile_bytes(2)];    // the tiles as they are in memory
   alignas(16) uint8_t value[kv4_tile_bytes(2)];
   alignas(16) uint8_t code[kKv4Tile][kKv4D + 16];  // the values' codes, one a byte
-  uint32_t live;                                 // positions that are written
+  alignas(16) uint32_t live[8];                    // positions that are written: 4 i + bit
 };
 
 // One tile of one head: 256 threads write the positions that are live.  `source(w)` is where
@@ -129,7 +129,6 @@ template <int G, typename Source>
 __device__ __forceinline__ void kv4_store_tile(uint8_t* kt, uint8_t* vt, const uint16_t* k, const uint16_t* v, Kv4TileLds& L,
                                                Source source) {
   const int t = threadIdx.x, col = t % 16, r = t / 16;
-  if (t == 0) L.live = 0;
   uint4 x[2][2];
   bool live[2];
   const long long at[2] = {source(r), source(16 + r)};
@@ -141,10 +140,12 @@ __device__ __forceinline__ void kv4_store_tile(uint8_t* kt, uint8_t* vt, const u
       x[b][1] = *reinterpret_cast<const uint4*>(v + at[b] + 8 * col);
     }
   }
-  __syncthreads();
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int w = 16 * b + r;
+    // a wavefront's four rows
+    const unsigned long long rows = __builtin_amdgcn_ballot_w64(live[b]) & 0x0001000100010001ull;
+    if (t % kWave == 0) L.live[4 * b + t / kWave] = static_cast<uint32_t>((rows * 0x0001000200040008ull) >> 48) & 0xFu;
     if (!live[b]) continue;
     Kv4Meta meta;
     const bool head = col % (16 / G) == 0;
@@ -163,10 +164,11 @@ __device__ __forceinline__ void kv4_store_tile(uint8_t* kt, uint8_t* vt, const u
       *reinterpret_cast<_Float16*>(L.value + at) = meta.s;
       *reinterpret_cast<_Float16*>(L.value + at + 16) = meta.m;
     }
-    if (col == 0) atomicOr(&L.live, 1u << w);
   }
   __syncthreads();
-  const uint32_t all = L.live;
+  uint32_t all = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) all |= L.live[i] << (4 * i);
   if (t < 128) {
     // four adjacent columns of one of a lane's words: dimensions 64 half + 16 dl + vc .. + 3
     const int vc = 4 * (t % 4), quarter = t / 4 % 4, dl = t / 16 % 4, half = t / 64;

@@ -148,27 +148,28 @@ def _stream(s):
     return s.cuda_stream
 
 
-_tensor_base = None
+_get_device = _is_contiguous = _data_ptr = None
 
 
-def _device_ptrs(fn: str, stream, *args):
-    """Data pointers of one call's tensors.  Each has to be contiguous and on the device the call
-    runs on: the C entry points see neither (an address is taken as it is, None stays None).
-    torch's methods mapped over the tensors: a method call each is most of the binding's
-    time at a few microseconds a kernel (nine tensors 2.4 us against 4.6 in a loop)."""
-    global _tensor_base
-    if _tensor_base is None:
-        import torch
-        _tensor_base = torch._C.TensorBase if hasattr(torch._C, "TensorBase") else torch.Tensor
-    base = _tensor_base
-    given = [t for t in args if t is not None]
-    try:
-        if {*map(base.get_device, given)} == {_current_device(stream)} and all(map(base.is_contiguous, given)):
-            if len(given) == len(args):
-                return map(base.data_ptr, given)
-            return [None if t is None else t.data_ptr() for t in args]
-    except TypeError:  # addresses among them
-        pass
+def _device_args(fn: str, stream, *args):
+    """One call's stream handle and its tensors' data pointers.  Each tensor has to be contiguous and
+    on the device the call runs on: the C entry points see neither (an address is taken as it is,
+    None stays None).  torch's methods mapped over the tensors, the stream with them: a method call
+    each is most of the binding's time at a few microseconds a kernel (nine tensors 1.6 us against
+    4.6 in a loop)."""
+    global _get_device, _is_contiguous, _data_ptr
+    if stream is None and _get_device is not None:
+        given = [t for t in args if t is not None]
+        try:
+            on = {*map(_get_device, given)}
+            dev = on.pop()
+            if not on and dev >= 0 and dev == _device() and all(map(_is_contiguous, given)):
+                ptr = map(_data_ptr, given)
+                if len(given) == len(args):
+                    return [_raw_stream(dev), *ptr]
+                return [_raw_stream(dev), *[None if t is None else next(ptr) for t in args]]
+        except TypeError:  # addresses among them
+            pass
     dev, out = _current_device(stream), []
     for t in args:
         if t is None or isinstance(t, int):
@@ -182,7 +183,11 @@ def _device_ptrs(fn: str, stream, *args):
             raise SubspecError(fn, -1, f"a {'' if whole else 'not contiguous '}tensor on device {on}: needs a contiguous "
                                "one on the current device, and a stream of that device")
         out.append(t.data_ptr())
-    return out
+    handle = _stream(stream)
+    if _get_device is None and _raw_stream is not None and _device is not None:
+        base = getattr(_torch._C, "TensorBase", _torch.Tensor)
+        _get_device, _is_contiguous, _data_ptr = base.get_device, base.is_contiguous, base.data_ptr
+    return [handle, *out]
 
 
 def _current_device(stream) -> int:
@@ -349,10 +354,10 @@ def subspec_tree_attention_plan(M, Hq, Hkv, P, T):
 
 def subspec_qkv_rope(qkv, ld, bias, q_weight, k_weight, eps, positions, inv_freq, rot, interleaved, M, Hq, Hkv,
                      q, k_new, v_new, stream=None) -> int:
-    x, b, qw, kw, pos, freq, qo, ko, vo = _device_ptrs("subspec_qkv_rope", stream, qkv, bias, q_weight, k_weight, positions,
-                                                       inv_freq, q, k_new, v_new)
+    st, x, b, qw, kw, pos, freq, qo, ko, vo = _device_args("subspec_qkv_rope", stream, qkv, bias, q_weight, k_weight,
+                                                           positions, inv_freq, q, k_new, v_new)
     return _check("subspec_qkv_rope", load_library().subspec_qkv_rope(
-        x, ld, b, qw, kw, eps, pos, freq, rot, int(interleaved), M, Hq, Hkv, qo, ko, vo, _stream(stream)))
+        x, ld, b, qw, kw, eps, pos, freq, rot, int(interleaved), M, Hq, Hkv, qo, ko, vo, st))
 
 
 def subspec_kv4_bytes(Hkv: int, S: int, group: int) -> int:
@@ -360,21 +365,21 @@ def subspec_kv4_bytes(Hkv: int, S: int, group: int) -> int:
 
 
 def subspec_kv4_append(k, v, src_rows, rows, count, n, Hkv, S, pos, group, k_cache, v_cache, stream=None) -> int:
-    pk, pv, pr, pc, ck, cv = _device_ptrs("subspec_kv4_append", stream, k, v, rows, count, k_cache, v_cache)
+    st, pk, pv, pr, pc, ck, cv = _device_args("subspec_kv4_append", stream, k, v, rows, count, k_cache, v_cache)
     return _check("subspec_kv4_append", load_library().subspec_kv4_append(
-        pk, pv, src_rows, pr, pc, n, Hkv, S, pos, group, ck, cv, _stream(stream)))
+        pk, pv, src_rows, pr, pc, n, Hkv, S, pos, group, ck, cv, st))
 
 
 def subspec_kv4_read(k_cache, v_cache, Hkv, S, pos, n, group, k, v, stream=None) -> int:
-    ck, cv, pk, pv = _device_ptrs("subspec_kv4_read", stream, k_cache, v_cache, k, v)
+    st, ck, cv, pk, pv = _device_args("subspec_kv4_read", stream, k_cache, v_cache, k, v)
     return _check("subspec_kv4_read", load_library().subspec_kv4_read(
-        ck, cv, Hkv, S, pos, n, group, pk, pv, _stream(stream)))
+        ck, cv, Hkv, S, pos, n, group, pk, pv, st))
 
 
 def subspec_tree_attention_kv4(q, k_cache, v_cache, mask, M, Hq, Hkv, S, P, T, group, scale, out, stream=None) -> int:
-    pq, ck, cv, pm, po = _device_ptrs("subspec_tree_attention_kv4", stream, q, k_cache, v_cache, mask, out)
+    st, pq, ck, cv, pm, po = _device_args("subspec_tree_attention_kv4", stream, q, k_cache, v_cache, mask, out)
     return _check("subspec_tree_attention_kv4", load_library().subspec_tree_attention_kv4(
-        pq, ck, cv, pm, M, Hq, Hkv, S, P, T, group, scale, po, _stream(stream)))
+        pq, ck, cv, pm, M, Hq, Hkv, S, P, T, group, scale, po, st))
 
 
 def subspec_tree_attention_kv4_workspace_bytes(M, Hq, Hkv, P, T) -> int:
@@ -390,10 +395,10 @@ def subspec_tree_attention_kv4_plan(M, Hq, Hkv, P, T):
 
 
 def subspec_tree_verify(logits, parent, token, uniform, N, V, temperature, path, accepted, next_token, stream=None) -> int:
-    pl, pp, pt, pu, po, pa, pn = _device_ptrs("subspec_tree_verify", stream, logits, parent, token, uniform, path, accepted,
-                                              next_token)
+    st, pl, pp, pt, pu, po, pa, pn = _device_args("subspec_tree_verify", stream, logits, parent, token, uniform, path,
+                                                  accepted, next_token)
     return _check("subspec_tree_verify", load_library().subspec_tree_verify(
-        pl, pp, pt, pu, N, V, temperature, po, pa, pn, _stream(stream)))
+        pl, pp, pt, pu, N, V, temperature, po, pa, pn, st))
 
 
 def subspec_tree_verify_workspace_bytes(N, V) -> int:

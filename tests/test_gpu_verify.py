@@ -32,7 +32,14 @@ def _tree(rng, N, V, width, agree, logits):
     return parent, token
 
 
+PAD = 0  # entries behind a case's own, which nothing can accept: long drafts take other kernels
+
+
 def _run(logits, parent, token, u, T, stream=None):
+    if PAD:
+        logits = np.concatenate([logits, np.zeros((PAD, logits.shape[1]), logits.dtype)])
+        parent, token = np.append(parent, np.full(PAD, -2)), np.append(token, np.zeros(PAD, int))
+        u = None if u is None else np.append(u, np.full(PAD, 0.5))
     N, V = logits.shape[0] - 1, logits.shape[1]
     i32 = lambda a: torch.from_numpy(np.asarray(a, np.int32)).to(DEV)  # noqa: E731
     path = torch.full((N + 1,), -9, dtype=torch.int32, device=DEV)
@@ -187,6 +194,20 @@ def test_tree_verify_all_mass_on_drafted_tokens():
     got = _run(_bf16(logits), [-1, -1], [60, 4], [one, 0.5, 0.5], 1.0)
     assert got in (([1], 2), ([], 60)), got  # the last of them, or, where rounding keeps u from both, the larger token
     assert _run(_bf16(logits), [-1, -1], [60, 4], [0.1, 0.5, 0.5], 1.0) == ([0], 2)
+
+
+@pytest.mark.parametrize("case,args", [
+    (test_tree_verify_uniform_numbers_across_a_row, ()),
+    (test_tree_verify_uniform_number_next_to_one_and_zero, (40,)),
+    (test_tree_verify_uniform_number_next_to_one_and_zero, (152064,)),
+    (test_tree_verify_entries_that_cannot_be_accepted, ()),
+    (test_tree_verify_rows_without_a_distribution, (0.0,)),
+    (test_tree_verify_rows_without_a_distribution, (0.7,)),
+    (test_tree_verify_all_mass_on_drafted_tokens, ()),
+])
+def test_tree_verify_same_cases_in_long_drafts(case, args, monkeypatch):
+    monkeypatch.setitem(globals(), "PAD", 300)
+    case(*args)
 
 
 def test_tree_verify_repeats_and_leaves_the_counters_clear():

@@ -67,16 +67,22 @@ def _check(M, Hq, Hkv, P, T, group, seed, q_scale=1.0, mask=None, S=None, scale=
     S = S or (n + 31) // 32 * 32 + 32
     rng = np.random.default_rng([M, Hq, Hkv, P, T, seed])
     q = _bf16(rng.standard_normal((M, Hq, D)) * q_scale)
-    k = rng.standard_normal((n, Hkv, D))
+    own = min(Hkv, 8)  # many heads share the rows of eight
+    k = rng.standard_normal((n, own, D))
     k[:, :, ::16] *= 3.0
-    v = rng.standard_normal((n, Hkv, D)) + 0.5
+    v = rng.standard_normal((n, own, D)) + 0.5
     if v_scale is not None:
         v *= v_scale(rng, n)[:, None, None]
-    k, v = _bf16(k), _bf16(v)
+    k, v = (_bf16(a)[:, np.arange(Hkv) % own] for a in (k, v))
     if mask is None:
         mask = synth.tree_levels_mask(T, 6, M, seed)
     dk, dv = _fill(k, v, S, group, junk)
     got = _run(q, dk, dv, mask, M, Hq, Hkv, S, P, T, group, scale)
+    if Hkv > own:  # and three of them are compared
+        some = np.array([0, Hkv // 2, Hkv - 1])
+        G, Hkv = Hq // Hkv, 3
+        heads = (some[:, None] * G + np.arange(G)).ravel()
+        q, got, k, v, Hq = q[:, heads], got[:, heads], k[:, some], v[:, some], 3 * G
     kh, vh = _held(k, group), _held(v, group)
     K, V = oracle.kv4_value(*kh), oracle.kv4_value(*vh)
     ref, wabs = oracle.tree_attention_values(q, K, V, P, T, mask, scale)
@@ -113,6 +119,12 @@ SHAPES = [
     (5, 10, 2, 5000, 95, 1.0),
     (1, 16, 16, 9000, 0, 2.0),    # several rounds of tiles per wavefront
     (10, 12, 2, 6001, 200, 1.0),  # 60 rows, long
+    # many heads, so that a wavefront has five tiles and more: 1, 17, 64, 20 and 40 rows a head
+    (1, 128, 128, 2500, 0, 1.0),
+    (17, 34, 34, 5000, 20, 1.0),
+    (16, 64, 16, 4900, 90, 2.0),
+    (20, 64, 64, 5101, 13, 1.0),
+    (40, 40, 40, 4000, 20, 1.0),
 ]
 
 

@@ -6,6 +6,8 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
+from itertools import compress
+from operator import ge
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libsubspec.so"
@@ -148,22 +150,33 @@ def _stream(s):
     return s.cuda_stream
 
 
-_get_device = _is_contiguous = _data_ptr = None
+_get_device = _is_contiguous = _data_ptr = _dtype = _numel = None
+
+# What a tensor may hold, by what the kernel takes its elements for: numbers of that type, or integers
+# of its size with their bits.
+_TYPES = {"bf16": ("bfloat16", "int16", "uint16"), "i32": ("int32", "uint32"), "f32": ("float32",),
+          "f64": ("float64",), "u8": ("uint8", "int8")}
+_usual = {}  # a call's kinds -> the first torch type of each
 
 
-def _device_args(fn: str, stream, *args):
-    """One call's stream handle and its tensors' data pointers.  Each tensor has to be contiguous and
-    on the device the call runs on: the C entry points see neither (an address is taken as it is,
-    None stays None).  torch's methods mapped over the tensors, the stream with them: a method call
-    each is most of the binding's time at a few microseconds a kernel (nine tensors 1.6 us against
-    4.6 in a loop)."""
-    global _get_device, _is_contiguous, _data_ptr
+def _device_args(fn: str, stream, kinds, needs, *args):
+    """One call's stream handle and its tensors' data pointers.  Each tensor has to be contiguous, on
+    the device the call runs on, of its kind (a name of _TYPES) and of at least as many elements as
+    `needs` says: the C entry points see none of this, and a kernel that is handed anything else
+    reads or writes past it (an address is taken as it is, None stays None).  torch's methods mapped
+    over the tensors: a method call each is most of the binding's time at a few microseconds a kernel."""
+    global _get_device, _is_contiguous, _data_ptr, _dtype, _numel
     if stream is None and _get_device is not None:
         given = [t for t in args if t is not None]
+        types, least = _usual.get(kinds) or _usual_types(kinds), needs
+        if len(given) < len(args):
+            there = [t is not None for t in args]
+            types, least = [*compress(types, there)], compress(needs, there)
         try:
             on = {*map(_get_device, given)}
             dev = on.pop()
-            if not on and dev >= 0 and dev == _device() and all(map(_is_contiguous, given)):
+            if (not on and dev >= 0 and dev == _device() and all(map(_is_contiguous, given)) and
+                    [*map(_dtype, given)] == types and all(map(ge, map(_numel, given), least))):
                 ptr = map(_data_ptr, given)
                 if len(given) == len(args):
                     return [_raw_stream(dev), *ptr]
@@ -171,7 +184,7 @@ def _device_args(fn: str, stream, *args):
         except TypeError:  # addresses among them
             pass
     dev, out = _current_device(stream), []
-    for t in args:
+    for t, kind, need in zip(args, kinds, needs):
         if t is None or isinstance(t, int):
             out.append(t)
             continue
@@ -182,12 +195,22 @@ def _device_args(fn: str, stream, *args):
         if on != dev or not whole:
             raise SubspecError(fn, -1, f"a {'' if whole else 'not contiguous '}tensor on device {on}: needs a contiguous "
                                "one on the current device, and a stream of that device")
+        if str(t.dtype).rpartition(".")[2] not in _TYPES[kind]:
+            raise SubspecError(fn, -1, f"a tensor of {t.dtype}: needs one of {' or '.join(_TYPES[kind])}")
+        if t.numel() < need:
+            raise SubspecError(fn, -1, f"a tensor of {t.numel()} elements: needs {need}")
         out.append(t.data_ptr())
     handle = _stream(stream)
     if _get_device is None and _raw_stream is not None and _device is not None:
         base = getattr(_torch._C, "TensorBase", _torch.Tensor)
         _get_device, _is_contiguous, _data_ptr = base.get_device, base.is_contiguous, base.data_ptr
+        _dtype, _numel = base.dtype.__get__, base.numel
     return [handle, *out]
+
+
+def _usual_types(kinds):
+    _usual[kinds] = [getattr(_torch, _TYPES[k][0]) for k in kinds]
+    return _usual[kinds]
 
 
 def _current_device(stream) -> int:
@@ -354,8 +377,13 @@ def subspec_tree_attention_plan(M, Hq, Hkv, P, T):
 
 def subspec_qkv_rope(qkv, ld, bias, q_weight, k_weight, eps, positions, inv_freq, rot, interleaved, M, Hq, Hkv,
                      q, k_new, v_new, stream=None) -> int:
-    st, x, b, qw, kw, pos, freq, qo, ko, vo = _device_args("subspec_qkv_rope", stream, qkv, bias, q_weight, k_weight,
-                                                           positions, inv_freq, q, k_new, v_new)
+    heads = Hq + 2 * Hkv
+    if not rot:  # not read
+        positions = inv_freq = None
+    st, x, b, qw, kw, pos, freq, qo, ko, vo = _device_args(
+        "subspec_qkv_rope", stream, ("bf16", "bf16", "bf16", "bf16", "i32", "f64", "bf16", "bf16", "bf16"),
+        ((M - 1) * ld + heads * 128, heads * 128, 128, 128, M, rot // 2, M * Hq * 128, M * Hkv * 128, M * Hkv * 128),
+        qkv, bias, q_weight, k_weight, positions, inv_freq, q, k_new, v_new)
     return _check("subspec_qkv_rope", load_library().subspec_qkv_rope(
         x, ld, b, qw, kw, eps, pos, freq, rot, int(interleaved), M, Hq, Hkv, qo, ko, vo, st))
 
@@ -364,20 +392,33 @@ def subspec_kv4_bytes(Hkv: int, S: int, group: int) -> int:
     return int(load_library().subspec_kv4_bytes(Hkv, S, group))
 
 
+def _kv4_size(Hkv, S, group):
+    """subspec_kv4_bytes without the call; of an invalid shape, which the library refuses, anything."""
+    return Hkv * (S // 32) * (2304 if group == 64 else 2176)
+
+
 def subspec_kv4_append(k, v, src_rows, rows, count, n, Hkv, S, pos, group, k_cache, v_cache, stream=None) -> int:
-    st, pk, pv, pr, pc, ck, cv = _device_args("subspec_kv4_append", stream, k, v, rows, count, k_cache, v_cache)
+    src, cache = src_rows * Hkv * 128, _kv4_size(Hkv, S, group)
+    st, pk, pv, pr, pc, ck, cv = _device_args(
+        "subspec_kv4_append", stream, ("bf16", "bf16", "i32", "i32", "u8", "u8"), (src, src, n, 1, cache, cache),
+        k, v, rows, count, k_cache, v_cache)
     return _check("subspec_kv4_append", load_library().subspec_kv4_append(
         pk, pv, src_rows, pr, pc, n, Hkv, S, pos, group, ck, cv, st))
 
 
 def subspec_kv4_read(k_cache, v_cache, Hkv, S, pos, n, group, k, v, stream=None) -> int:
-    st, ck, cv, pk, pv = _device_args("subspec_kv4_read", stream, k_cache, v_cache, k, v)
+    out, cache = n * Hkv * 128, _kv4_size(Hkv, S, group)
+    st, ck, cv, pk, pv = _device_args("subspec_kv4_read", stream, ("u8", "u8", "bf16", "bf16"), (cache, cache, out, out),
+                                      k_cache, v_cache, k, v)
     return _check("subspec_kv4_read", load_library().subspec_kv4_read(
         ck, cv, Hkv, S, pos, n, group, pk, pv, st))
 
 
 def subspec_tree_attention_kv4(q, k_cache, v_cache, mask, M, Hq, Hkv, S, P, T, group, scale, out, stream=None) -> int:
-    st, pq, ck, cv, pm, po = _device_args("subspec_tree_attention_kv4", stream, q, k_cache, v_cache, mask, out)
+    rows, cache = M * Hq * 128, _kv4_size(Hkv, S, group)
+    st, pq, ck, cv, pm, po = _device_args(
+        "subspec_tree_attention_kv4", stream, ("bf16", "u8", "u8", "i32", "bf16"),
+        (rows, cache, cache, M * ((T + M + 31) // 32), rows), q, k_cache, v_cache, mask, out)
     return _check("subspec_tree_attention_kv4", load_library().subspec_tree_attention_kv4(
         pq, ck, cv, pm, M, Hq, Hkv, S, P, T, group, scale, po, st))
 
@@ -395,8 +436,11 @@ def subspec_tree_attention_kv4_plan(M, Hq, Hkv, P, T):
 
 
 def subspec_tree_verify(logits, parent, token, uniform, N, V, temperature, path, accepted, next_token, stream=None) -> int:
-    st, pl, pp, pt, pu, po, pa, pn = _device_args("subspec_tree_verify", stream, logits, parent, token, uniform, path,
-                                                  accepted, next_token)
+    if not temperature:  # not read
+        uniform = None
+    st, pl, pp, pt, pu, po, pa, pn = _device_args(
+        "subspec_tree_verify", stream, ("bf16", "i32", "i32", "f32", "i32", "i32", "i32"),
+        ((N + 1) * V, N, N, N + 1, N, 1, 1), logits, parent, token, uniform, path, accepted, next_token)
     return _check("subspec_tree_verify", load_library().subspec_tree_verify(
         pl, pp, pt, pu, N, V, temperature, po, pa, pn, st))
 

@@ -174,7 +174,7 @@ def _device_args(fn: str, stream, kinds, needs, *args):
             types, least = [*compress(types, there)], compress(needs, there)
         try:
             on = {*map(_get_device, given)}
-            dev = on.pop()
+            dev = on.pop() if on else -1
             if (not on and dev >= 0 and dev == _device() and all(map(_is_contiguous, given)) and
                     [*map(_dtype, given)] == types and all(map(ge, map(_numel, given), least))):
                 ptr = map(_data_ptr, given)

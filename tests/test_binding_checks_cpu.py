@@ -160,3 +160,14 @@ def test_sizes_of_caches_agree_with_the_library():
 def test_arrays_are_no_device_tensors(calls):
     with pytest.raises(TypeError):
         _append(_args("append", k=np.zeros(8 * Hkv * 128, np.int16)))
+
+
+@pytest.mark.parametrize("call", CALLS)
+def test_calls_without_any_tensor_reach_the_librarys_refusal(monkeypatch, call):
+    # the mapped way is there from the first call on a device on
+    for name, value in dict(_torch=torch, _get_device=Fake.get_device, _device=lambda: 0, _raw_stream=lambda dev: 0).items():
+        monkeypatch.setattr(_binding, name, value)
+    monkeypatch.setattr(_binding, "_current_device", lambda stream: 0)
+    monkeypatch.setattr(_binding, "_stream", lambda stream: 0)
+    with pytest.raises(ss.SubspecError, match="EINVAL.*null pointer"):
+        CALLS[call][0](dict.fromkeys(CALLS[call][1]))

@@ -435,8 +435,8 @@ int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, i
  *   out      device bf16 [M][Hq][128]; a query with no visible position gets zeros
  * Scores are fp32 sums over exact codes.  A position's weight is rounded to fp16, and its product
  * with the value's scale once more, before the second product, which sums in fp32: 11 bits each, or
- * 2^(E - 29) of the heaviest weight in absolute terms (2^E, at least 1, the largest scale of a
- * value seen).  What positions hold that no query sees changes no bit of the result.  Limits as
+ * in absolute terms 2^-29 of the heaviest weight times the largest scale of a value (of the weight
+ * alone 2^(E - 29), 2^E at least 1 and at least that scale).  What positions hold that no query sees changes no bit of the result.  Limits as
  * subspec_tree_attention's (Hkv at most 65535, S a multiple of 32); q, caches and out
  * 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one where
  * a single range covers the positions); workspace as for subspec_qlinear

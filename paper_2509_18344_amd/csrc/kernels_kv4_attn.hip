@@ -17,8 +17,10 @@
 // Roundings: a weight p to fp16, its product with the scale to fp16 again (2^-11 relative at most, an
 // eighth of what rounding the output to bf16 may cost, and independent from position to
 // position); everything else is exact or in 32 bits.  fp16 spans 2^-24 .. 65504, so weights are
-// relative to a reference that covers score + log2 of the tile's largest scale: p and p s stay
-// below 2^15, and the heaviest position's p is at least 2^8 while scales lie below 1.  The
+// relative to a reference that covers score + log2 of the tile's largest scale where that passes 1: p
+// and p s stay below 2^15, and the heaviest position's p is at least 2^8 while scales lie below 1.
+// Scales below 1 are raised by the power of two that brings the largest of the wavefront's so far to
+// 1/2 .. 1, and its sums lowered when a larger one comes: values of any size keep the same bits.  The
 // reference moves only when a weight would pass 2^14 (a few times in a row's life), so most
 // tiles scale nothing.
 //
@@ -203,6 +205,9 @@ __device__ __forceinline__ uint32_t kv4_row_max(uint32_t v) {
   return max(v & 0xFFFFu, v >> 16);
 }
 
+// 2^n, n in -126 .. 127.
+__device__ __forceinline__ float kv4_exp2i(int n) { return __uint_as_float(static_cast<uint32_t>(n + 127) << 23); }
+
 // Orders a wavefront's LDS accesses to each other's words, for the compiler (the hardware keeps
 // them in order).
 __device__ __forceinline__ void kv4_wave_fence() {
@@ -228,6 +233,7 @@ struct Kv4Rows {
   int qi[QW];
   float ref[QW];              // what weights are relative to: 2^(score - ref)
   f32x4_t o[QW][8], aux[QW];  // aux: in quarter 0 the sum of weights, and of weights times minima
+  int field;                  // the largest fp16 exponent field of a scale so far, at most 14: o stands for 2^(14 - field) of its sums
   u32x4_t raw[QW][4];
 
   __device__ __forceinline__ void request(const Kv4AttnArgs& a, int g, int row0, int lane) {
@@ -244,6 +250,7 @@ struct Kv4Rows {
   }
 
   __device__ __forceinline__ void begin(const Kv4AttnArgs& a) {
+    field = 0;
 #pragma unroll
     for (int t = 0; t < QW; ++t) {
       uint32_t top = 0;
@@ -332,14 +339,28 @@ struct Kv4Rows {
   // Weights of the tile's positions, and their products with the values.  keep, ones: the
   // auxiliary operand's first row is ones.
   __device__ __forceinline__ void values(const Kv4Values<G>& v, const f32x4_t (&x)[QW][2], uint32_t keep, uint32_t ones) {
-    // the exponent of the tile's largest scale, at least 0 (fp16's field: s < 2^(field - 14))
+    // The largest scale's exponent (fp16's field: s < 2^(field - 14)).  Scales from 1 on lower the weights;
+    // of smaller ones all are raised by the same power of two (exact), so that neither they nor their
+    // products with weights fall to fp16's subnormals before a weight does by itself.
     uint32_t top = 0;
 #pragma unroll
     for (int gg = 0; gg < G; ++gg)
 #pragma unroll
       for (int e = 0; e < 4; ++e) top = kv4_max_halves(top, v.s[gg][e]);
-    const int field = static_cast<int>((kv4_row_max(top) & 0x7FFFu) >> 10);
-    const float lift = static_cast<float>(max(field - 14, 0) - 8);
+    const int most = __builtin_amdgcn_readfirstlane(static_cast<int>((kv4_row_max(top) & 0x7FFFu) >> 10));
+    const float lift = static_cast<float>(max(most - 14, 0) - 8);
+    if (min(most, 14) > field) {  // the largest so far
+      const float down = kv4_exp2i(field - min(most, 14));
+      field = min(most, 14);
+#pragma unroll
+      for (int t = 0; t < QW; ++t)
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) o[t][dt] *= down;
+    }
+    const _Float16 raise = __builtin_bit_cast(_Float16, static_cast<uint16_t>((29 - field) << 10));  // 2^(14 - field)
+    f16x8_t sc[G];
+#pragma unroll
+    for (int gg = 0; gg < G; ++gg) sc[gg] = __builtin_bit_cast(f16x8_t, v.s[gg]) * raise;
 
     f16x8_t pf[QW][G], ps[QW];
 #pragma unroll
@@ -371,7 +392,7 @@ struct Kv4Rows {
       for (int e = 2; e < 8; ++e)
         if (e % 4 >= 2) pq[e] = ps[t][e] * static_cast<_Float16>(0.0625f);
 #pragma unroll
-      for (int gg = 0; gg < G; ++gg) pf[t][gg] = pq * __builtin_bit_cast(f16x8_t, v.s[gg]);
+      for (int gg = 0; gg < G; ++gg) pf[t][gg] = pq * sc[gg];
     }
     u32x4_t w;
 #pragma unroll
@@ -388,8 +409,9 @@ struct Kv4Rows {
     }
   }
 
-  // Codes back from 2^-24, minima added.
+  // Codes back from 2^-24, scales from their raise, minima added.
   __device__ __forceinline__ void finish(int col) {
+    const float back = kv4_exp2i(10 + field);
 #pragma unroll
     for (int t = 0; t < QW; ++t)
 #pragma unroll
@@ -398,7 +420,7 @@ struct Kv4Rows {
 #pragma unroll
         for (int dt = gg * (8 / G); dt < (gg + 1) * (8 / G); ++dt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[t][dt][e] = __builtin_fmaf(o[t][dt][e], 0x1p24f, z);
+          for (int e = 0; e < 4; ++e) o[t][dt][e] = __builtin_fmaf(o[t][dt][e], back, z);
       }
   }
 };

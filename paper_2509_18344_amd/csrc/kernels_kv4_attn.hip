@@ -220,6 +220,13 @@ __device__ __forceinline__ void kv4_wave_fence() {
 // half of 1 / M before the 32-bit product's rounding.
 __device__ __forceinline__ int kv4_row_head(int row, float inv_m) { return static_cast<int>((static_cast<float>(row) + 0.5f) * inv_m); }
 
+// From this reference on a row's scores are rounded before the reference is taken from them.  Below,
+// the rounding of the reference (2^-5) is a common factor of the row's weights.  Above, the exact
+// product and the rounded reference may lie further apart than fp16's range, while fp32 holds no
+// score more closely than that; the rounded ones of equal positions are equal, and the reference is
+// the largest itself, so that no weight passes 1.
+constexpr float kVast = 0x1p20f;
+
 // Query rows of one wavefront (QW tiles of 16) and what it has summed for them.
 template <int QW, int G>
 struct Kv4Rows {
@@ -278,7 +285,8 @@ struct Kv4Rows {
           for (int i = 0; i < 8; ++i) (i / 2 % 2 == 0 ? sum : sum16) += static_cast<float>(qf[t][j][i]);
         qs[t][gg] = kv4_cross_sum(__builtin_fmaf(16.f, sum16, sum)) * 0x1p-24f;
       }
-      factor[t] = fminf(fmaxf(ldexpf(a.scale_log2, 9 + e), 0x1p-126f), 0x1p126f);
+      // |x| stays below 2^16, so no score overflows; a factor of 2^110 has long left one position alone.
+      factor[t] = fminf(fmaxf(ldexpf(a.scale_log2, 9 + e), 0x1p-126f), 0x1p110f);
       ref[t] = -INFINITY;
       aux[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -370,9 +378,12 @@ struct Kv4Rows {
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, x[t][u][e]);
-      const float cand = __builtin_fmaf(kv4_cross_max(mx), factor[t], lift);
-      if (__builtin_amdgcn_ballot_w64(cand > ref[t] + 6.f)) {  // some row's weights would pass 2^14
-        const float r = cand > ref[t] + 6.f ? cand : ref[t];
+      const float most_score = kv4_cross_max(mx) * factor[t];
+      const bool vast = fabsf(most_score) >= kVast;
+      const float cand = vast ? most_score : most_score + lift;
+      const bool move = cand - ref[t] > (vast ? 0.f : 6.f);
+      if (__builtin_amdgcn_ballot_w64(move)) {  // some row's weights would pass 2^14
+        const float r = move ? cand : ref[t];
         const float alpha = ref[t] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[t] - r);
         ref[t] = r;
         aux[t] *= alpha;
@@ -380,11 +391,21 @@ struct Kv4Rows {
         for (int dt = 0; dt < 8; ++dt) o[t][dt] *= alpha;
       }
       const float base = ref[t] == -INFINITY ? 0.f : ref[t];  // nothing visible yet: every weight is 2^-inf
+      f32x4_t y[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          ps[t][4 * u + e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(__builtin_fmaf(x[t][u][e], factor[t], -base)));
+        for (int e = 0; e < 4; ++e) y[u][e] = __builtin_fmaf(x[t][u][e], factor[t], -base);
+      if (__builtin_amdgcn_ballot_w64(fabsf(base) >= kVast)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[u][e] = fabsf(base) >= kVast ? x[t][u][e] * factor[t] - base : y[u][e];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) ps[t][4 * u + e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(y[u][e]));
       // times the scales, and 2^-4 where the codes are 16 times as large (positions 2 and 3 of each
       // four: before the scale, which may be a subnormal already)
       f16x8_t pq = ps[t];

@@ -9,6 +9,8 @@ import pytest
 
 import oracle
 import paper_2509_18344_amd as ss
+from paper_2509_18344_amd import synth
+from oracle.tree_attn import visible_positions
 from test_gpu_kv4_attn import _bf16, _fill, _held, _run
 
 torch = pytest.importorskip("torch")
@@ -30,6 +32,75 @@ def _score_error(q, kh, group, scale=SCALE):
     G = q.shape[1] // size.shape[1]
     return np.stack([2.0 ** -20 * abs(scale) * (qa[:, h] @ size[:, h // G].T).max(1) for h in range(q.shape[1])], 1)
 
+
+# --- very large scores -----------------------------------------------------------------------------
+
+LARGE = [
+    (6, 28, 4, 100, 42),    # a workgroup takes a head whole
+    (6, 28, 4, 2048, 60),   # ranges, tiles in registers
+    (8, 16, 2, 3000, 90),   # 64 rows a head
+    (1, 128, 128, 2500, 0),   # five tiles a wavefront and more, in a ring
+    (6, 64, 32, 5000, 20),
+]
+
+
+@pytest.mark.parametrize("q_size,k_size", [(1e3, 1e2), (1e5, 1e3), (1e6, 3e3), (1e8, 1e4), (1e30, 1e4), (1e36, 1e4)])
+@pytest.mark.parametrize("M,Hq,Hkv,P,T", LARGE)
+def test_kv4_attention_of_very_large_scores_is_the_largest_ones_value(M, Hq, Hkv, P, T, q_size, k_size):
+    """Scores of 2^17 and more, where fp32 holds no fraction of them: a row whose largest score
+    lies further above the second than both may be off gets that position's value."""
+    group = 64 if P % 3 else 128
+    n, S = P + T + M, (P + T + M + 31) // 32 * 32
+    rng = np.random.default_rng([M, Hq, P, int(math.log10(q_size))])
+    q = _bf16(rng.standard_normal((M, Hq, D)) * q_size)
+    own = min(Hkv, 2)
+    k, v = rng.standard_normal((n, own, D)) * k_size, rng.standard_normal((n, own, D)) + 0.5
+    k, v = (_bf16(a)[:, np.arange(Hkv) % own] for a in (k, v))
+    mask = synth.tree_levels_mask(T, 6, M, 5)
+    got = _run(q, *_fill(k, v, S, group), mask, M, Hq, Hkv, S, P, T, group, SCALE)
+    assert np.isfinite(got).all()
+    some = sorted({0, Hkv // 2, Hkv - 1})
+    G = Hq // Hkv
+    heads = [g * G + i for g in some for i in range(G)]
+    q, got, k, v = q[:, heads], got[:, heads], k[:, some], v[:, some]
+    kh, vh = _held(k, group), _held(v, group)
+    K, V = oracle.kv4_value(*kh), oracle.kv4_value(*vh)
+    err = _score_error(q, kh, group)
+    apart = 0
+    for i in range(M):
+        pos = visible_positions(mask, i, P, T, M)
+        for h in range(len(heads)):
+            sc = K[pos, h // G] @ oracle.bf16_bits_to_f64(q)[i, h] * SCALE
+            first, second = np.argsort(sc)[-1:-3:-1]
+            if sc[first] - sc[second] < 2 * err[i, h] + 30:  # e^-30: the others' share is nothing
+                continue
+            apart += 1
+            ref = V[pos[first], h // G]
+            tol = 2.0 ** -8 * np.abs(ref) + 2.0 ** -10 * np.abs(V).max()
+            assert np.all(np.abs(got[i, h] - ref) <= tol), (i, h, np.abs(got[i, h] - ref).max())
+    assert apart > 0.8 * M * len(heads)
+
+
+@pytest.mark.parametrize("q_size", [1e3, 1e5, 1e7, 1e9])
+@pytest.mark.parametrize("M,Hq,Hkv,P,T", LARGE)
+def test_kv4_attention_of_equal_large_scores_is_their_values_mean(M, Hq, Hkv, P, T, q_size):
+    """Positions with the same key have the same score to the bit, however large, and weigh the
+    same wherever they lie: in other tiles, wavefronts and ranges."""
+    group, n = 64, P + T + M
+    S = (n + 31) // 32 * 32
+    rng = np.random.default_rng([M, Hq, P])
+    q = _bf16(np.abs(rng.standard_normal((M, Hq, D)) + 2.0) * q_size)
+    k = -np.abs(rng.standard_normal((n, 1, D))) * 1e3
+    alike = np.unique(np.concatenate([[3, P - 1], rng.choice(P, 5, replace=False)]))
+    k[alike] = np.abs(rng.standard_normal((1, 1, D))) * 1e3  # scores above every other
+    v = rng.standard_normal((n, 1, D))
+    k, v = (_bf16(a)[:, np.zeros(Hkv, int)] for a in (k, v))
+    mask = synth.tree_levels_mask(T, 6, M, 5)
+    got = _run(q, *_fill(k, v, S, group), mask, M, Hq, Hkv, S, P, T, group, SCALE)
+    ref = oracle.kv4_value(*_held(v[:, :1], group))[alike, 0]
+    # the weights are equal, but each rounds with its value's scale: 2^-11 of the parts of a value
+    tol = 2.0 ** -8 * np.abs(ref.mean(0)) + 2.0 ** -10 * (np.abs(ref).mean(0) + 4.0)
+    assert np.all(np.abs(got - ref.mean(0)) <= tol), np.abs(got - ref.mean(0)).max()
 
 
 # --- small values ------------------------------------------------------------------------------------

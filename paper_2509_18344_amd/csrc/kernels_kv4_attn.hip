@@ -14,9 +14,12 @@
 // from one more product against rows of ones and of minima, so that the numerator's and the
 // denominator's weights are the same numbers.
 //
-// Roundings: a weight p to fp16, its product with the scale to fp16 again (2^-11 relative at most, an
-// eighth of what rounding the output to bf16 may cost, and independent from position to
-// position); everything else is exact or in 32 bits.  fp16 spans 2^-24 .. 65504, so weights are
+// A weight p, and its product with the scale, go into the products as sums of two fp16 numbers each:
+// the number rounded and what the rounding left (of the product an fma returns it exactly), 21 bits
+// and more.  One number each costs 13 % less at 131138 positions (42.8 us against 48.2) and 1 to 4 %
+// at a few thousand, but is off by 2^-11 twice, which 5 to 9 % of outputs show in their last bit where
+// values cancel.
+// Everything else is exact or in 32 bits.  fp16 spans 2^-24 .. 65504, so weights are
 // relative to a reference that covers score + log2 of the tile's largest scale where that passes 1: p
 // and p s stay below 2^15, and the heaviest position's p is at least 2^8 while scales lie below 1.
 // Scales below 1 are raised by the power of two that brings the largest of the wavefront's so far to
@@ -55,6 +58,8 @@ namespace subspec {
 namespace {
 
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
 
 // Visibility of the 32 positions key0 .. for one query row (bit k: key0 + k): committed
@@ -203,6 +208,14 @@ __device__ __forceinline__ uint32_t kv4_row_max(uint32_t v) {
   w = kv4_swap32(kv4_max_halves(w[0], w[1]));
   v = kv4_max_halves(w[0], w[1]);
   return max(v & 0xFFFFu, v >> 16);
+}
+
+// -1, unknown to the compiler: the difference of an fp32 number and an fp16 one stays one fma that takes
+// both as they are (otherwise a conversion and a subtraction).
+__device__ __forceinline__ float kv4_minus_one() {
+  float m = -1.f;
+  asm("" : "+v"(m));
+  return m;
 }
 
 // 2^n, n in -126 .. 127.
@@ -366,11 +379,14 @@ struct Kv4Rows {
         for (int dt = 0; dt < 8; ++dt) o[t][dt] *= down;
     }
     const _Float16 raise = __builtin_bit_cast(_Float16, static_cast<uint16_t>((29 - field) << 10));  // 2^(14 - field)
-    f16x8_t sc[G];
+    f16x2_t sc[G][4];
 #pragma unroll
-    for (int gg = 0; gg < G; ++gg) sc[gg] = __builtin_bit_cast(f16x8_t, v.s[gg]) * raise;
+    for (int gg = 0; gg < G; ++gg)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[gg][e] = __builtin_bit_cast(f16x2_t, static_cast<uint32_t>(v.s[gg][e])) * raise;
 
-    f16x8_t pf[QW][G], ps[QW];
+    const float minus = kv4_minus_one();
+    u32x4_t ps[QW][2], pf[QW][G][2];  // weights, and their products with the scales, as sums of two
 #pragma unroll
     for (int t = 0; t < QW; ++t) {
       float mx = -INFINITY;
@@ -405,28 +421,43 @@ struct Kv4Rows {
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) ps[t][4 * u + e] = static_cast<_Float16>(__builtin_amdgcn_exp2f(y[u][e]));
-      // times the scales, and 2^-4 where the codes are 16 times as large (positions 2 and 3 of each
-      // four: before the scale, which may be a subnormal already)
-      f16x8_t pq = ps[t];
+        for (int e = 0; e < 4; e += 2) {
+          const f32x2_t w{__builtin_amdgcn_exp2f(y[u][e]), __builtin_amdgcn_exp2f(y[u][e + 1])};
+          const f16x2_t hi = __builtin_convertvector(w, f16x2_t);
+          const f16x2_t lo = __builtin_convertvector(f32x2_t{__builtin_fmaf(static_cast<float>(hi[0]), minus, w[0]),
+                                                             __builtin_fmaf(static_cast<float>(hi[1]), minus, w[1])}, f16x2_t);
+          ps[t][0][2 * u + e / 2] = __builtin_bit_cast(uint32_t, hi);
+          ps[t][1][2 * u + e / 2] = __builtin_bit_cast(uint32_t, lo);
+          // Times the scales, and 2^-4 where the codes are 16 times as large (positions 2 and 3 of each
+          // four).  The first product's rounding is exact in the fma that returns it, and goes to the second.
+          const _Float16 part = static_cast<_Float16>(e == 0 ? 1.f : 0.0625f);
+          const f16x2_t qh = hi * part, ql = lo * part;
 #pragma unroll
-      for (int e = 2; e < 8; ++e)
-        if (e % 4 >= 2) pq[e] = ps[t][e] * static_cast<_Float16>(0.0625f);
-#pragma unroll
-      for (int gg = 0; gg < G; ++gg) pf[t][gg] = pq * sc[gg];
+          for (int gg = 0; gg < G; ++gg) {
+            const f16x2_t c = sc[gg][2 * u + e / 2], h = qh * c;
+            pf[t][gg][0][2 * u + e / 2] = __builtin_bit_cast(uint32_t, h);
+            pf[t][gg][1][2 * u + e / 2] =
+                __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(ql, c, __builtin_elementwise_fma(qh, c, -h)));
+          }
+        }
     }
     u32x4_t w;
 #pragma unroll
     for (int e = 0; e < 4; ++e) w[e] = and_or(v.m[e], keep, ones);
 #pragma unroll
-    for (int t = 0; t < QW; ++t)
-      aux[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, w), ps[t], aux[t], 0, 0, 0);
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int t = 0; t < QW; ++t)
+        aux[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, w), __builtin_bit_cast(f16x8_t, ps[t][i]),
+                                                       aux[t], 0, 0, 0);
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) {
       const f16x8_t vf = kv4_codes(v.c[dt / 4][dt % 4]);
 #pragma unroll
-      for (int t = 0; t < QW; ++t)
-        o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[t][dt * G / 8], o[t][dt], 0, 0, 0);
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int t = 0; t < QW; ++t)
+          o[t][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, __builtin_bit_cast(f16x8_t, pf[t][dt * G / 8][i]), o[t][dt], 0, 0, 0);
     }
   }
 

@@ -33,6 +33,11 @@ def _score_error(q, kh, group, scale=SCALE):
     return np.stack([2.0 ** -20 * abs(scale) * (qa[:, h] @ size[:, h // G].T).max(1) for h in range(q.shape[1])], 1)
 
 
+def _half_step(x):
+    """Half the distance of bf16 numbers (8 bits) at |x|."""
+    return np.ldexp(1.0, np.frexp(np.maximum(np.abs(x), 2.0 ** -126))[1] - 9)
+
+
 # --- very large scores -----------------------------------------------------------------------------
 
 LARGE = [
@@ -132,3 +137,31 @@ def test_kv4_attention_keeps_small_values_beside_heavy_positions(M, Hq, Hkv, P, 
     err = 2 * _score_error(q[:, :1], kh, group)[..., None]
     tol = 2.0 ** -8 * np.abs(ref) + (err + 2.0 ** -11) * (3 * wabs + wmin)
     assert np.all(np.abs(got - ref) <= tol), float((np.abs(got - ref) / tol).max())
+
+
+# --- the weights' bits -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("M,Hq,Hkv,P,T", [(6, 28, 4, 0, 26), (1, 8, 8, 40, 0), (8, 16, 2, 3, 90), (4, 128, 128, 11, 8),
+                                          (6, 28, 4, 2048, 60), (1, 128, 128, 2500, 0)])
+def test_kv4_attention_rounds_once(M, Hq, Hkv, P, T, group):
+    """Values of either sign, so that outputs are small beside the terms they are sums of: an output
+    is the bf16 number next to the exact one but for the scores' error and 2^-17 of the terms' sizes
+    (a weight carries 21 bits, its product with the scale 20, sums are in fp32)."""
+    n, S = P + T + M, (P + T + M + 31) // 32 * 32
+    rng = np.random.default_rng([M, Hq, P, T])
+    q, k = rng.standard_normal((M, Hq, D)) * 0.2, rng.standard_normal((n, 1, D)) * 0.2
+    v = np.where(rng.random((n, 1, D)) < 0.5, -1.0, 1.0) * 2.0 ** rng.integers(-2, 3, (n, 1, 1))
+    q, k, v = _bf16(q), _bf16(k), _bf16(v)
+    mask = rng.integers(0, 2 ** 32, (M, (T + M + 31) // 32), dtype=np.uint64).astype(np.uint32)
+    mask[:, 0] |= 1
+    heads = np.zeros(Hkv, int)
+    got = _run(q, *_fill(k[:, heads], v[:, heads], S, group), mask, M, Hq, Hkv, S, P, T, group, SCALE)
+    q, got = q[:, :28], got[:, :28]
+    kh, vh = _held(k, group), _held(v, group)
+    ref, wabs = oracle.tree_attention_values(q, oracle.kv4_value(*kh), oracle.kv4_value(*vh), P, T, mask, SCALE)
+    # the sums run over the minimum's and the codes' parts of a value: up to three times its size
+    err = (2 * _score_error(q, kh, group)[..., None] + 2.0 ** -17) * 3 * wabs
+    tol = _half_step(np.abs(ref) + err) + err
+    off = np.abs(got - ref) > tol
+    assert not off.any(), (int(off.sum()), off.size, float((np.abs(got - ref) / tol).max()))

@@ -61,7 +61,8 @@ struct RopeTurn {
 };
 
 // cs: cos and sin of the rot / 2 frequencies.  Pairs are (d, d + rot / 2), the partner rot / 16
-// lanes away, or (interleaved) neighbours in the lane.  Past `rot` the turn is none.
+// lanes away, or (interleaved) neighbours in the lane.  Lanes past `rot` have no turn (rope_rotate
+// leaves them alone: a turn by nothing would make NaN of infinities).
 __device__ __forceinline__ RopeTurn rope_turn(int col, int rot, int interleaved, const float2* cs) {
   RopeTurn t;
   const int chunks = rot / 8, h = chunks / 2;
@@ -87,8 +88,9 @@ __device__ __forceinline__ void rope_norm(float (&x)[8], const float (&w)[8], fl
   for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
 }
 
-// The rotation of a head row.  FULL: all 128 dimensions in pairs (d, d + 64), whose partner
-// is eight lanes away in the row of 16 (a DPP move instead of one through LDS).
+// The rotation of a head row; the dimensions past `rot`, whole lanes, stay as they are.  FULL: all 128
+// dimensions in pairs (d, d + 64), whose partner is eight lanes away in the row of 16 (a DPP move
+// instead of one through LDS).
 template <bool FULL>
 __device__ __forceinline__ void rope_rotate(float (&x)[8], int col, int rot, int interleaved, const RopeTurn& t) {
   float other[8];
@@ -105,8 +107,9 @@ __device__ __forceinline__ void rope_rotate(float (&x)[8], int col, int rot, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) other[i] = __shfl(x[i], from);
   }
+  const bool turned = FULL || 8 * col < rot;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __builtin_fmaf(x[i], t.c[i], other[i] * t.s[i]);
+  for (int i = 0; i < 8; ++i) x[i] = turned ? __builtin_fmaf(x[i], t.c[i], other[i] * t.s[i]) : x[i];
 }
 
 }  // namespace subspec

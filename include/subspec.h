@@ -473,7 +473,9 @@ int subspec_tree_attention_kv4_plan(int M, int Hq, int Hkv, int P, int T, int* s
  *   accepted  device int32 [1]: how many
  *   next_token  device int32 [1]: the token after them; -1 where its row has none (NaN or +inf
  *             among its logits, or -inf in all)
- * Probabilities of drafted tokens in fp32 (relative error about 2^-20), the rest of the last row in fp64.
+ * A row's probabilities of drafted tokens rest on exponentials in fp32 (fp64 in drafts of up to about
+ * 2000 slices of 2048 logits), summed in fp64: the borders between them are off by less than 2^-18 of
+ * their place in [0, 1).  The rest of the last row is in fp64.
  * Needs 0 <= N <= 1024, V a multiple of 8 in 8 .. 2^20, temperature 0 or finite with finite
  * inverse; logits 16-byte aligned, the others 4-byte; N = 0 needs no parent, token or path
  * (null).  Workspace as for subspec_qlinear (subspec_tree_verify_workspace_bytes). */

@@ -1326,7 +1326,7 @@ int subspec_tree_verify(const void* logits, const int* parent, const int* token,
     return fail(SUBSPEC_EUNSUPPORTED, "tree_verify: N=%d: must be in 0..%d", N, subspec::kVerifyMaxTokens);
   if (V < 8 || V % 8 || V > subspec::kVerifyMaxV)
     return fail(SUBSPEC_EUNSUPPORTED, "tree_verify: V=%d: must be a multiple of 8 in 8..%d", V, subspec::kVerifyMaxV);
-  const float c = 1.4426950408889634f / temperature;
+  const float c = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
   if (temperature != 0.f && (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(c)))
     return fail(SUBSPEC_EINVAL, "tree_verify: temperature must be 0 or positive and finite, with a finite inverse");
   if (!logits || !accepted || !next_token || (N > 0 && (!parent || !token || !path)) || (temperature != 0.f && !uniform))

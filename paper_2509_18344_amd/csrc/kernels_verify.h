@@ -22,7 +22,7 @@ struct VerifyArgs {
   int chunks, chunk_len;   // workgroups per row and the logits each one covers
   // workspace
   unsigned* cnt;           // completion counters (zero between launches): the residual's slices, rows, slices of each row
-  float2* stat;            // [N + 1][chunks] maximum, and sum of 2^(c (l - maximum)) (greedy: the maximum's token)
+  float2* stat;            // [N + 1][chunks] reference, and sum of 2^(c (l - reference)) (greedy: the maximum and its token)
   float2* row_stat;        // [N + 1] the same of whole rows
   int* next;               // [N + 1] the drafted token that a row picks, or -1
   float2* last_stat;       // [1] row_stat of the path's last row

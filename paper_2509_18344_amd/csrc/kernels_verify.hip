@@ -17,8 +17,8 @@
 // V = 32000 9.8 us a call against 15.3 with two kernels, 26 tokens at V = 152064, 2025 slices, 15.3
 // against 17.7; 130 at 32000, 2096, 17.0 against 16.5).  Beyond, two, since 64-bit exponentials of all
 // logits would bound them:
-//   k_verify_rows      per (row, slice) workgroup the maximum and the sum, in 32 bits; the last
-//                      of a row finds the child that the row picks, the last of all the path
+//   k_verify_rows      per (row, slice) workgroup a reference and the sum, of exponentials in 32 bits; the
+//                      last of a row finds the child that the row picks, the last of all the path
 //   k_verify_residual  the last row's other tokens in 64 bits: with V = 152064 tokens the
 //                      borders lie 10^-5 apart, and a sum in 32 bits, 10^-7 off, would pick a
 //                      neighbour in one call of a hundred; the last workgroup finds the token
@@ -71,12 +71,18 @@ __device__ __forceinline__ void best_of(float& m, int& i, float m2, int i2) {
   i = take ? i2 : i;
 }
 
-// What is kept of logits seen: (maximum, sum of 2^(c (l - maximum))), or greedy (maximum, the first
-// token of the eight that it was found in).
+// What is kept of logits seen: (reference, sum of 2^(c (l - reference))), or greedy (maximum, the first
+// token of the eight that it was found in).  The reference is a logit that the largest one passes by less
+// than 2^kAhead: it moves so far that what the move's rounding costs the sum so far is nothing
+// beside what comes.  A thread adds its sums of eight in 64 bits (`sum`, one addition in eight terms): bf16
+// logits repeat, and in 32 bits the roundings of 4096 equal terms were off by 2^-14 together.
+constexpr float kAhead = 16.f;
+
 template <bool GREEDY>
 struct Seen {
   float m = -INFINITY;
   float s = GREEDY ? __int_as_float(INT_MAX) : 0.f;
+  double sum = 0.0;
 
   __device__ __forceinline__ void add(float c, const float (&x)[8], int v0) {
     if constexpr (GREEDY) {
@@ -88,17 +94,25 @@ struct Seen {
       m = take ? mx : m;
       s = take ? __int_as_float(v0) : s;
     } else {
-      float mx = m;
+      float mx = x[0];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mx = fmaxf(mx, x[e]);
-      if (__builtin_amdgcn_ballot_w64(mx > m)) {
-        s = m == -INFINITY ? s : s * __builtin_amdgcn_exp2f(c * (m - mx));
-        m = mx;
+      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
+      const bool move = c * (mx - m) > kAhead;
+      if (__builtin_amdgcn_ballot_w64(move)) {
+        sum = move && m != -INFINITY ? sum * static_cast<double>(__builtin_amdgcn_exp2f(c * (m - mx))) : sum;
+        m = move ? mx : m;
       }
       const float base = m == -INFINITY ? 0.f : m;  // (2^-inf of -inf, and a NaN that the sum has to show)
+      float t[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s += __builtin_amdgcn_exp2f(c * (x[e] - base));
+      for (int e = 0; e < 8; ++e) t[e] = __builtin_amdgcn_exp2f(c * (x[e] - base));
+      sum += static_cast<double>(((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7])));
     }
+  }
+
+  // The thread's logits are all added.
+  __device__ __forceinline__ void close() {
+    if constexpr (!GREEDY) s = static_cast<float>(sum);
   }
 
   // What the wavefront's lanes have seen, in every lane.
@@ -252,6 +266,7 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
         take(now, i + j);
       }
   if (lo + tiles * kRowTile + 8 * t < hi) take(tile(tiles), tiles);  // its last, partial tile
+  seen.close();
   seen.across_wave(a.c);
   if (t % kWave == 0) waves[t / kWave] = make_float2(seen.m, seen.s);
   __syncthreads();
@@ -301,10 +316,10 @@ __global__ __launch_bounds__(kRowThreads) void k_verify_rows(VerifyArgs a) {
     }
     __syncthreads();
     if (!GREEDY && t == 0) {
-      const float at = a.uniform[row];
-      float f = 0.f;
+      const double at = static_cast<double>(a.uniform[row]);
+      double f = 0.0;  // (a thousand shares in a row)
       for (int k = 0; k < nk; ++k) {
-        const float f2 = f + u.order.p[k];
+        const double f2 = f + static_cast<double>(u.order.p[k]);
         if (f <= at && at < f2) {
           pick = u.order.j[k];
           break;
@@ -697,7 +712,7 @@ bool verify_small(int N, int V) {
 
 // After the completion counters, small calls: the slices' sums and maxima, the rows' picks and the
 // tokens of those that end the path.  Others: the last row
-// and its (maximum, sum), its slices' sums, the rows' (maximum, sum) pairs, the slices' of
+// and its (reference, sum), its slices' sums, the rows' (reference, sum) pairs, the slices' of
 // rows, the rows' picks.
 size_t verify_workspace_bytes(int N, int V) {
   int chunks = 0, len = 0;

@@ -9,7 +9,6 @@ namespace subspec {
 constexpr int kVerifyMaxTokens = 1024;
 constexpr int kVerifyMaxV = 1 << 20;
 constexpr int kVerifySlice = 2048;  // logits per workgroup of the kernels in 64 bits
-constexpr int kVerifySmall = 2200;   // slices in all up to which one kernel does everything
 
 struct VerifyArgs {
   const uint16_t* logits;  // bf16 [N + 1][V]

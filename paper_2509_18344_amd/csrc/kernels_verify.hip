@@ -11,11 +11,10 @@
 // All rows are read at once, although only those on the path matter, because the path is
 // known only at its end: a row needs its maximum and its sum of exponentials to say which
 // child it picks, not the whole distribution.
-// Up to kVerifySmall slices of 2048 logits in all one kernel does everything in 64 bits
+// Up to 1750 to 2200 slices of 2048 logits in all (verify_small) one kernel does everything in 64 bits
 // (k_verify_small: a slice its maximum and its sum without the row's children, the last workgroup of a
 // row the row's pick and, where that ends the path, its token, the last of all the path: a chain of 4 at
-// V = 32000 9.8 us a call against 15.3 with two kernels, 26 tokens at V = 152064, 2025 slices, 15.3
-// against 17.7; 130 at 32000, 2096, 17.0 against 16.5).  Beyond, two, since 64-bit exponentials of all
+// V = 32000 9.8 us a call against 15.3 with two kernels).  Beyond, two, since 64-bit exponentials of all
 // logits would bound them:
 //   k_verify_rows      per (row, slice) workgroup a reference and the sum, of exponentials in 32 bits; the
 //                      last of a row finds the child that the row picks, the last of all the path
@@ -696,8 +695,9 @@ __global__ __launch_bounds__(kResThreads) void k_verify_small(VerifyArgs a) {
 }  // namespace
 
 void verify_plan(int N, int V, int* chunks, int* chunk_len) {
-  // about 640 workgroups (289 rows in three slices 21.2 us, in four 23.7, in seven 24.4), each with at
-  // least two tiles
+  // about 640 workgroups, each with at least two tiles (a call at V = 152064 against 320 and 1280 of them:
+  // 34 rows 18.5 us, 19.4 and 18.7; 101 rows 20.7, 21.4 and 21.2; 289 rows 29.0, 29.3 and 29.2; 1025
+  // rows 73.5, 74.1 and 83.3; greedy 61 rows 10.1, 10.7 and 10.6)
   int c = (640 + N) / (N + 1);
   const int most = (V + 2 * kRowTile - 1) / (2 * kRowTile);
   if (c > most) c = most;
@@ -706,8 +706,12 @@ void verify_plan(int N, int V, int* chunks, int* chunk_len) {
   *chunks = (V + *chunk_len - 1) / *chunk_len;
 }
 
+// One kernel against two, us a call.  16 slices a row: 1456 in all 14.7 against 15.9, 1776 16.1 against 16.1,
+// 2016 17.2 against 16.3 (8 a row: 1024 13.6 against 16.6, 2048 18.9 against 17.5).  63 a row: 2142 16.4
+// against 17.8, 75 a row: 2175 16.2 against 18.2; the two kernels take longer there, a row being longer.
 bool verify_small(int N, int V) {
-  return N < kResThreads && static_cast<long long>(N + 1) * ((V + kVerifySlice - 1) / kVerifySlice) <= kVerifySmall;
+  const long long slices = (V + kVerifySlice - 1) / kVerifySlice;
+  return N < kResThreads && (N + 1) * slices <= (slices < 32 ? 1750 : 2200);
 }
 
 // After the completion counters, small calls: the slices' sums and maxima, the rows' picks and the

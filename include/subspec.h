@@ -526,9 +526,11 @@ int subspec_prefetch_release(subspec_prefetch* pf, long long ticket, hipStream_t
  * device's last captured graph is destroyed; both synchronise the device first.  A
  * call made after subspec_reserve(bytes) with a need of at most `bytes` neither
  * allocates, frees nor synchronises.  subspec_tree_attention_kv4 and subspec_tree_verify
- * use the same buffer; called while the caller captures the stream into a graph of its own,
- * they keep it allocated until the process ends, and replays of such graphs must not overlap
- * in time with each other or with other calls that use the workspace.
+ * use the same buffer.  Any of these calls, made while the caller captures the stream into a graph
+ * of its own, keeps the buffer that it uses allocated until the process ends (the library does not
+ * learn when that graph does; `retired` of subspec_workspace_info counts it once a larger one has
+ * replaced it), and replays of such graphs must not overlap in time with each other or with
+ * other calls that use the workspace.
  *
  * subspec_reserve: grow the calling device's workspace to at least `bytes` now
  * (synchronous; may call hipMalloc) and free retired buffers as above, so that later

@@ -706,21 +706,23 @@ int free_retired(Workspace& w) {
   return rc;
 }
 
+thread_local bool t_own_capture = false;  // this thread is inside subspec_stack_capture
+
 // Returns the device's workspace, grown to `bytes` if needed.  Growth allocates a new
 // buffer (at least twice the old size, so retired buffers total less than the live
 // one), zeroes its completion counters on `st` and waits for that stream only.  The
 // old buffer is retired, not freed: kernels queued on other streams and captured
-// graphs may still use it.  Growth is refused while `st` is being captured.  note_capture:
-// a call inside the caller's own stream capture keeps its buffer until the process ends (the
-// library never learns when that graph does).
-int get_workspace(size_t bytes, hipStream_t st, void** out, bool note_capture = false) {
+// graphs may still use it.  Growth is refused while `st` is being captured.  A call inside
+// the caller's own stream capture keeps its buffer until the process ends (the library never
+// learns when that graph does); subspec_stack_capture's graphs are counted instead.
+int get_workspace(size_t bytes, hipStream_t st, void** out) {
   int dev = 0;
   int rc = current_device(&dev);
   if (rc) return rc;
   std::lock_guard<std::mutex> lock(g_ws_mutex);
   Workspace& w = workspace_of(dev);
   if (w.bytes >= bytes) {
-    if (note_capture && !w.foreign && st != nullptr) {
+    if (!t_own_capture && !w.foreign && st != nullptr) {
       hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
       const hipError_t e = hipStreamIsCapturing(st, &cs);
       if (e != hipSuccess) return hip_fail(e, "hipStreamIsCapturing");
@@ -993,7 +995,9 @@ int subspec_stack_capture(const subspec_proj* projs, int nproj, int bits, int gr
   }
   hipError_t e = hipStreamBeginCapture(stream, hipStreamCaptureModeThreadLocal);
   if (e != hipSuccess) return hip_fail(e, "hipStreamBeginCapture");
+  t_own_capture = true;
   const int rc = subspec_stack_forward(projs, nproj, bits, group, M, stream);
+  t_own_capture = false;
   hipGraph_t graph = nullptr;
   e = hipStreamEndCapture(stream, &graph);
   if (rc) {
@@ -1288,7 +1292,7 @@ int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v
   a.rows_pad = 16 * ((Hq / Hkv * M + 15) / 16);
   if (a.splits > 1) {
     void* ws = nullptr;
-    const int rc = get_workspace(subspec::kv4_attn_workspace_bytes(M, Hq, Hkv, P, T), stream, &ws, true);
+    const int rc = get_workspace(subspec::kv4_attn_workspace_bytes(M, Hq, Hkv, P, T), stream, &ws);
     if (rc) return rc;
     // the partials go after the completion counters that other calls rely on being zero
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + subspec::kSplitCounterBytes);
@@ -1336,7 +1340,7 @@ int subspec_tree_verify(const void* logits, const int* parent, const int* token,
       !aligned_to(accepted, 4) || !aligned_to(next_token, 4))
     return fail(SUBSPEC_EINVAL, "tree_verify: tree, numbers and outputs must be 4-byte aligned");
   void* ws = nullptr;
-  const int rc = get_workspace(subspec::verify_workspace_bytes(N, V), stream, &ws, true);
+  const int rc = get_workspace(subspec::verify_workspace_bytes(N, V), stream, &ws);
   if (rc) return rc;
   subspec::VerifyArgs a{};
   a.logits = static_cast<const uint16_t*>(logits);

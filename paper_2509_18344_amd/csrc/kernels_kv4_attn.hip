@@ -151,13 +151,16 @@ __device__ __forceinline__ f16x8_t kv4_codes(uint32_t d) {
 // One load straight into LDS: lane l's SIZE bytes at base + offset (the lane's) land at byte
 // dst + SIZE * l.  Written as assembly because the compiler, where it sees such loads, waits for all
 // of them before it reads the ring again; it has no register result, and the ring's own waits order
-// it (a wait state after the write of m0 included).
+// it (a wait state after the write of m0 included).  m0 is named as written, for whatever the compiler may
+// keep there (it warns that m0 is not for it to allocate, which nothing asks of it).
 template <int SIZE>
 __device__ __forceinline__ void kv4_to_lds(const uint8_t* base, uint32_t offset, uint32_t dst) {
   if constexpr (SIZE == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base)
+                 : "memory", "m0");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(dst), "v"(offset), "s"(base)
+                 : "memory", "m0");
 }
 
 // The halves of a metadata word, two positions', of which bits 0 and 1 of `seen` say which stay; the

@@ -433,10 +433,10 @@ int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, i
  *            no mask row allows may hold anything
  *   mask     device uint32 [M][W], W = ceil((T + M) / 32), as subspec_tree_attention's
  *   out      device bf16 [M][Hq][128]; a query with no visible position gets zeros
- * Scores are fp32 sums over exact codes.  A position's weight, and its product with the value's
- * scale, are sums of two fp16 numbers in the second product, which sums in fp32: 21 bits each, or in
- * absolute terms 2^-28 of the heaviest weight times the largest scale of a value (of the weight alone
- * 2^(E - 33), 2^E at least 1 and at least that scale).  What positions hold that no query sees
+ * Scores are fp32 sums of exact products of codes.  A position's weight, and its product with the
+ * value's scale, are sums of two fp16 numbers in the second product, which sums in fp32: 21 bits each,
+ * or in absolute terms 2^-32 of the heaviest weight times the largest scale of a value (of the weight
+ * alone 2^(E - 33), 2^E at least 1 and at least that scale).  What positions hold that no query sees
  * changes no bit of the result.  Limits as subspec_tree_attention's (Hkv at most 65535, S a multiple of 32); q, caches and out
  * 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one where
  * a single range covers the positions); workspace as for subspec_qlinear

@@ -8,9 +8,9 @@
 // Neither product forms those numbers.  With x the sum over a group g of dimensions,
 //   q.k = sum_g s_g (q.c)_g + m_g (sum q)_g
 //   sum_j p_j v_j = sum_j (p_j s_jg) c_j + sum_j p_j m_jg
-// where q.c and (p s) c are fp16 matrix products that take the 4-bit codes as they lie: a code is the
-// mantissa of an fp16 subnormal, so unpacking a word of eight is four ands and a shift.  bf16 q fits
-// fp16 once its row is scaled by a power of two.  The sum of the weights and the minima's share come
+// where q.c and (p s) c are fp16 matrix products: a code as it lies is the mantissa of an fp16 subnormal,
+// so unpacking a word of eight is four ands, a shift and four packed products that make them normal
+// numbers.  bf16 q fits fp16 once its row is scaled by a power of two.  The sum of the weights and the minima's share come
 // from one more product against rows of ones and of minima, so that the numerator's and the
 // denominator's weights are the same numbers.
 //
@@ -139,13 +139,20 @@ __device__ __forceinline__ uint32_t kv4_pack(float lo, float hi) {
   return static_cast<uint32_t>(float_to_bf16_bits(lo)) | (static_cast<uint32_t>(float_to_bf16_bits(hi)) << 16);
 }
 
-// Eight codes of a word as fp16 numbers: a code is the mantissa of a subnormal, which the matrix
-// instruction takes as it is.  Codes 0, 1, 4 and 5 come as 2^-24 c and codes 2, 3, 6 and 7, left a
-// nibble higher, as 2^-20 c (two shifts fewer a word); the other operand is 2^-4 times as
-// large there.
+// Eight codes of a word as fp16 numbers 2^-9 c: a code is the mantissa of a subnormal, 2^-24 c or, left a
+// nibble higher, 2^-20 c (two shifts fewer a word), and a product makes it a normal number.  The matrix
+// instruction would take subnormals as they are, but it aligns a group of eight products by the exponents
+// of their operands, a subnormal's counting as 2^-14, and drops what lies 24 bits below the largest: of
+// that all but 14 bits would be the leading zeros of the codes, and a weight of 2^-14 of its
+// neighbour's, or a dimension of q beside a large one, was lost.
 __device__ __forceinline__ f16x8_t kv4_codes(uint32_t d) {
   const uint32_t low = 0x000F000Fu, high = 0x00F000F0u, e = d >> 8;
-  return __builtin_bit_cast(f16x8_t, u32x4_t{d & low, d & high, e & low, e & high});
+  const uint32_t w[4] = {d & low, d & high, e & low, e & high};
+  u32x4_t c;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    c[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, w[i]) * static_cast<_Float16>(i % 2 == 0 ? 0x1p15f : 0x1p11f));
+  return __builtin_bit_cast(f16x8_t, c);
 }
 
 // One load straight into LDS: lane l's SIZE bytes at base + offset (the lane's) land at byte
@@ -247,9 +254,8 @@ constexpr float kVast = 0x1p20f;
 template <int QW, int G>
 struct Kv4Rows {
   // Per lane the query row's fragments of q times 2^(15 - e), where the row's largest value
-  // lies below 2^e, as fp16 (bf16's 8 bits fit, down to 2^-25 of the largest; those that meet codes
-  // 16 times as large 2^-4 times that), their sums per group times 2^-24, and the factor that takes
-  // a score to log2.
+  // lies below 2^e, as fp16 (bf16's 8 bits fit, down to 2^-29 of the largest), their sums per group times
+  // 2^-9, and the factor that takes a score to log2.
   f16x8_t qf[QW][4];
   float qs[QW][G], factor[QW];
   bool live[QW];
@@ -288,21 +294,20 @@ struct Kv4Rows {
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int up = i % 2 == 0 ? 15 - e : 11 - e;  // codes 2, 3, 6 and 7 are 16 times as large
-          qf[t][j][2 * i] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] << 16), up));
-          qf[t][j][2 * i + 1] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] & 0xFFFF0000u), up));
+          qf[t][j][2 * i] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] << 16), 15 - e));
+          qf[t][j][2 * i + 1] = static_cast<_Float16>(ldexpf(__uint_as_float(raw[t][j][i] & 0xFFFF0000u), 15 - e));
         }
 #pragma unroll
       for (int gg = 0; gg < G; ++gg) {
-        float sum = 0.f, sum16 = 0.f;
+        float sum = 0.f;
 #pragma unroll
         for (int j = gg * (4 / G); j < (gg + 1) * (4 / G); ++j)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) (i / 2 % 2 == 0 ? sum : sum16) += static_cast<float>(qf[t][j][i]);
-        qs[t][gg] = kv4_cross_sum(__builtin_fmaf(16.f, sum16, sum)) * 0x1p-24f;
+          for (int i = 0; i < 8; ++i) sum += static_cast<float>(qf[t][j][i]);
+        qs[t][gg] = kv4_cross_sum(sum) * 0x1p-9f;
       }
-      // |x| stays below 2^16, so no score overflows; a factor of 2^110 has long left one position alone.
-      factor[t] = fminf(fmaxf(ldexpf(a.scale_log2, 9 + e), 0x1p-126f), 0x1p110f);
+      // |x| stays below 2^31, so no score overflows; a factor of 2^95 has long left one position alone.
+      factor[t] = fminf(fmaxf(ldexpf(a.scale_log2, e - 6), 0x1p-126f), 0x1p95f);
       ref[t] = -INFINITY;
       aux[t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -310,7 +315,7 @@ struct Kv4Rows {
     }
   }
 
-  // Scores times 2^-24: lane holds positions 16u + 4 quarter + e of its query.
+  // Scores times 2^(6 - e): lane holds positions 16u + 4 quarter + e of its query.
   __device__ __forceinline__ void scores(const Kv4Keys<G>& k, f32x4_t (&x)[QW][2]) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -431,16 +436,13 @@ struct Kv4Rows {
                                                              __builtin_fmaf(static_cast<float>(hi[1]), minus, w[1])}, f16x2_t);
           ps[t][0][2 * u + e / 2] = __builtin_bit_cast(uint32_t, hi);
           ps[t][1][2 * u + e / 2] = __builtin_bit_cast(uint32_t, lo);
-          // Times the scales, and 2^-4 where the codes are 16 times as large (positions 2 and 3 of each
-          // four).  The first product's rounding is exact in the fma that returns it, and goes to the second.
-          const _Float16 part = static_cast<_Float16>(e == 0 ? 1.f : 0.0625f);
-          const f16x2_t qh = hi * part, ql = lo * part;
+          // Times the scales: the first product's rounding, which an fma returns exactly, goes to the second.
 #pragma unroll
           for (int gg = 0; gg < G; ++gg) {
-            const f16x2_t c = sc[gg][2 * u + e / 2], h = qh * c;
+            const f16x2_t c = sc[gg][2 * u + e / 2], h = hi * c;
             pf[t][gg][0][2 * u + e / 2] = __builtin_bit_cast(uint32_t, h);
             pf[t][gg][1][2 * u + e / 2] =
-                __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(ql, c, __builtin_elementwise_fma(qh, c, -h)));
+                __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(lo, c, __builtin_elementwise_fma(hi, c, -h)));
           }
         }
     }
@@ -464,9 +466,9 @@ struct Kv4Rows {
     }
   }
 
-  // Codes back from 2^-24, scales from their raise, minima added.
+  // Codes back from 2^-9, scales from their raise, minima added.
   __device__ __forceinline__ void finish(int col) {
-    const float back = kv4_exp2i(10 + field);
+    const float back = kv4_exp2i(field - 5);
 #pragma unroll
     for (int t = 0; t < QW; ++t)
 #pragma unroll

@@ -165,3 +165,61 @@ def test_kv4_attention_rounds_once(M, Hq, Hkv, P, T, group):
     tol = _half_step(np.abs(ref) + err) + err
     off = np.abs(got - ref) > tol
     assert not off.any(), (int(off.sum()), off.size, float((np.abs(got - ref) / tol).max()))
+
+
+# --- products of very different sizes beside each other --------------------------------------------------
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("heads", [1, 4, 30, 64])
+def test_kv4_attention_keeps_light_weights_beside_a_heavy_one(heads, group):
+    """One position of every eight that a matrix product takes together is 2^12 times as heavy as the
+    others and 0 in most dimensions, though none of its codes is: what the others add there stands to
+    2^-19 of what the products sum over."""
+    M, P = 1, 31
+    n, S = P + M, 32
+    rng = np.random.default_rng([heads, group])
+    heavy = np.array([1, 5, 9, 13])
+    k, v = rng.standard_normal((n, 1, D)) * 0.05, rng.standard_normal((n, 1, D))
+    k[heavy] = 12 * math.log(2.0) / math.sqrt(D)  # against a query of ones
+    v[heavy] = 0.0
+    v[heavy, :, ::64], v[heavy, :, 1::64] = -1.0, 0.875  # minimum -1, scale 1 / 8: a 0 is code 8
+    q = _bf16(np.ones((M, heads, D)))
+    k, v = _bf16(k), _bf16(v)
+    mask = np.array([[1]], np.uint32)
+    got = _run(q, *_fill(k, v, S, group), mask, M, heads, 1, S, P, 0, group, SCALE)
+    kh, vh = _held(k, group), _held(v, group)
+    K, V = oracle.kv4_value(*kh), oracle.kv4_value(*vh)
+    zero = (V[heavy, 0] == 0).all(0)
+    assert zero.sum() == 124 and (vh[0][heavy][:, 0, zero] == 8).all()
+    ref, wabs = oracle.tree_attention_values(q, K, V, P, 0, mask, SCALE)
+    _, parts = oracle.tree_attention_values(q, K, _wide(vh[1], group) * vh[0] + np.abs(_wide(vh[2], group)), P, 0, mask, SCALE)
+    tol = _half_step(ref) + 2 * _score_error(q, kh, group)[..., None] * wabs + 2.0 ** -19 * parts
+    off = (np.abs(got - ref) > tol)[..., zero]
+    assert not off.any(), (int(off.sum()), off.size, float((np.abs(got - ref) / tol)[..., zero].max()))
+
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("M,P", [(1, 11), (6, 700)])
+def test_kv4_attention_keeps_small_dimensions_of_a_query_beside_a_large_one(M, P, group):
+    """One dimension of a query is thousands of times the others, and the keys agree in it (code 1):
+    scores differ by the others alone, and by the fp32 roundings of sums of that size."""
+    heads, n, S = min(28, 64 // M), P + M, (P + M + 31) // 32 * 32
+    rng = np.random.default_rng([M, P, group])
+    q = rng.standard_normal((M, heads, D)) * 3.0
+    q[..., 8::group] = 2.0 ** 13
+    k = rng.uniform(-1.0, 1.0, (n, 1, D))
+    k[..., 0::group], k[..., 1::group] = -1.0, 0.875  # minimum -1, scale 1 / 8
+    k[..., 8::group] = -0.875                       # code 1
+    v = rng.standard_normal((n, 1, D))
+    q, k, v = _bf16(q), _bf16(np.clip(k, -1.0, 0.875)), _bf16(v)
+    mask = rng.integers(0, 2 ** 32, (M, 1), dtype=np.uint64).astype(np.uint32)
+    got = _run(q, *_fill(k, v, S, group), mask, M, heads, 1, S, P, 0, group, SCALE)
+    kh, vh = _held(k, group), _held(v, group)
+    assert (kh[0][..., 8::group] == 1).all() and (_wide(kh[1], group) == 0.125).all()
+    ref, wabs = oracle.tree_attention_values(q, oracle.kv4_value(*kh), oracle.kv4_value(*vh), P, 0, mask, SCALE)
+    # sums of 16 groups of eight products and what precedes them, rounded once each; the minima's share, three times
+    qa = np.abs(oracle.bf16_bits_to_f64(q))
+    err = SCALE * (16 * 2.0 ** -24 * (qa @ (0.125 * kh[0][:, 0]).T).max(-1) + 3 * 2.0 ** -24 * qa.sum(-1))[..., None]
+    tol = _half_step(np.abs(ref) + 2 * err * wabs) + (2 * err + 2.0 ** -17) * 3 * wabs
+    off = np.abs(got - ref) > tol
+    assert not off.any(), (int(off.sum()), off.size, float((np.abs(got - ref) / tol).max()))

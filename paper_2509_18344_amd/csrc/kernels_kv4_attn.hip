@@ -500,7 +500,7 @@ constexpr int kKv4WaitLds = 15 | (7 << 4) | (3 << 14);  // no LDS operation outs
 //
 // RING: a wavefront's tiles go from memory into a ring of four in LDS of its own (no register is
 // held by a load in flight, so three tiles are, 14 KB a wavefront); otherwise into registers, for
-// ranges of a tile or two per wavefront, which a ring could not get ahead of.
+// ranges of few tiles per wavefront, which a ring could not get ahead of (kv4_shape has the line).
 template <int QW, int QG, int G, bool RING>
 __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(2))) void k_kv4_partial(Kv4AttnArgs a) {
   constexpr int KW = kWaves / QG;  // tiles of positions at a time
@@ -800,14 +800,18 @@ struct Kv4Shape {
 };
 
 // A range has a workgroup, and there are as many as CUs (16385 positions of eight heads with 5 rows
-// 9.9 us; with ranges of whole turns of a workgroup's wavefronts, 171 workgroups, 10.4), but no
-// wavefront goes without a tile.
-// Up to kAlone tiles a wavefront one workgroup takes a whole head, and the second kernel is saved (300
-// positions of four heads 7.3 us a call against 10.0, 800 8.7 against 9.9; at five tiles 9.8 either way).
-// From kRingFrom tiles on the ring in LDS gets ahead of its wavefront (131138 positions of eight heads, 17
-// tiles: 42.6 us against 47.8 from registers, and with one query tile a wavefront 51.1; at three
-// tiles 11.3 against 9.9), and two query tiles a wavefront share the unpacking.
-constexpr int kAlone = 4, kRingFrom = 5;
+// 11.0 us; with ranges of whole turns of a workgroup's wavefronts, 171 workgroups, 11.7; 8407 with 64
+// rows 18.0 against 19.3), but no wavefront goes without a tile.
+// Up to three and a half tiles a wavefront one workgroup takes a whole head, and the second kernel is
+// saved (four heads of 7 rows: 20 tiles 7.8 us a call against 10.0, 28 9.2 against 10.0, 32 10.3 against
+// 9.9; of 21 rows, four wavefronts side by side: 12 9.2 against 9.9, 14 9.8 against 9.7).
+// Two query tiles a wavefront share the unpacking, and from kRingFrom tiles on the ring in LDS gets ahead
+// of it (five tiles: 20 rows a head 24.3 us against 24.4 with one query tile from registers, 64 rows 24.3
+// against 25.5; 131138 positions of eight heads with 30 rows, 17 tiles, 49.7 against 65.7, and 60.0 in a
+// ring with one query tile).  One query tile a wavefront is faster from registers up to kRingFromOne (5 rows,
+// five tiles 15.4 against 17.6, eight 19.9 against 21.4, ten 24.0 both, twelve 28.0 against 27.4).
+constexpr int kRingFrom = 5, kRingFromOne = 9;
+static_assert(kRingFromOne - 1 >= 2 * (kRingFrom - 1), "a ring of one query tile only where no wavefronts share positions");
 
 Kv4Shape kv4_shape(int M, int Hq, int Hkv, int P, int T) {
   const int tiles = (P + T + M + kKv4Tile - 1) / kKv4Tile;
@@ -817,8 +821,8 @@ Kv4Shape kv4_shape(int M, int Hq, int Hkv, int P, int T) {
     const int qg = qt <= qw ? 1 : qt <= 2 * qw ? 2 : 4;
     const int at_once = kWaves / qg;
     int tiles_a_split = std::max((tiles + ranges - 1) / ranges, at_once);
-    if (tiles <= kAlone * at_once) tiles_a_split = tiles;
-    return Kv4Shape{qw, qg, tiles_a_split, (tiles_a_split + at_once - 1) / at_once >= kRingFrom};
+    if (2 * tiles <= 7 * at_once) tiles_a_split = tiles;
+    return Kv4Shape{qw, qg, tiles_a_split, (tiles_a_split + at_once - 1) / at_once >= (qw == 2 ? kRingFrom : kRingFromOne)};
   };
   if (qt > 1) {
     const Kv4Shape wide = cut(2);
@@ -834,14 +838,6 @@ void launch_shape(const Kv4AttnArgs& a, int groups, hipStream_t st) {
     hipLaunchKernelGGL((k_kv4_partial<QW, QG, 1, RING>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((k_kv4_partial<QW, QG, 2, RING>), grid, block, 0, st, a);
-}
-
-template <int QG>
-void launch_narrow(const Kv4AttnArgs& a, int groups, bool ring, hipStream_t st) {
-  if (ring)
-    launch_shape<1, QG, true>(a, groups, st);
-  else
-    launch_shape<1, QG, false>(a, groups, st);
 }
 
 }  // namespace
@@ -869,12 +865,14 @@ hipError_t launch_kv4_attention(const Kv4AttnArgs& a, int groups, hipStream_t st
     launch_shape<2, 1, true>(a, groups, st);
   else if (sh.qw == 2)
     launch_shape<2, 2, true>(a, groups, st);
+  else if (sh.ring)
+    launch_shape<1, 1, true>(a, groups, st);
   else if (sh.qg == 1)
-    launch_narrow<1>(a, groups, sh.ring, st);
+    launch_shape<1, 1, false>(a, groups, st);
   else if (sh.qg == 2)
-    launch_narrow<2>(a, groups, sh.ring, st);
+    launch_shape<1, 2, false>(a, groups, st);
   else
-    launch_narrow<4>(a, groups, sh.ring, st);
+    launch_shape<1, 4, false>(a, groups, st);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   hipLaunchKernelGGL(k_kv4_combine, dim3(a.Hq, a.M), dim3(kCombineThreads), 0, st, a);

@@ -39,7 +39,7 @@ def kernels(tmp_path_factory):
                     key = (*(int(v) for v in re.findall(r"Li(\d+)E", m.group(1))), "Lb1E" in m.group(1))
             elif key and line.split():
                 found.setdefault(key, []).append(line.split("//")[0].split())
-    assert len(found) == 16, sorted(found)
+    assert len(found) == 12, sorted(found)
     return found
 
 

@@ -11,7 +11,7 @@ import oracle
 import paper_2509_18344_amd as ss
 from paper_2509_18344_amd import synth
 from oracle.tree_attn import visible_positions
-from test_gpu_kv4_attn import _bf16, _fill, _held, _run
+from test_gpu_kv4_attn import _bf16, _check, _fill, _held, _run
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -44,7 +44,8 @@ LARGE = [
     (6, 28, 4, 100, 42),    # a workgroup takes a head whole
     (6, 28, 4, 2048, 60),   # ranges, tiles in registers
     (8, 16, 2, 3000, 90),   # 64 rows a head
-    (1, 128, 128, 2500, 0),   # five tiles a wavefront and more, in a ring
+    (1, 128, 128, 2500, 0),   # five tiles a wavefront
+    (1, 128, 128, 5000, 0),   # ten, in a ring
     (6, 64, 32, 5000, 20),
 ]
 
@@ -223,3 +224,15 @@ def test_kv4_attention_keeps_small_dimensions_of_a_query_beside_a_large_one(M, P
     tol = _half_step(np.abs(ref) + 2 * err * wabs) + (2 * err + 2.0 ** -17) * 3 * wabs
     off = np.abs(got - ref) > tol
     assert not off.any(), (int(off.sum()), off.size, float((np.abs(got - ref) / tol).max()))
+
+
+# --- one query tile in a ring -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("group", [64, 128])
+@pytest.mark.parametrize("M,Hq,Hkv,P,T,q_scale", [(1, 128, 128, 5000, 0, 1.0), (1, 64, 64, 9300, 40, 2.0), (5, 96, 48, 15000, 33, 1.0),
+                                                  (16, 64, 64, 9500, 90, 1.5)])
+def test_kv4_attention_of_few_rows_over_many_tiles(M, Hq, Hkv, P, T, q_scale, group):
+    """Up to 16 rows a head and nine tiles a wavefront and more."""
+    splits, tiles = ss.subspec_tree_attention_kv4_plan(M, Hq, Hkv, P, T)
+    assert splits > 1 and -(-tiles // 8) >= 9
+    _check(M, Hq, Hkv, P, T, group, P + T, q_scale=q_scale, what=f"M={M} Hkv={Hkv} P={P} group={group}")

@@ -188,7 +188,7 @@ __device__ __forceinline__ bool last_to_arrive(unsigned* cnt, unsigned of, int* 
 // Token j continues `row` (a parent p that does not come before it, or a token k outside the
 // vocabulary, continues nothing).
 __device__ __forceinline__ bool continues(const VerifyArgs& a, int j, int p, int k, int row) {
-  return p + 1 == row && p >= -1 && p < j && k >= 0 && k < a.V;
+  return p >= -1 && p < j && p + 1 == row && k >= 0 && k < a.V;
 }
 
 struct Children {

@@ -6,8 +6,8 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
-from itertools import compress
-from operator import ge
+from itertools import compress, repeat
+from operator import ge, is_not
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_NAME = "libsubspec.so"
@@ -156,6 +156,7 @@ _get_device = _is_contiguous = _data_ptr = _dtype = _numel = None
 # of its size with their bits.
 _TYPES = {"bf16": ("bfloat16", "int16", "uint16"), "i32": ("int32", "uint32"), "f32": ("float32",),
           "f64": ("float64",), "u8": ("uint8", "int8")}
+_NONE = repeat(None)
 _usual = {}  # a call's kinds -> the first torch type of each
 
 
@@ -167,20 +168,19 @@ def _device_args(fn: str, stream, kinds, needs, *args):
     over the tensors: a method call each is most of the binding's time at a few microseconds a kernel."""
     global _get_device, _is_contiguous, _data_ptr, _dtype, _numel
     if stream is None and _get_device is not None:
-        given = [t for t in args if t is not None]
-        types, least = _usual.get(kinds) or _usual_types(kinds), needs
-        if len(given) < len(args):
-            there = [t is not None for t in args]
-            types, least = [*compress(types, there)], compress(needs, there)
+        there = [*map(is_not, args, _NONE)]
+        given, types, least = args, _usual.get(kinds) or _usual_types(kinds), needs
+        if not all(there):
+            given, types, least = [*compress(args, there)], [*compress(types, there)], compress(needs, there)
         try:
             on = {*map(_get_device, given)}
             dev = on.pop() if on else -1
             if (not on and dev >= 0 and dev == _device() and all(map(_is_contiguous, given)) and
                     [*map(_dtype, given)] == types and all(map(ge, map(_numel, given), least))):
                 ptr = map(_data_ptr, given)
-                if len(given) == len(args):
+                if given is args:
                     return [_raw_stream(dev), *ptr]
-                return [_raw_stream(dev), *[None if t is None else next(ptr) for t in args]]
+                return [_raw_stream(dev), *[next(ptr) if t else None for t in there]]
         except TypeError:  # addresses among them
             pass
     dev, out = _current_device(stream), []

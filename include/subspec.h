@@ -357,7 +357,9 @@ int subspec_tree_attention_plan(int M, int Hq, int Hkv, int P, int T, int* split
  *     query and key heads, where their weight is given: x <- x / sqrt(mean(x^2) + eps) * weight;
  *     query and key heads, pairs (a, b) of the first `rot` dimensions, pair p < rot / 2:
  *         (a cos t - b sin t, b cos t + a sin t),  t = positions[i] * inv_freq[p],
- * all in fp32 (the angle in fp64) and rounded once to bf16.  Value heads get the bias alone.
+ * all in fp32 (the angle in fp64; a norm's mean square has to lie in fp32's range) and rounded once to
+ * bf16.  Dimensions from `rot` on are not rotated and come through as they are.  Value heads get the
+ * bias alone.
  *   qkv        device bf16 [M][ld]: Hq query heads, then Hkv key heads, then Hkv value
  *              heads of 128; ld >= (Hq + 2 Hkv) * 128, a multiple of 8
  *   bias       device bf16 [(Hq + 2 Hkv) * 128], or null
@@ -437,9 +439,10 @@ int subspec_kv4_read(const void* k_cache, const void* v_cache, int Hkv, int S, i
  * value's scale, are sums of two fp16 numbers in the second product, which sums in fp32: 21 bits each,
  * or in absolute terms 2^-32 of the heaviest weight times the largest scale of a value (of the weight
  * alone 2^(E - 33), 2^E at least 1 and at least that scale).  What positions hold that no query sees
- * changes no bit of the result.  Limits as subspec_tree_attention's (Hkv at most 65535, S a multiple of 32); q, caches and out
- * 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one where
- * a single range covers the positions); workspace as for subspec_qlinear
+ * changes no bit of the result.  Limits as subspec_tree_attention's: (Hq / Hkv) * M <= 64 (a target's
+ * pass over a larger tree, or a prompt, takes several calls), Hkv at most 65535, S a multiple of 32; q,
+ * caches and out 16-byte aligned, mask 4-byte; out must not overlap the inputs.  Two kernels (one
+ * where a single range covers the positions); workspace as for subspec_qlinear
  * (subspec_tree_attention_kv4_workspace_bytes). */
 int subspec_tree_attention_kv4(const void* q, const void* k_cache, const void* v_cache,
                                const uint32_t* mask, int M, int Hq, int Hkv, int S, int P, int T,

@@ -7,7 +7,8 @@
 //
 // Measured, 16384 positions of 8 heads in groups of 128: append 22.7 us for 67 MB read and 18 written,
 // 3.7 TB/s, issuing vector instructions 70 % of the time (455 a wavefront, 95 of them for a lane's 8
-// values); read 15.5 us for the same bytes, 5.5 TB/s, as a large copy: bound by memory.  A few rows
+// values), with no load in flight while a workgroup quantizes and turns its tile; read 15.5 us for the
+// same bytes, 5.5 TB/s, as a large copy: bound by memory.  A few rows
 // 3.9 and 3.4 us, the launch and one chain of loads.
 #include "kv4_device.h"
 

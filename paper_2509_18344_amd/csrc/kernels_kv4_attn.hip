@@ -10,15 +10,14 @@
 //   sum_j p_j v_j = sum_j (p_j s_jg) c_j + sum_j p_j m_jg
 // where q.c and (p s) c are fp16 matrix products: a code in a byte is an fp8 number, so unpacking a word
 // of eight is two ands, a shift and four conversions.  bf16 q fits fp16 once its row is scaled by a power
-// of two.  The sum of the weights and the minima's share come
-// from one more product against rows of ones and of minima, so that the numerator's and the
-// denominator's weights are the same numbers.
+// of two.  The sum of the weights and the minima's share come from one more product against rows of
+// ones and of minima, so that the numerator's and the denominator's weights are the same numbers.
 //
 // A weight p, and its product with the scale, go into the products as sums of two fp16 numbers each:
 // the number rounded and what the rounding left (of the product an fma returns it exactly), 21 bits
-// and more.  One number each costs 13 % less at 131138 positions (42.8 us against 48.2) and 1 to 4 %
-// at a few thousand, but is off by 2^-11 twice, which 5 to 9 % of outputs show in their last bit where
-// values cancel.
+// and more.  With one number each and the codes left as subnormals a call at 131138 positions took 42.8 us
+// instead of 49.4 and one at 2336 10.8 instead of 11.0, but 8 to 24 % of the outputs were not the bf16
+// number next to the exact one, where now 0.1 to 0.2 % are not, as of a plain form in 32 bits.
 // Everything else is exact or in 32 bits.  fp16 spans 2^-24 .. 65504, so weights are
 // relative to a reference that covers score + log2 of the tile's largest scale where that passes 1: p
 // and p s stay below 2^15, and the heaviest position's p is at least 2^8 while scales lie below 1.
@@ -40,12 +39,12 @@
 // output itself.
 //
 // Measured (a call, both kernels): 131138 positions of 8 heads in groups of 64, 30 query rows a head:
-// 151 MB of cache in 40 us, 3.8 TB/s.  The first kernel takes 37 us, 28 with nothing but its loads:
-// unpacking, softmax and products bound it (vector ALUs busy two thirds of the time).  8407
-// positions of 8 heads in groups of 128, 64 rows a head: 9 MB in 16.6 us, a chain of the launch with
-// the first loads (3.4 us), four or five tiles a wavefront (1.2 to 2 each), the merge (1 to 2.5) and the
-// second kernel (2.5 to 3.3).  2336 positions of 4 heads, 42 rows: 10.3 us, the same chain with one
-// tile; 16385 of 8 heads with 5 rows 9.9 us.
+// 151 MB of cache in 49.4 us, 3.1 TB/s.  The first kernel takes 46 to 49 us, 28 with nothing but its loads:
+// unpacking, softmax and products bound it (508 vector instructions a tile of 32 positions x 32 query rows, 52 of
+// them matrix products; the vector ALUs issue two thirds of the time).  8407 positions of 8 heads in groups of
+// 128, 64 rows a head: 9 MB in 17.8 us, a chain of the launch with the first loads (3.4 us), five tiles a
+// wavefront, the merge (1 to 2.5) and the second kernel (2.5 to 3.3).  2336 positions of 4 heads, 42 rows:
+// 10.9 us, the same chain with one tile; 16385 of 8 heads with 5 rows 11.0 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

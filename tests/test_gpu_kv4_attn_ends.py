@@ -61,6 +61,8 @@ def test_kv4_attention_of_very_large_scores_is_the_largest_ones_value(M, Hq, Hkv
     q = _bf16(rng.standard_normal((M, Hq, D)) * q_size)
     own = min(Hkv, 2)
     k, v = rng.standard_normal((n, own, D)) * k_size, rng.standard_normal((n, own, D)) + 0.5
+    if q_size in (1e5, 1e30):
+        v *= 2.0 ** 11  # value scales far above 1
     k, v = (_bf16(a)[:, np.arange(Hkv) % own] for a in (k, v))
     mask = synth.tree_levels_mask(T, 6, M, 5)
     got = _run(q, *_fill(k, v, S, group), mask, M, Hq, Hkv, S, P, T, group, SCALE)
@@ -113,15 +115,18 @@ def test_kv4_attention_of_equal_large_scores_is_their_values_mean(M, Hq, Hkv, P,
 
 @pytest.mark.parametrize("size", [0, -6, -9, -12, -16])
 @pytest.mark.parametrize("group", [64, 128])
-@pytest.mark.parametrize("M,Hq,Hkv,P", [(1, 128, 128, 20000), (6, 384, 128, 9000), (6, 28, 4, 20000), (8, 16, 2, 200)])
-def test_kv4_attention_keeps_small_values_beside_heavy_positions(M, Hq, Hkv, P, group, size):
-    """Every wavefront meets a position 2^20 times as heavy as the others, whose value is 0: the output is
-    the others' share alone.  Its error is bounded relative to the values, whatever their size: 2^-11 for
+@pytest.mark.parametrize("M,Hq,Hkv,P,each", [(1, 128, 128, 20000, True), (6, 384, 128, 9000, True), (6, 28, 4, 20000, True),
+                                             (8, 16, 2, 200, True), (6, 40, 8, 40000, True), (6, 40, 8, 40000, False),
+                                             (1, 8, 8, 90000, False)])
+def test_kv4_attention_keeps_small_values_beside_heavy_positions(M, Hq, Hkv, P, each, group, size):
+    """Every wavefront (or one) meets a position 2^20 times as heavy as the others, whose value is 0: the
+    output is the others' share alone.  Its error is bounded relative to the values, whatever their size: 2^-11 for
     each of three roundings of a weight (with its scale and without), nothing absolute."""
     n, S = P + M, (P + M + 31) // 32 * 32
     rng = np.random.default_rng([M, Hkv, P, -size])
     splits, tiles = ss.subspec_tree_attention_kv4_plan(M, Hq, Hkv, P, 0)
     heavy = np.array([32 * (s * tiles + t) + 7 for s in range(splits) for t in range(min(8, tiles)) if 32 * (s * tiles + t) + 7 < P])
+    heavy = heavy if each else heavy[len(heavy) // 2:][:1]
     k, v = rng.standard_normal((n, 1, D)) * 0.05, (rng.standard_normal((n, 1, D)) + 0.5) * 2.0 ** size
     k[heavy] = 20 * math.log(2.0) / math.sqrt(D)  # against a query of ones
     v[heavy] = 0.0

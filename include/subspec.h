@@ -54,7 +54,9 @@
  * Sec. 4.3 and App. E), the preparation of queries and keys in front of the attention
  * (subspec_qkv_rope), a key/value cache held in 4 bits (subspec_kv4_*) with the tree
  * attention over it (subspec_tree_attention_kv4*), the verification of the drafted tree
- * (subspec_tree_verify*) and the quantizer with an HQQ-style optimised zero-point
+ * (subspec_tree_verify*), the row operators between two projections (subspec_add_norm,
+ * subspec_silu_mul), the product in 8-bit floating point (subspec_fp8_*) and the quantizer
+ * with an HQQ-style optimised zero-point
  * (subspec_quantize_hqq, Sec. 4.1 and 5.1).  The shape limits listed above are the
  * substitute linear's; the other calls state theirs.
  */
@@ -489,6 +491,80 @@ int subspec_tree_verify(const void* logits, const int* parent, const int* token,
 /* Workspace bytes subspec_tree_verify needs for (N, V); 0 on bad arguments. */
 size_t subspec_tree_verify_workspace_bytes(int N, int V);
 
+/* 8-bit rows, the activations and weights of subspec_fp8_linear.  Every row falls into blocks of 128
+ * values with one power of two each: e is the smallest whole number >= -126 with max |x| <= 448 * 2^e
+ * (the largest finite magnitude of the block), and a value's code is x * 2^-e as e4m3 (OCP: 4 exponent
+ * bits, bias 7, largest 448), rounded once to nearest even; infinities and NaN become NaN.  A code c
+ * stands for c * 2^e.
+ *   codes    uint8 [rows][K] row-major
+ *   scales   uint32 [ceil(K / 512)][rows]: byte j (of rising significance) of word [g][r] is e + 127 of
+ *            block 4 g + j of row r, 1 .. 254; bytes past the last block are neither written nor used
+ * (A power of two and not a number of 32 bits: codes float, so a scale's mantissa would move only what
+ * lies at the subnormal end, and the matrix instruction takes such bytes as operands.)
+ *
+ * Weight tiles: the codes of 16 rows x 128 k of a weight [N][K] in the order in which a wavefront reads
+ * them.  Tile (nt, kb) starts at byte 2048 (nt (K / 128) + kb); the code of row n = 16 nt + i and
+ * k = 128 kb + 64 h + 16 q + j (i, j < 16, h < 2, q < 4) is its byte 1024 h + 256 q + 16 i + j.  N * K
+ * bytes in all; the scales stay as they are. */
+
+/* Rows of bf16 as 8-bit rows.  x: device bf16 [M][K]; codes, scales: device, written.  Needs
+ * 1 <= M <= 2^20, K a positive multiple of 128 up to 2^24, M * K <= 2^40; 16-byte alignment (scales 4).
+ * One kernel. */
+int subspec_fp8_rows(const void* x, int M, int K, void* codes, uint32_t* scales, hipStream_t stream);
+
+/* The values that 8-bit rows stand for, rounded to bf16.  y: device bf16 [M][K], written.  Same limits. */
+int subspec_fp8_read(const void* codes, const uint32_t* scales, int M, int K, void* y, hipStream_t stream);
+
+/* Codes [N][K] of a weight (subspec_fp8_rows of its rows) as weight tiles.  tiles: device, N * K bytes,
+ * written, not the codes' own memory.  Needs N a positive multiple of 16, K a positive multiple of 128 up
+ * to 2^24, N * K <= 2^40; 16-byte alignment. */
+int subspec_fp8_pack(const void* codes, int N, int K, void* tiles, hipStream_t stream);
+
+/* y = x w^T, both in 8-bit rows:
+ *   y[m][n] = sum_k x[m][k] w[n][k]
+ * of the values that the codes stand for, rounded once to bf16.  The matrix units add in fp32, but for the
+ * products of eight neighbouring k (8 i .. 8 i + 7): those are cut towards zero to multiples of 2^-13 of the
+ * largest one's power of two before they are added (found on the card; every 8-bit matrix instruction of it
+ * does so).  A NaN code makes NaN of what it reaches.
+ *   x        device: codes uint8 [M][K] with x_scales; or, x_scales null, bf16 [M][K], which the call
+ *            turns into 8-bit rows itself (exactly subspec_fp8_rows)
+ *   x_scales device uint32 [ceil(K / 512)][M], or null
+ *   w        device: weight tiles (subspec_fp8_pack), w_scales device uint32 [ceil(K / 512)][N]
+ *   y        device bf16 [M][N], fully overwritten
+ * Needs 1 <= M <= 2^20, K a positive multiple of 128 up to 2^24, N a positive multiple of 16 up to 2^24,
+ * M * K, N * K and M * N at most 2^40; 16-byte alignment (scales 4); y must not overlap the inputs.  Equal
+ * calls give equal bits.  Workspace as for subspec_qlinear (subspec_fp8_linear_workspace_bytes). */
+int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M,
+                       int N, int K, void* y, hipStream_t stream);
+
+/* Workspace bytes subspec_fp8_linear needs, with x as 8-bit rows (rows8 = 1) or bf16 (0); 0 on bad
+ * arguments, and where it needs none. */
+size_t subspec_fp8_linear_workspace_bytes(int M, int N, int K, int rows8);
+
+/* What stands between two projections of a layer.  The residual's addition and the RMS norm of M rows:
+ *     s = x + residual;   y = s / sqrt(mean(s^2) + eps) * weight
+ * in fp32 (s has to lie in its range; its squares need not), each output rounded once.
+ *   x         device bf16 [M][K]
+ *   residual  device bf16 [M][K], or null (s = x)
+ *   weight    device bf16 [K]
+ *   sum       device bf16 [M][K]: s, the next residual; or null.  May be x or residual itself
+ *   y         device bf16 [M][K], or null.  May be x or residual itself, where sum is not
+ *   codes, scales  y as 8-bit rows (of the fp32 values), or both null; one of y and codes is needed
+ * Needs 1 <= M <= 2^20, K a positive multiple of 8 (of 128 with codes) up to 65536, finite eps >= 0;
+ * 16-byte alignment (scales 4); apart from what is named above outputs must not overlap inputs or each
+ * other.  One kernel, no workspace. */
+int subspec_add_norm(const void* x, const void* residual, const void* weight, float eps, int M, int K, void* sum,
+                     void* y, void* codes, uint32_t* scales, hipStream_t stream);
+
+/* The gated activation between gate|up and down: h = g / (1 + exp(-g)) * u for the rows g | u of a fused
+ * projection, in fp32, each output rounded once.
+ *   gate_up   device bf16 [M][2 I]: I gate values, then I up values
+ *   h         device bf16 [M][I], or null
+ *   codes, scales  h as 8-bit rows (of the fp32 values), or both null; one of h and codes is needed
+ * Needs 1 <= M <= 2^20, I a positive multiple of 8 (of 128 with codes) up to 2^23; 16-byte alignment
+ * (scales 4); outputs must not overlap inputs or each other.  One kernel, no workspace. */
+int subspec_silu_mul(const void* gate_up, int M, int I, void* h, void* codes, uint32_t* scales, hipStream_t stream);
+
 /* Cross-layer asynchronous weight prefetch for the verification pass (SubSpec
  * Sec. 4.3 "Asynchronous Data Transfer", App. E): while the GPU computes with one
  * offloaded tensor, the next ones are copied from pinned host memory into a fixed
@@ -528,8 +604,8 @@ int subspec_prefetch_release(subspec_prefetch* pf, long long ticket, hipStream_t
  * subspec_reserve while no captured graph is alive on the device, and when the
  * device's last captured graph is destroyed; both synchronise the device first.  A
  * call made after subspec_reserve(bytes) with a need of at most `bytes` neither
- * allocates, frees nor synchronises.  subspec_tree_attention_kv4 and subspec_tree_verify
- * use the same buffer.  Any of these calls, made while the caller captures the stream into a graph
+ * allocates, frees nor synchronises.  subspec_tree_attention_kv4, subspec_tree_verify and
+ * subspec_fp8_linear use the same buffer.  Any of these calls, made while the caller captures the stream into a graph
  * of its own, keeps the buffer that it uses allocated until the process ends (the library does not
  * learn when that graph does; `retired` of subspec_workspace_info counts it once a larger one has
  * replaced it), and replays of such graphs must not overlap in time with each other or with

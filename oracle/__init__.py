@@ -2,7 +2,8 @@
 and for the draft-tree expansion step with probability sharpening (Sec. 4.2, App. D)
 and the draft model's tree attention over the shared KV cache (Sec. 4.1), and for the
 quantizer with an HQQ-style optimised zero-point (Sec. 4.1, Sec. 5.1), the preparation of
-queries and keys, the key/value cache held in 4 bits and the verification of a drafted tree.
+queries and keys, the key/value cache held in 4 bits, the verification of a drafted tree, 8-bit rows
+and their product, and the row operators between two projections.
 
 TEST INFRASTRUCTURE ONLY.  Only ``tests/``, ``__graft_entry__.smoke()`` and the
 ``cpu_baseline`` leg of ``bench.py`` may import or call anything in this package.
@@ -54,4 +55,15 @@ from .kv4 import (  # noqa: F401
 from .verify import (  # noqa: F401
     tree_children,
     tree_verify,
+)
+from .fp8 import (  # noqa: F401
+    E4M3,
+    e4m3_code,
+    fp8_rows,
+    fp8_values,
+    scale_bytes,
+    scale_words,
+    weight_tiles,
+    add_norm,
+    silu_mul,
 )

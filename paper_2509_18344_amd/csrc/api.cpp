@@ -19,6 +19,7 @@
 #include "kernels.h"
 #include "kernels_tree.h"
 #include "kernels_attn.h"
+#include "kernels_fp8.h"
 #include "kernels_hqq.h"
 #include "kernels_qstream.h"
 #include "kernels_rope.h"
@@ -1359,6 +1360,155 @@ int subspec_tree_verify(const void* logits, const int* parent, const int* token,
   a.next_token = next_token;
   const hipError_t e = subspec::launch_tree_verify(a, stream);
   if (e != hipSuccess) return hip_fail(e, "tree_verify launch");
+  return SUBSPEC_OK;
+}
+
+namespace {
+
+constexpr long long kMostElements = 1ll << 40;
+
+// Limits that every call on 8-bit rows shares; `K` under its caller's name.
+int rows_check(const char* fn, const char* name, int M, int K, int step, int most) {
+  if (M < 1 || M > (1 << 20)) return fail(SUBSPEC_EUNSUPPORTED, "%s: M=%d: must be in 1..2^20", fn, M);
+  if (K < 1 || K > most || K % step)
+    return fail(SUBSPEC_EUNSUPPORTED, "%s: %s=%d: must be a multiple of %d in %d..%d", fn, name, K, step, step, most);
+  if (static_cast<long long>(M) * K > kMostElements) return fail(SUBSPEC_EUNSUPPORTED, "%s: M * %s exceeds 2^40", fn, name);
+  return SUBSPEC_OK;
+}
+
+int outputs_check(const char* fn, const void* y, const void* codes, const void* scales) {
+  if (!codes != !scales) return fail(SUBSPEC_EINVAL, "%s: codes and scales belong together", fn);
+  if (!y && !codes) return fail(SUBSPEC_EINVAL, "%s: no output", fn);
+  if (!aligned16(y) || !aligned16(codes) || !aligned_to(scales, 4))
+    return fail(SUBSPEC_EINVAL, "%s: outputs must be 16-byte and scales 4-byte aligned", fn);
+  return SUBSPEC_OK;
+}
+
+int fp8_weight_check(const char* fn, int N, int K) {
+  if (N < 1 || N > (1 << 24) || N % 16) return fail(SUBSPEC_EUNSUPPORTED, "%s: N=%d: must be a multiple of 16 in 16..2^24", fn, N);
+  if (K < 1 || K > (1 << 24) || K % 128) return fail(SUBSPEC_EUNSUPPORTED, "%s: K=%d: must be a multiple of 128 in 128..2^24", fn, K);
+  if (static_cast<long long>(N) * K > kMostElements) return fail(SUBSPEC_EUNSUPPORTED, "%s: N * K exceeds 2^40", fn);
+  return SUBSPEC_OK;
+}
+
+int fp8_linear_check(int M, int N, int K) {
+  int rc = rows_check("fp8_linear", "K", M, K, 128, 1 << 24);
+  if (!rc) rc = fp8_weight_check("fp8_linear", N, K);
+  if (!rc && static_cast<long long>(M) * N > kMostElements) rc = fail(SUBSPEC_EUNSUPPORTED, "fp8_linear: M * N exceeds 2^40");
+  return rc;
+}
+
+}  // namespace
+
+int subspec_add_norm(const void* x, const void* residual, const void* weight, float eps, int M, int K, void* sum, void* y,
+                     void* codes, uint32_t* scales, hipStream_t stream) {
+  if (!x || !weight) return fail(SUBSPEC_EINVAL, "add_norm: null pointer argument");
+  if (!aligned16(x) || !aligned16(residual) || !aligned16(weight) || !aligned16(sum))
+    return fail(SUBSPEC_EINVAL, "add_norm: rows, weight and sum must be 16-byte aligned");
+  int rc = outputs_check("add_norm", y, codes, scales);
+  if (rc) return rc;
+  if (sum && sum == y) return fail(SUBSPEC_EINVAL, "add_norm: sum and y must not be the same");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SUBSPEC_EINVAL, "add_norm: eps must be finite and not negative");
+  rc = rows_check("add_norm", "K", M, K, codes ? 128 : 8, subspec::kNormMostK);
+  if (rc) return rc;
+  subspec::NormArgs a{};
+  a.x = static_cast<const uint16_t*>(x);
+  a.residual = static_cast<const uint16_t*>(residual);
+  a.weight = static_cast<const uint16_t*>(weight);
+  a.eps = eps;
+  a.M = M;
+  a.K = K;
+  a.sum = static_cast<uint16_t*>(sum);
+  a.y = static_cast<uint16_t*>(y);
+  a.codes = static_cast<uint8_t*>(codes);
+  a.scales = reinterpret_cast<uint8_t*>(scales);
+  const hipError_t e = subspec::launch_add_norm(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "add_norm launch");
+  return SUBSPEC_OK;
+}
+
+int subspec_silu_mul(const void* gate_up, int M, int I, void* h, void* codes, uint32_t* scales, hipStream_t stream) {
+  if (!gate_up) return fail(SUBSPEC_EINVAL, "silu_mul: null pointer argument");
+  if (!aligned16(gate_up)) return fail(SUBSPEC_EINVAL, "silu_mul: rows must be 16-byte aligned");
+  int rc = outputs_check("silu_mul", h, codes, scales);
+  if (!rc) rc = rows_check("silu_mul", "I", M, I, codes ? 128 : 8, 1 << 23);
+  if (rc) return rc;
+  subspec::ActArgs a{};
+  a.gu = static_cast<const uint16_t*>(gate_up);
+  a.M = M;
+  a.I = I;
+  a.y = static_cast<uint16_t*>(h);
+  a.codes = static_cast<uint8_t*>(codes);
+  a.scales = reinterpret_cast<uint8_t*>(scales);
+  const hipError_t e = subspec::launch_silu_mul(a, stream);
+  if (e != hipSuccess) return hip_fail(e, "silu_mul launch");
+  return SUBSPEC_OK;
+}
+
+int subspec_fp8_rows(const void* x, int M, int K, void* codes, uint32_t* scales, hipStream_t stream) {
+  if (!x || !codes || !scales) return fail(SUBSPEC_EINVAL, "fp8_rows: null pointer argument");
+  if (!aligned16(x) || !aligned16(codes) || !aligned_to(scales, 4))
+    return fail(SUBSPEC_EINVAL, "fp8_rows: rows and codes must be 16-byte and scales 4-byte aligned");
+  const int rc = rows_check("fp8_rows", "K", M, K, 128, 1 << 24);
+  if (rc) return rc;
+  const hipError_t e = subspec::launch_fp8_rows(static_cast<const uint16_t*>(x), M, K, static_cast<uint8_t*>(codes),
+                                                reinterpret_cast<uint8_t*>(scales), stream);
+  if (e != hipSuccess) return hip_fail(e, "fp8_rows launch");
+  return SUBSPEC_OK;
+}
+
+int subspec_fp8_read(const void* codes, const uint32_t* scales, int M, int K, void* y, hipStream_t stream) {
+  if (!codes || !scales || !y) return fail(SUBSPEC_EINVAL, "fp8_read: null pointer argument");
+  if (!aligned16(y) || !aligned16(codes) || !aligned_to(scales, 4))
+    return fail(SUBSPEC_EINVAL, "fp8_read: rows and codes must be 16-byte and scales 4-byte aligned");
+  const int rc = rows_check("fp8_read", "K", M, K, 128, 1 << 24);
+  if (rc) return rc;
+  const hipError_t e = subspec::launch_fp8_read(static_cast<const uint8_t*>(codes), reinterpret_cast<const uint8_t*>(scales), M, K,
+                                                static_cast<uint16_t*>(y), stream);
+  if (e != hipSuccess) return hip_fail(e, "fp8_read launch");
+  return SUBSPEC_OK;
+}
+
+int subspec_fp8_pack(const void* codes, int N, int K, void* tiles, hipStream_t stream) {
+  if (!codes || !tiles) return fail(SUBSPEC_EINVAL, "fp8_pack: null pointer argument");
+  if (codes == tiles) return fail(SUBSPEC_EINVAL, "fp8_pack: codes and tiles must not be the same");
+  if (!aligned16(codes) || !aligned16(tiles)) return fail(SUBSPEC_EINVAL, "fp8_pack: codes and tiles must be 16-byte aligned");
+  const int rc = fp8_weight_check("fp8_pack", N, K);
+  if (rc) return rc;
+  const hipError_t e = subspec::launch_fp8_pack(static_cast<const uint8_t*>(codes), N, K, static_cast<uint8_t*>(tiles), stream);
+  if (e != hipSuccess) return hip_fail(e, "fp8_pack launch");
+  return SUBSPEC_OK;
+}
+
+size_t subspec_fp8_linear_workspace_bytes(int M, int N, int K, int rows8) {
+  if (fp8_linear_check(M, N, K) || (rows8 != 0 && rows8 != 1)) return 0;
+  return subspec::fp8_plan(M, N, K, rows8 != 0).workspace_bytes;
+}
+
+int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K,
+                       void* y, hipStream_t stream) {
+  if (!x || !w || !w_scales || !y) return fail(SUBSPEC_EINVAL, "fp8_linear: null pointer argument");
+  if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned_to(x_scales, 4) || !aligned_to(w_scales, 4))
+    return fail(SUBSPEC_EINVAL, "fp8_linear: x, w and y must be 16-byte and scales 4-byte aligned");
+  int rc = fp8_linear_check(M, N, K);
+  if (rc) return rc;
+  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, x_scales != nullptr);
+  void* ws = nullptr;
+  if (p.workspace_bytes) {
+    rc = get_workspace(p.workspace_bytes, stream, &ws);
+    if (rc) return rc;
+  }
+  subspec::Fp8Args a{};
+  a.x = x;
+  a.xs = x_scales;
+  a.w = static_cast<const uint8_t*>(w);
+  a.ws = w_scales;
+  a.M = M;
+  a.N = N;
+  a.K = K;
+  a.y = static_cast<uint16_t*>(y);
+  const hipError_t e = subspec::launch_fp8_linear(p, a, ws, stream);
+  if (e != hipSuccess) return hip_fail(e, "fp8_linear launch");
   return SUBSPEC_OK;
 }
 

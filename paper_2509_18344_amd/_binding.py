@@ -162,7 +162,8 @@ _get_device = _is_contiguous = _data_ptr = _dtype = _numel = None
 # What a tensor may hold, by what the kernel takes its elements for: numbers of that type, or integers
 # of its size with their bits.
 _TYPES = {"bf16": ("bfloat16", "int16", "uint16"), "i32": ("int32", "uint32"), "f32": ("float32",),
-          "f64": ("float64",), "u8": ("uint8", "int8"), "e4m3": ("uint8", "int8", "float8_e4m3fn")}
+          "f64": ("float64",), "u8": ("uint8", "int8"), "e4m3": ("uint8", "int8", "float8_e4m3fn"),
+          "e8m0": ("uint8", "float8_e8m0fnu")}
 _NONE = repeat(None)
 _usual = {}  # a call's kinds -> the first torch type of each
 
@@ -456,32 +457,37 @@ def subspec_tree_verify_workspace_bytes(N, V) -> int:
     return int(load_library().subspec_tree_verify_workspace_bytes(N, V))
 
 
+def _scales(t, words):
+    """Kind and least elements of `words` scale words: words, or their bytes in order, [words / rows][rows][4]."""
+    if getattr(getattr(t, "dtype", None), "itemsize", 4) == 1:
+        return "e8m0", 4 * words
+    return "i32", words
+
+
 def subspec_add_norm(x, residual, weight, eps, M, K, sum, y, codes, scales, stream=None) -> int:
-    n = M * K
+    n, (kind, least) = M * K, _scales(scales, (K + 511) // 512 * M)
     st, px, pr, pw, ps, py, pc, pe = _device_args(
-        "subspec_add_norm", stream, ("bf16", "bf16", "bf16", "bf16", "bf16", "e4m3", "i32"),
-        (n, n, K, n, n, n, (K + 511) // 512 * M), x, residual, weight, sum, y, codes, scales)
+        "subspec_add_norm", stream, ("bf16", "bf16", "bf16", "bf16", "bf16", "e4m3", kind), (n, n, K, n, n, n, least),
+        x, residual, weight, sum, y, codes, scales)
     return _check("subspec_add_norm", load_library().subspec_add_norm(px, pr, pw, eps, M, K, ps, py, pc, pe, st))
 
 
 def subspec_silu_mul(gate_up, M, I, h, codes, scales, stream=None) -> int:
-    n = M * I
-    st, pg, ph, pc, pe = _device_args("subspec_silu_mul", stream, ("bf16", "bf16", "e4m3", "i32"),
-                                      (2 * n, n, n, (I + 511) // 512 * M), gate_up, h, codes, scales)
+    n, (kind, least) = M * I, _scales(scales, (I + 511) // 512 * M)
+    st, pg, ph, pc, pe = _device_args("subspec_silu_mul", stream, ("bf16", "bf16", "e4m3", kind), (2 * n, n, n, least),
+                                      gate_up, h, codes, scales)
     return _check("subspec_silu_mul", load_library().subspec_silu_mul(pg, M, I, ph, pc, pe, st))
 
 
 def subspec_fp8_rows(x, M, K, codes, scales, stream=None) -> int:
-    n = M * K
-    st, px, pc, pe = _device_args("subspec_fp8_rows", stream, ("bf16", "e4m3", "i32"), (n, n, (K + 511) // 512 * M),
-                                  x, codes, scales)
+    n, (kind, least) = M * K, _scales(scales, (K + 511) // 512 * M)
+    st, px, pc, pe = _device_args("subspec_fp8_rows", stream, ("bf16", "e4m3", kind), (n, n, least), x, codes, scales)
     return _check("subspec_fp8_rows", load_library().subspec_fp8_rows(px, M, K, pc, pe, st))
 
 
 def subspec_fp8_read(codes, scales, M, K, y, stream=None) -> int:
-    n = M * K
-    st, pc, pe, py = _device_args("subspec_fp8_read", stream, ("e4m3", "i32", "bf16"), (n, (K + 511) // 512 * M, n),
-                                  codes, scales, y)
+    n, (kind, least) = M * K, _scales(scales, (K + 511) // 512 * M)
+    st, pc, pe, py = _device_args("subspec_fp8_read", stream, ("e4m3", kind, "bf16"), (n, least, n), codes, scales, y)
     return _check("subspec_fp8_read", load_library().subspec_fp8_read(pc, pe, M, K, py, st))
 
 
@@ -490,15 +496,12 @@ def subspec_fp8_pack(codes, N, K, tiles, stream=None) -> int:
     return _check("subspec_fp8_pack", load_library().subspec_fp8_pack(pc, N, K, pt, st))
 
 
-_FP8_ROWS = ("e4m3", "i32", "e4m3", "i32", "bf16")
-_BF16_ROWS = ("bf16", "i32", "e4m3", "i32", "bf16")
-
-
 def subspec_fp8_linear(x, x_scales, w, w_scales, M, N, K, y, stream=None) -> int:
     words = (K + 511) // 512
+    (xk, xn), (wk, wn) = _scales(x_scales, words * M), _scales(w_scales, words * N)
     st, px, pe, pw, pf, py = _device_args(
-        "subspec_fp8_linear", stream, _BF16_ROWS if x_scales is None else _FP8_ROWS,
-        (M * K, words * M, N * K, words * N, M * N), x, x_scales, w, w_scales, y)
+        "subspec_fp8_linear", stream, ("bf16" if x_scales is None else "e4m3", xk, "e4m3", wk, "bf16"),
+        (M * K, xn, N * K, wn, M * N), x, x_scales, w, w_scales, y)
     return _check("subspec_fp8_linear", load_library().subspec_fp8_linear(px, pe, pw, pf, M, N, K, py, st))
 
 

@@ -121,6 +121,8 @@ def test_bf16_rows_give_the_bits_of_their_8_bit_rows(M, N, K):
     y8 = linear(c, s, t, ws, M, N, K)
     assert torch.equal(y.view(torch.int16), y8.view(torch.int16))
     check(y, oracle.fp8_rows(f64(x)), (wc, wb))
+    bytes_ = ws.view(torch.uint8).view(-1, N, 4)  # scales as bytes
+    assert torch.equal(linear(c.view(torch.float8_e4m3fn), s.view(torch.float8_e8m0fnu), t, bytes_, M, N, K).view(torch.int16), y.view(torch.int16))
     for _ in range(3):
         assert torch.equal(linear(xd, None, t, ws, M, N, K).view(torch.int16), y.view(torch.int16))
 

@@ -123,7 +123,7 @@ CALLS = {
                 dict(x=(U8, M * K), xs=(I32, 2 * M), w=(U8, N * K), ws=(I32, 2 * N), y=(BF, M * N))),
 }
 EACH = [(call, name) for call in CALLS for name in CALLS[call][1]]
-OTHER = {BF: [torch.float16, F32, U8], I32: [torch.int64, F32], U8: [BF, I32, torch.float8_e5m2]}
+OTHER = {BF: [torch.float16, F32, U8], I32: [torch.int64, F32, torch.int16], U8: [BF, I32, torch.float8_e5m2]}
 
 
 def _args(call, **changed):
@@ -137,12 +137,15 @@ def test_tensors_of_exactly_the_size_needed_pass(calls, call):  # noqa: F811
     for name, (dtype, n) in CALLS[call][1].items():
         if dtype == U8:  # codes under their own type
             CALLS[call][0](_args(call, **{name: Fake(torch.float8_e4m3fn, n)}))
+        if dtype == I32:  # scales as bytes
+            for t in (U8, torch.float8_e8m0fnu):
+                CALLS[call][0](_args(call, **{name: Fake(t, 4 * n)}))
 
 
 @pytest.mark.parametrize("call,name", EACH)
 def test_a_tensor_too_small_or_of_another_type_is_refused(calls, call, name):  # noqa: F811
     dtype, n = CALLS[call][1][name]
-    for bad in [Fake(dtype, n - 1)] + [Fake(t, n) for t in OTHER[dtype]]:
+    for bad in [Fake(dtype, n - 1)] + [Fake(t, n) for t in OTHER[dtype]] + [Fake(U8, 4 * n - 1)] * (dtype == I32):
         with refused("EINVAL"):
             CALLS[call][0](_args(call, **{name: bad}))
     assert not calls

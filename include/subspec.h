@@ -516,8 +516,8 @@ int subspec_fp8_rows(const void* x, int M, int K, void* codes, uint32_t* scales,
 int subspec_fp8_read(const void* codes, const uint32_t* scales, int M, int K, void* y, hipStream_t stream);
 
 /* Codes [N][K] of a weight (subspec_fp8_rows of its rows) as weight tiles.  tiles: device, N * K bytes,
- * written, not the codes' own memory.  Needs N a positive multiple of 16, K a positive multiple of 128 up
- * to 2^24, N * K <= 2^40; 16-byte alignment. */
+ * written, not the codes' own memory.  Needs N a positive multiple of 16 up to 2^24, K a positive multiple
+ * of 128 up to 2^20, N * K <= 2^40; 16-byte alignment. */
 int subspec_fp8_pack(const void* codes, int N, int K, void* tiles, hipStream_t stream);
 
 /* y = x w^T, both in 8-bit rows:
@@ -531,7 +531,7 @@ int subspec_fp8_pack(const void* codes, int N, int K, void* tiles, hipStream_t s
  *   x_scales device uint32 [ceil(K / 512)][M], or null
  *   w        device: weight tiles (subspec_fp8_pack), w_scales device uint32 [ceil(K / 512)][N]
  *   y        device bf16 [M][N], fully overwritten
- * Needs 1 <= M <= 2^20, K a positive multiple of 128 up to 2^24, N a positive multiple of 16 up to 2^24,
+ * Needs 1 <= M <= 2^20, K a positive multiple of 128 up to 2^20, N a positive multiple of 16 up to 2^24,
  * M * K, N * K and M * N at most 2^40; 16-byte alignment (scales 4); y must not overlap the inputs.  Equal
  * calls give equal bits.  Workspace as for subspec_qlinear (subspec_fp8_linear_workspace_bytes). */
 int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M,

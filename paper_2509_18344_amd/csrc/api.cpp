@@ -19,12 +19,12 @@
 #include "kernels.h"
 #include "kernels_tree.h"
 #include "kernels_attn.h"
-#include "kernels_fp8.h"
 #include "kernels_hqq.h"
 #include "kernels_qstream.h"
 #include "kernels_rope.h"
 #include "kernels_kv4.h"
 #include "kernels_verify.h"
+#include "kernels_fp8.h"
 
 namespace {
 
@@ -1386,13 +1386,13 @@ int outputs_check(const char* fn, const void* y, const void* codes, const void* 
 
 int fp8_weight_check(const char* fn, int N, int K) {
   if (N < 1 || N > (1 << 24) || N % 16) return fail(SUBSPEC_EUNSUPPORTED, "%s: N=%d: must be a multiple of 16 in 16..2^24", fn, N);
-  if (K < 1 || K > (1 << 24) || K % 128) return fail(SUBSPEC_EUNSUPPORTED, "%s: K=%d: must be a multiple of 128 in 128..2^24", fn, K);
+  if (K < 1 || K > (1 << 20) || K % 128) return fail(SUBSPEC_EUNSUPPORTED, "%s: K=%d: must be a multiple of 128 in 128..2^20", fn, K);
   if (static_cast<long long>(N) * K > kMostElements) return fail(SUBSPEC_EUNSUPPORTED, "%s: N * K exceeds 2^40", fn);
   return SUBSPEC_OK;
 }
 
 int fp8_linear_check(int M, int N, int K) {
-  int rc = rows_check("fp8_linear", "K", M, K, 128, 1 << 24);
+  int rc = rows_check("fp8_linear", "K", M, K, 128, 1 << 20);
   if (!rc) rc = fp8_weight_check("fp8_linear", N, K);
   if (!rc && static_cast<long long>(M) * N > kMostElements) rc = fail(SUBSPEC_EUNSUPPORTED, "fp8_linear: M * N exceeds 2^40");
   return rc;
@@ -1482,7 +1482,7 @@ int subspec_fp8_pack(const void* codes, int N, int K, void* tiles, hipStream_t s
 
 size_t subspec_fp8_linear_workspace_bytes(int M, int N, int K, int rows8) {
   if (fp8_linear_check(M, N, K) || (rows8 != 0 && rows8 != 1)) return 0;
-  return subspec::fp8_plan(M, N, K, rows8 != 0).workspace_bytes;
+  return subspec::fp8_plan(M, N, K, rows8 != 0, device_cus()).workspace_bytes;
 }
 
 int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K,
@@ -1492,7 +1492,7 @@ int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, c
     return fail(SUBSPEC_EINVAL, "fp8_linear: x, w and y must be 16-byte and scales 4-byte aligned");
   int rc = fp8_linear_check(M, N, K);
   if (rc) return rc;
-  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, x_scales != nullptr);
+  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, x_scales != nullptr, device_cus());
   void* ws = nullptr;
   if (p.workspace_bytes) {
     rc = get_workspace(p.workspace_bytes, stream, &ws);

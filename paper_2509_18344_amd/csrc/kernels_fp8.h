@@ -13,12 +13,22 @@ struct Fp8Args {
   const uint32_t* ws;     // [fp8_words(K)][N]
   int M, N, K;
   uint16_t* y;            // bf16 [M][N]
+  // Work of the tiles' kernel.  Its workgroups ("workers") take tiles whole in `rounds` rounds of one
+  // each; the tiles left over are cut along K among the first `sharers` workers, in equal runs of
+  // blocks.
+  int tiles_m, tiles_n;
+  int workers, rounds, left, sharers;
+  float* part;            // [sharers][2] tiles of partial sums
+  unsigned* count;        // per left tile: workers done (zero between launches)
 };
 
 struct Fp8Plan {
-  size_t workspace_bytes;  // completion counters, then x's codes and scales where the call makes them
+  int rows;                // rows of a tile
+  int workers, rounds, left, sharers;
+  size_t code_bytes;       // x's codes and scales, where the call makes them
+  size_t workspace_bytes;  // completion counters, codes and scales, partial sums; 0: none
 };
-Fp8Plan fp8_plan(int M, int N, int K, bool rows8);
+Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus);
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st);
 hipError_t launch_fp8_pack(const uint8_t* codes, int N, int K, uint8_t* tiles, hipStream_t st);
 

@@ -18,18 +18,22 @@ struct Fp8Args {
   // blocks.
   int tiles_m, tiles_n;
   int workers, rounds, left, sharers;
-  float* part;            // [sharers][2] tiles of partial sums
-  unsigned* count;        // per left tile: workers done (zero between launches)
+  float* part;            // [sharers][2] tiles of partial sums; few rows: [columns][splits]
+  unsigned* count;        // per left tile, or columns: workers done (zero between launches)
+  int splits;             // few rows: workgroups that share columns
 };
 
 struct Fp8Plan {
-  int rows;                // rows of a tile
+  int few;                 // at most 16 rows: tiles of 16 columns a wavefront; 0: the tiles' kernel
+  int waves, splits;       // wavefronts of a workgroup and workgroups that share columns then
+  int rows;                // rows of a tile otherwise
   int workers, rounds, left, sharers;
   size_t code_bytes;       // x's codes and scales, where the call makes them
   size_t workspace_bytes;  // completion counters, codes and scales, partial sums; 0: none
 };
 Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus);
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st);
+hipError_t launch_fp8_few(const Fp8Args& a, int tiles, int waves, hipStream_t st);
 hipError_t launch_fp8_pack(const uint8_t* codes, int N, int K, uint8_t* tiles, hipStream_t st);
 
 }  // namespace subspec

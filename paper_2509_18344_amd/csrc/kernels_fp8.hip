@@ -291,6 +291,7 @@ __global__ __launch_bounds__(256) void k_fp8_pack(const uint8_t* codes, int N, i
   *reinterpret_cast<uint4*>(tiles + 16 * t) = *reinterpret_cast<const uint4*>(codes + n * K + k);
 }
 
+constexpr int kFewRows = 16;   // up to here kernels_fp8_few.hip
 constexpr int kColumns = 256;  // of every tile
 
 template <int MF, int NF, int WM, int WN, int STAGES>
@@ -308,6 +309,15 @@ hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
 
 Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
   Fp8Plan p{};
+  if (M <= kFewRows) {
+    const int tiles = N / 16, units = (K + 255) / 256;
+    p.few = tiles >= 4 * cus ? 2 : 1;
+    p.waves = tiles > cus ? 4 : 8;
+    const int sets = (tiles + p.few - 1) / p.few;
+    p.splits = std::max(1, std::min({(p.waves == 4 ? 4 : 1) * cus / sets, units / (4 * p.waves), 64}));
+    if (p.splits > 1) p.workspace_bytes = kSplitCounterBytes + static_cast<size_t>(sets) * p.splits * p.few * kWave * 16;
+    return p;
+  }
   p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
   const long long tiles = static_cast<long long>((M + p.rows - 1) / p.rows) * ((N + kColumns - 1) / kColumns);
   const long long KB = K / 128;
@@ -327,6 +337,14 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
 
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
+  if (p.few) {
+    a.splits = p.splits;
+    if (ws) {
+      a.count = reinterpret_cast<unsigned*>(ws);
+      a.part = reinterpret_cast<float*>(ws + kSplitCounterBytes);
+    }
+    return launch_fp8_few(a, p.few, p.waves, st);
+  }
   if (!a.xs) {
     uint8_t* codes = ws + kSplitCounterBytes;
     uint8_t* scales = codes + static_cast<size_t>(a.M) * a.K;

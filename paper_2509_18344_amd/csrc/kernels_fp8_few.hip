@@ -1,0 +1,208 @@
+// The product in 8-bit floating point for at most 16 rows, where the weights' bytes are all that counts:
+// codes become bf16 numbers on the way (exactly) and meet in the 16-bit matrix instruction, whose products
+// are exact and whose sums are in fp32, a block of 128 k at a time; the block's two powers of two are
+// applied to its sum.  (The 8-bit matrix instruction would cut products to 13 bits, and its rate is not
+// needed here: at 5 TB/s a SIMD has about 1000 cycles for a tile of 16 columns and 128 k.)
+//
+// A wavefront takes CT tiles of 16 columns and a run of K, its weights straight from memory to registers, a
+// group of four blocks ahead; the wavefronts of a workgroup share the columns and cut K among them, as do
+// `splits` workgroups where there are few columns.
+#include <algorithm>
+
+#include "fp8_device.h"
+#include "kernels_fp8.h"
+
+namespace subspec {
+
+namespace {
+
+constexpr int kUnit = 2;    // blocks that a wavefront loads at once, one unit ahead of the products
+constexpr int kAgent = 16;  // sc1: coherent at agent scope
+
+// Two codes (the low or the high half of w) as bf16 numbers.
+template <bool HI>
+__device__ __forceinline__ bf16x2_t two_bf16(uint32_t w) {
+  return __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HI));
+}
+__device__ __forceinline__ bf16x8_t eight_bf16(uint32_t lo, uint32_t hi) {
+  const bf16x2_t a = two_bf16<false>(lo), b = two_bf16<true>(lo), c = two_bf16<false>(hi), d = two_bf16<true>(hi);
+  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+__device__ __forceinline__ float max_across_rows(float v) {  // over the lanes l, l ^ 16, l ^ 32, l ^ 48
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// What a lane holds of a block of x: row lane % 16, k = 16 q .. and 64 + 16 q .. (q = lane / 16), 16 each, the
+// places that a weight tile gives it too.
+template <bool FUSED>
+struct XBlock {
+  u32x4_t v[FUSED ? 4 : 2];
+};
+
+template <bool FUSED>
+__device__ __forceinline__ XBlock<FUSED> load_x(const uint8_t* row, int kb) {
+  XBlock<FUSED> b;
+  if constexpr (FUSED) {
+    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(row + 256ll * kb);
+    b.v[0] = p[0];
+    b.v[1] = p[1];
+    b.v[2] = p[8];
+    b.v[3] = p[9];
+  } else {
+    const u32x4_t* p = reinterpret_cast<const u32x4_t*>(row + 128ll * kb);
+    b.v[0] = p[0];
+    b.v[1] = p[4];
+  }
+  return b;
+}
+
+// The block's codes as four operands of the matrix instruction, and the scale byte.
+template <bool FUSED>
+__device__ __forceinline__ void x_operands(const XBlock<FUSED>& b, bf16x8_t (&out)[4], uint32_t* byte) {
+  if constexpr (FUSED) {
+    float x[4][8];
+    float top = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      unpack8(make_uint4(b.v[u][0], b.v[u][1], b.v[u][2], b.v[u][3]), x[u]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float m = fabsf(x[u][i]);
+        top = fmaxf(top, m < __builtin_inff() ? m : 0.f);
+      }
+    }
+    *byte = fp8_scale_byte(max_across_rows(top));
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint2 c = fp8_codes(x[u], *byte);
+      out[u] = eight_bf16(c.x, c.y);
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) out[u] = eight_bf16(b.v[u / 2][2 * (u % 2)], b.v[u / 2][2 * (u % 2) + 1]);
+  }
+}
+
+template <int WAVES, int CT, bool FUSED>
+__global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
+  __shared__ f32x4_t sums[WAVES][CT][kWave];
+  __shared__ int last;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, q = lane / 16;
+  const int KB = a.K / 128, units = (KB + kUnit - 1) / kUnit;
+  const int set = blockIdx.x / a.splits, split = blockIdx.x % a.splits, parts = a.splits * WAVES, part = split * WAVES + wave;
+  const int g0 = static_cast<int>(static_cast<long long>(part) * units / parts), g1 = static_cast<int>(static_cast<long long>(part + 1) * units / parts);
+  const int m = min(lane % 16, a.M - 1);  // (rows past the last: that one again)
+  const uint8_t* xrow = static_cast<const uint8_t*>(a.x) + (FUSED ? 2 : 1) * (static_cast<size_t>(m) * a.K + 16 * q);
+  const uint8_t* wt[CT];
+  const uint32_t* wst[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) {
+    const int tile = min(set * CT + c, a.N / 16 - 1);
+    wt[c] = a.w + static_cast<size_t>(tile) * KB * 2048 + 16 * lane;
+    wst[c] = a.ws + 16 * tile + 4 * q;
+  }
+  struct Unit {
+    u32x4_t w[CT][kUnit][2];
+    u32x4_t ws[CT];
+    XBlock<FUSED> x[kUnit];
+    uint32_t xs;
+  };
+  auto load = [&](int g, Unit& r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CT; ++c) {
+#pragma unroll
+      for (int j = 0; j < kUnit; ++j) {
+        const u32x4_t* p = reinterpret_cast<const u32x4_t*>(wt[c] + 2048ll * min(kUnit * g + j, KB - 1));
+        r.w[c][j][0] = __builtin_nontemporal_load(p);
+        r.w[c][j][1] = __builtin_nontemporal_load(p + 64);
+      }
+      r.ws[c] = *reinterpret_cast<const u32x4_t*>(wst[c] + static_cast<size_t>(kUnit * g / 4) * a.N);
+    }
+    if constexpr (!FUSED) r.xs = a.xs[static_cast<size_t>(kUnit * g / 4) * a.M + m];
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) r.x[j] = load_x<FUSED>(xrow, min(kUnit * g + j, KB - 1));
+  };
+  f32x4_t acc[CT];
+#pragma unroll
+  for (int c = 0; c < CT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  Unit next;
+  if (g0 < g1) load(g0, next);
+  for (int g = g0; g < g1; ++g) {
+    const Unit now = next;
+    if (g + 1 < g1) load(g + 1, next);
+#pragma unroll
+    for (int j = 0; j < kUnit; ++j) {
+      if (kUnit * g + j >= KB) break;
+      const int shift = 8 * ((kUnit * g + j) % 4);
+      bf16x8_t x[4];
+      uint32_t xs = FUSED ? 0u : now.xs >> shift & 255u;
+      x_operands<FUSED>(now.x[j], x, &xs);
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(now.w[c][j][u / 2][2 * (u % 2)], now.w[c][j][u / 2][2 * (u % 2) + 1]), x[u], s, 0, 0, 0);
+        // this lane's row of x, and four columns
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[c][e] += ldexpf(s[e], static_cast<int>(xs + (now.ws[c][e] >> shift & 255u)) - 254);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CT; ++c) sums[wave][c][lane] = acc[c];
+  __syncthreads();
+  // A wavefront for every tile adds the runs of K in their order.
+  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+  if (wave < CT) {
+    v = sums[0][wave][lane];
+#pragma unroll
+    for (int u = 1; u < WAVES; ++u) v += sums[u][wave][lane];
+  }
+  if (a.splits > 1) {
+    // Agent-scope stores, counted in once they are acknowledged; the last workgroup of the columns adds all.
+    const uint32_t bytes = static_cast<uint32_t>(a.splits) * CT * kWave * 16;
+    const __amdgpu_buffer_rsrc_t part_of = buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(set) * bytes, bytes);
+    if (wave < CT) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), part_of, ((split * CT + wave) * kWave + lane) * 16, 0, kAgent);
+    __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
+    __syncthreads();
+    if (threadIdx.x == 0)
+      last = __hip_atomic_fetch_add(a.count + set, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(a.splits - 1);
+    __syncthreads();
+    if (!last) return;
+    if (wave < CT) {
+      v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      for (int s = 0; s < a.splits; ++s)
+        v += __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(part_of, ((s * CT + wave) * kWave + lane) * 16, 0, kAgent));
+    }
+    if (threadIdx.x == 0) __hip_atomic_store(a.count + set, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  const int tile = set * CT + wave;
+  if (wave < CT && tile < a.N / 16 && lane % 16 < a.M) {
+    const uint32_t lo = float_to_bf16_bits(v[0]) | static_cast<uint32_t>(float_to_bf16_bits(v[1])) << 16;
+    const uint32_t hi = float_to_bf16_bits(v[2]) | static_cast<uint32_t>(float_to_bf16_bits(v[3])) << 16;
+    *reinterpret_cast<uint2*>(a.y + static_cast<size_t>(lane % 16) * a.N + 16 * tile + 4 * q) = make_uint2(lo, hi);
+  }
+}
+
+template <int WAVES, int CT>
+void few_at(const Fp8Args& a, hipStream_t st) {
+  const dim3 grid((a.N / 16 + CT - 1) / CT * a.splits), block(WAVES * kWave);
+  if (a.xs) hipLaunchKernelGGL((k_fp8_few<WAVES, CT, false>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_fp8_few<WAVES, CT, true>), grid, block, 0, st, a);
+}
+
+}  // namespace
+
+hipError_t launch_fp8_few(const Fp8Args& a, int tiles, int waves, hipStream_t st) {
+  if (tiles == 2) few_at<4, 2>(a, st);
+  else if (waves == 4) few_at<4, 1>(a, st);
+  else few_at<8, 1>(a, st);
+  return hipGetLastError();
+}
+
+}  // namespace subspec

@@ -24,7 +24,7 @@ struct Fp8Args {
 };
 
 struct Fp8Plan {
-  int few;                 // at most 16 rows: tiles of 16 columns a wavefront; 0: the tiles' kernel
+  int few;                 // few rows: tiles of 16 columns a wavefront; 0: the tiles' kernel
   int waves, splits;       // wavefronts of a workgroup and workgroups that share columns then
   int rows;                // rows of a tile otherwise
   int workers, rounds, left, sharers;
@@ -33,7 +33,7 @@ struct Fp8Plan {
 };
 Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus);
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st);
-hipError_t launch_fp8_few(const Fp8Args& a, int tiles, int waves, hipStream_t st);
+hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t st);
 hipError_t launch_fp8_pack(const uint8_t* codes, int N, int K, uint8_t* tiles, hipStream_t st);
 
 }  // namespace subspec

@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256) void k_fp8_pack(const uint8_t* codes, int N, i
   *reinterpret_cast<uint4*>(tiles + 16 * t) = *reinterpret_cast<const uint4*>(codes + n * K + k);
 }
 
-constexpr int kFewRows = 16;   // up to here kernels_fp8_few.hip
+constexpr int kFewRows = 64;   // up to here kernels_fp8_few.hip
 constexpr int kColumns = 256;  // of every tile
 
 template <int MF, int NF, int WM, int WN, int STAGES>
@@ -305,6 +305,10 @@ hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+size_t fp8_row_bytes(int M, int K) {
+  return (static_cast<size_t>(M) * K + static_cast<size_t>(fp8_words(K)) * M * 4 + 255) & ~size_t(255);
+}
+
 }  // namespace
 
 Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
@@ -312,13 +316,16 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
   if (M <= kFewRows) {
     const int tiles = N / 16, units = (K + 255) / 256;
     p.few = tiles >= 4 * cus ? 2 : 1;
-    p.waves = tiles > cus ? 4 : 8;
-    const int sets = (tiles + p.few - 1) / p.few;
+    p.waves = M > 16 || tiles > cus ? 4 : 8;
+    const int sets = (tiles + p.few - 1) / p.few, rows = (M + 15) / 16;
     p.splits = std::max(1, std::min({(p.waves == 4 ? 4 : 1) * cus / sets, units / (4 * p.waves), 64}));
-    if (p.splits > 1) p.workspace_bytes = kSplitCounterBytes + static_cast<size_t>(sets) * p.splits * p.few * kWave * 16;
+    size_t at = kSplitCounterBytes;
+    if (!rows8 && M > 16) at += p.code_bytes = fp8_row_bytes(M, K);
+    if (p.splits > 1) at += static_cast<size_t>(sets) * p.splits * rows * p.few * kWave * 16;
+    p.workspace_bytes = at > kSplitCounterBytes ? at : 0;
     return p;
   }
-  p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+  p.rows = M <= 128 ? 128 : 256;
   const long long tiles = static_cast<long long>((M + p.rows - 1) / p.rows) * ((N + kColumns - 1) / kColumns);
   const long long KB = K / 128;
   p.rounds = static_cast<int>(tiles / cus);
@@ -326,10 +333,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
   p.sharers = static_cast<int>(std::min<long long>(cus, p.left * KB));
   p.workers = p.rounds ? cus : p.sharers;
   size_t at = kSplitCounterBytes;
-  if (!rows8) {
-    p.code_bytes = (static_cast<size_t>(M) * K + static_cast<size_t>(fp8_words(K)) * M * 4 + 255) & ~size_t(255);
-    at += p.code_bytes;
-  }
+  if (!rows8) at += p.code_bytes = fp8_row_bytes(M, K);
   if (p.sharers > p.left) at += static_cast<size_t>(p.sharers) * 2 * p.rows * kColumns * 4;
   p.workspace_bytes = at > kSplitCounterBytes ? at : 0;
   return p;
@@ -337,15 +341,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
 
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st) {
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (p.few) {
-    a.splits = p.splits;
-    if (ws) {
-      a.count = reinterpret_cast<unsigned*>(ws);
-      a.part = reinterpret_cast<float*>(ws + kSplitCounterBytes);
-    }
-    return launch_fp8_few(a, p.few, p.waves, st);
-  }
-  if (!a.xs) {
+  if (p.code_bytes) {
     uint8_t* codes = ws + kSplitCounterBytes;
     uint8_t* scales = codes + static_cast<size_t>(a.M) * a.K;
     const hipError_t e = launch_fp8_rows(static_cast<const uint16_t*>(a.x), a.M, a.K, codes, scales, st);
@@ -353,19 +349,21 @@ hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipSt
     a.x = codes;
     a.xs = reinterpret_cast<const uint32_t*>(scales);
   }
+  if (ws) {
+    a.count = reinterpret_cast<unsigned*>(ws);
+    a.part = reinterpret_cast<float*>(ws + kSplitCounterBytes + p.code_bytes);
+  }
+  if (p.few) {
+    a.splits = p.splits;
+    return launch_fp8_few(a, p.few, p.waves, st);
+  }
   a.tiles_m = (a.M + p.rows - 1) / p.rows;
   a.tiles_n = (a.N + kColumns - 1) / kColumns;
   a.workers = p.workers;
   a.rounds = p.rounds;
   a.left = p.left;
   a.sharers = p.sharers;
-  if (ws) {
-    a.count = reinterpret_cast<unsigned*>(ws);
-    a.part = reinterpret_cast<float*>(ws + kSplitCounterBytes + p.code_bytes);
-  }
   switch (p.rows) {
-    case 32: return tiles_at<1, 1, 1, 8, 4>(a, st);
-    case 64: return tiles_at<2, 1, 1, 8, 3>(a, st);
     case 128: return tiles_at<4, 1, 1, 8, 3>(a, st);
     default: return tiles_at<4, 2, 2, 4, 2>(a, st);
   }

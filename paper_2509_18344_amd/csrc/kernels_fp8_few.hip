@@ -1,4 +1,4 @@
-// The product in 8-bit floating point for at most 16 rows, where the weights' bytes are all that counts:
+// The product in 8-bit floating point for few rows, where the weights' bytes are all that counts:
 // codes become bf16 numbers on the way (exactly) and meet in the 16-bit matrix instruction, whose products
 // are exact and whose sums are in fp32, a block of 128 k at a time; the block's two powers of two are
 // applied to its sum.  (The 8-bit matrix instruction would cut products to 13 bits, and its rate is not
@@ -29,11 +29,11 @@ __device__ __forceinline__ bf16x8_t eight_bf16(uint32_t lo, uint32_t hi) {
   return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-__device__ __forceinline__ float max_across_rows(float v) {  // over the lanes l, l ^ 16, l ^ 32, l ^ 48
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+__device__ __forceinline__ uint32_t max_across_rows(uint32_t v) {  // over the lanes l, l ^ 16, l ^ 32, l ^ 48
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = max(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return max(b[0], b[1]);
 }
 
 // What a lane holds of a block of x: row lane % 16, k = 16 q .. and 64 + 16 q .. (q = lane / 16), 16 each, the
@@ -64,22 +64,45 @@ __device__ __forceinline__ XBlock<FUSED> load_x(const uint8_t* row, int kb) {
 template <bool FUSED>
 __device__ __forceinline__ void x_operands(const XBlock<FUSED>& b, bf16x8_t (&out)[4], uint32_t* byte) {
   if constexpr (FUSED) {
-    float x[4][8];
-    float top = 0.f;
+    // Magnitudes of pairs as 16-bit whole numbers, which order as the numbers do.
+    typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
+    u16x2_t top = {0, 0};
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      unpack8(make_uint4(b.v[u][0], b.v[u][1], b.v[u][2], b.v[u][3]), x[u]);
+    for (int u = 0; u < 4; ++u)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float m = fabsf(x[u][i]);
-        top = fmaxf(top, m < __builtin_inff() ? m : 0.f);
+      for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2_t, b.v[u][i] & 0x7FFF7FFFu));
+    const uint32_t most = max_across_rows(max(static_cast<uint32_t>(top[0]), static_cast<uint32_t>(top[1])));
+    if (__any(most >= 0x7F80u)) {  // infinities or NaN in some row's block
+      float x[4][8], finite = 0.f;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        unpack8(make_uint4(b.v[u][0], b.v[u][1], b.v[u][2], b.v[u][3]), x[u]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float m = fabsf(x[u][i]);
+          finite = fmaxf(finite, m < __builtin_inff() ? m : 0.f);
+        }
       }
+      *byte = fp8_scale_byte(__uint_as_float(max_across_rows(__float_as_uint(finite))));
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint2 c = fp8_codes(x[u], *byte);
+        out[u] = eight_bf16(c.x, c.y);
+      }
+      return;
     }
-    *byte = fp8_scale_byte(max_across_rows(top));
+    *byte = fp8_scale_byte(__uint_as_float(most << 16));
+    const float scale = __uint_as_float(*byte << 23);  // 2^e
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const uint2 c = fp8_codes(x[u], *byte);
-      out[u] = eight_bf16(c.x, c.y);
+      typedef short s16x2_t __attribute__((ext_vector_type(2)));
+      const uint32_t w[4] = {b.v[u][0], b.v[u][1], b.v[u][2], b.v[u][3]};
+      s16x2_t lo = {0, 0}, hi = {0, 0};
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2_t, w[0]), scale, false);
+      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2_t, w[1]), scale, true);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, w[2]), scale, false);
+      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, w[3]), scale, true);
+      out[u] = eight_bf16(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
     }
   } else {
 #pragma unroll
@@ -87,16 +110,25 @@ __device__ __forceinline__ void x_operands(const XBlock<FUSED>& b, bf16x8_t (&ou
   }
 }
 
-template <int WAVES, int CT, bool FUSED>
+// MT tiles of 16 rows, CT of 16 columns a wavefront.
+template <int WAVES, int MT, int CT, bool FUSED>
 __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
-  __shared__ f32x4_t sums[WAVES][CT][kWave];
+  constexpr int TILES = MT * CT;
+  __shared__ f32x4_t sums[WAVES][TILES][kWave];
   __shared__ int last;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, q = lane / 16;
   const int KB = a.K / 128, units = (KB + kUnit - 1) / kUnit;
   const int set = blockIdx.x / a.splits, split = blockIdx.x % a.splits, parts = a.splits * WAVES, part = split * WAVES + wave;
   const int g0 = static_cast<int>(static_cast<long long>(part) * units / parts), g1 = static_cast<int>(static_cast<long long>(part + 1) * units / parts);
-  const int m = min(lane % 16, a.M - 1);  // (rows past the last: that one again)
-  const uint8_t* xrow = static_cast<const uint8_t*>(a.x) + (FUSED ? 2 : 1) * (static_cast<size_t>(m) * a.K + 16 * q);
+  const int kb1 = min(kUnit * g1, KB);
+  const uint8_t* xrow[MT];
+  const uint32_t* xsrow[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    const int m = min(16 * t + lane % 16, a.M - 1);  // (rows past the last: that one again)
+    xrow[t] = static_cast<const uint8_t*>(a.x) + (FUSED ? 2 : 1) * (static_cast<size_t>(m) * a.K + 16 * q);
+    xsrow[t] = a.xs + m;
+  }
   const uint8_t* wt[CT];
   const uint32_t* wst[CT];
 #pragma unroll
@@ -105,13 +137,15 @@ __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
     wt[c] = a.w + static_cast<size_t>(tile) * KB * 2048 + 16 * lane;
     wst[c] = a.ws + 16 * tile + 4 * q;
   }
-  struct Unit {
+  struct Weights {
     u32x4_t w[CT][kUnit][2];
-    u32x4_t ws[CT];
-    XBlock<FUSED> x[kUnit];
-    uint32_t xs;
+    u32x4_t s[CT];
   };
-  auto load = [&](int g, Unit& r) __attribute__((always_inline)) {
+  struct Rows {
+    XBlock<FUSED> b[MT];
+    uint32_t s[MT];
+  };
+  auto load_w = [&](int g, Weights& r) __attribute__((always_inline)) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) {
 #pragma unroll
@@ -120,88 +154,139 @@ __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
         r.w[c][j][0] = __builtin_nontemporal_load(p);
         r.w[c][j][1] = __builtin_nontemporal_load(p + 64);
       }
-      r.ws[c] = *reinterpret_cast<const u32x4_t*>(wst[c] + static_cast<size_t>(kUnit * g / 4) * a.N);
+      r.s[c] = *reinterpret_cast<const u32x4_t*>(wst[c] + static_cast<size_t>(kUnit * g / 4) * a.N);
     }
-    if constexpr (!FUSED) r.xs = a.xs[static_cast<size_t>(kUnit * g / 4) * a.M + m];
-#pragma unroll
-    for (int j = 0; j < kUnit; ++j) r.x[j] = load_x<FUSED>(xrow, min(kUnit * g + j, KB - 1));
   };
-  f32x4_t acc[CT];
+  auto load_rows = [&](int kb, Rows& r) __attribute__((always_inline)) {
 #pragma unroll
-  for (int c = 0; c < CT; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  Unit next;
-  if (g0 < g1) load(g0, next);
+    for (int t = 0; t < MT; ++t) {
+      r.b[t] = load_x<FUSED>(xrow[t], kb);
+      if constexpr (!FUSED) r.s[t] = xsrow[t][static_cast<size_t>(kb / 4) * a.M];
+    }
+  };
+  f32x4_t acc[MT][CT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t)
+#pragma unroll
+    for (int c = 0; c < CT; ++c) acc[t][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  Weights next;
+  Rows rows;
+  if (g0 < g1) {
+    load_rows(kUnit * g0, rows);
+    load_w(g0, next);
+  }
   for (int g = g0; g < g1; ++g) {
-    const Unit now = next;
-    if (g + 1 < g1) load(g + 1, next);
+    const Weights now = next;
+    if (g + 1 < g1) load_w(g + 1, next);
 #pragma unroll
     for (int j = 0; j < kUnit; ++j) {
-      if (kUnit * g + j >= KB) break;
-      const int shift = 8 * ((kUnit * g + j) % 4);
-      bf16x8_t x[4];
-      uint32_t xs = FUSED ? 0u : now.xs >> shift & 255u;
-      x_operands<FUSED>(now.x[j], x, &xs);
+      const int kb = kUnit * g + j;
+      if (kb >= kb1) break;
+      const Rows x = rows;
+      if (kb + 1 < kb1) load_rows(kb + 1, rows);
+      const int shift = 8 * (kb % 4);
+      bf16x8_t w[CT][4];
 #pragma unroll
-      for (int c = 0; c < CT; ++c) {
-        f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < CT; ++c)
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_bf16(now.w[c][j][u / 2][2 * (u % 2)], now.w[c][j][u / 2][2 * (u % 2) + 1]), x[u], s, 0, 0, 0);
-        // this lane's row of x, and four columns
+        for (int u = 0; u < 4; ++u) w[c][u] = eight_bf16(now.w[c][j][u / 2][2 * (u % 2)], now.w[c][j][u / 2][2 * (u % 2) + 1]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[c][e] += ldexpf(s[e], static_cast<int>(xs + (now.ws[c][e] >> shift & 255u)) - 254);
+      for (int t = 0; t < MT; ++t) {
+        bf16x8_t xo[4];
+        uint32_t xs = FUSED ? 0u : x.s[t] >> shift & 255u;
+        x_operands<FUSED>(x.b[t], xo, &xs);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c][u], xo[u], s, 0, 0, 0);
+          // this lane's row of x, and four columns
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[t][c][e] += ldexpf(s[e], static_cast<int>(xs + (now.s[c][e] >> shift & 255u)) - 254);
+        }
       }
     }
   }
 #pragma unroll
-  for (int c = 0; c < CT; ++c) sums[wave][c][lane] = acc[c];
-  __syncthreads();
-  // A wavefront for every tile adds the runs of K in their order.
-  f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-  if (wave < CT) {
-    v = sums[0][wave][lane];
+  for (int t = 0; t < MT; ++t)
 #pragma unroll
-    for (int u = 1; u < WAVES; ++u) v += sums[u][wave][lane];
+    for (int c = 0; c < CT; ++c) sums[wave][t * CT + c][lane] = acc[t][c];
+  __syncthreads();
+  // The runs of K are added in their order, tile i by wavefront i % WAVES.
+  constexpr int MINE = (TILES + WAVES - 1) / WAVES;
+  f32x4_t v[MINE];
+#pragma unroll
+  for (int o = 0; o < MINE; ++o) {
+    const int i = min(wave + o * WAVES, TILES - 1);
+    v[o] = sums[0][i][lane];
+#pragma unroll
+    for (int u = 1; u < WAVES; ++u) v[o] += sums[u][i][lane];
   }
   if (a.splits > 1) {
     // Agent-scope stores, counted in once they are acknowledged; the last workgroup of the columns adds all.
-    const uint32_t bytes = static_cast<uint32_t>(a.splits) * CT * kWave * 16;
+    const uint32_t bytes = static_cast<uint32_t>(a.splits) * TILES * kWave * 16;
     const __amdgpu_buffer_rsrc_t part_of = buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(set) * bytes, bytes);
-    if (wave < CT) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v), part_of, ((split * CT + wave) * kWave + lane) * 16, 0, kAgent);
+#pragma unroll
+    for (int o = 0; o < MINE; ++o) {
+      const int i = min(wave + o * WAVES, TILES - 1);
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, v[o]), part_of, ((split * TILES + i) * kWave + lane) * 16, 0, kAgent);
+    }
     __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0)
     __syncthreads();
     if (threadIdx.x == 0)
       last = __hip_atomic_fetch_add(a.count + set, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(a.splits - 1);
     __syncthreads();
     if (!last) return;
-    if (wave < CT) {
-      v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      for (int s = 0; s < a.splits; ++s)
-        v += __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(part_of, ((s * CT + wave) * kWave + lane) * 16, 0, kAgent));
+#pragma unroll
+    for (int o = 0; o < MINE; ++o) v[o] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; s += 4) {
+      f32x4_t p[MINE][4];
+#pragma unroll
+      for (int o = 0; o < MINE; ++o)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {  // (past the last part: zeros, past the buffer)
+          const int i = min(wave + o * WAVES, TILES - 1);
+          const int at = s + u < a.splits ? (((s + u) * TILES + i) * kWave + lane) * 16 : -16;
+          p[o][u] = __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(part_of, at, 0, kAgent));
+        }
+#pragma unroll
+      for (int o = 0; o < MINE; ++o)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[o] += p[o][u];
     }
     if (threadIdx.x == 0) __hip_atomic_store(a.count + set, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
-  const int tile = set * CT + wave;
-  if (wave < CT && tile < a.N / 16 && lane % 16 < a.M) {
-    const uint32_t lo = float_to_bf16_bits(v[0]) | static_cast<uint32_t>(float_to_bf16_bits(v[1])) << 16;
-    const uint32_t hi = float_to_bf16_bits(v[2]) | static_cast<uint32_t>(float_to_bf16_bits(v[3])) << 16;
-    *reinterpret_cast<uint2*>(a.y + static_cast<size_t>(lane % 16) * a.N + 16 * tile + 4 * q) = make_uint2(lo, hi);
+#pragma unroll
+  for (int o = 0; o < MINE; ++o) {
+    const int i = wave + o * WAVES, tile = set * CT + i % CT, m = 16 * (i / CT) + lane % 16;
+    if (i >= TILES || tile >= a.N / 16 || m >= a.M) continue;
+    const uint32_t lo = float_to_bf16_bits(v[o][0]) | static_cast<uint32_t>(float_to_bf16_bits(v[o][1])) << 16;
+    const uint32_t hi = float_to_bf16_bits(v[o][2]) | static_cast<uint32_t>(float_to_bf16_bits(v[o][3])) << 16;
+    *reinterpret_cast<uint2*>(a.y + static_cast<size_t>(m) * a.N + 16 * tile + 4 * q) = make_uint2(lo, hi);
   }
 }
 
-template <int WAVES, int CT>
+template <int WAVES, int MT, int CT, bool FUSED>
 void few_at(const Fp8Args& a, hipStream_t st) {
-  const dim3 grid((a.N / 16 + CT - 1) / CT * a.splits), block(WAVES * kWave);
-  if (a.xs) hipLaunchKernelGGL((k_fp8_few<WAVES, CT, false>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_fp8_few<WAVES, CT, true>), grid, block, 0, st, a);
+  hipLaunchKernelGGL((k_fp8_few<WAVES, MT, CT, FUSED>), dim3((a.N / 16 + CT - 1) / CT * a.splits), dim3(WAVES * kWave), 0, st, a);
 }
 
 }  // namespace
 
-hipError_t launch_fp8_few(const Fp8Args& a, int tiles, int waves, hipStream_t st) {
-  if (tiles == 2) few_at<4, 2>(a, st);
-  else if (waves == 4) few_at<4, 1>(a, st);
-  else few_at<8, 1>(a, st);
+hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t st) {
+  const int rows = (a.M + 15) / 16;
+  const bool fused = !a.xs;
+  if (rows == 1) {
+    if (columns == 2) fused ? few_at<4, 1, 2, true>(a, st) : few_at<4, 1, 2, false>(a, st);
+    else if (waves == 4) fused ? few_at<4, 1, 1, true>(a, st) : few_at<4, 1, 1, false>(a, st);
+    else fused ? few_at<8, 1, 1, true>(a, st) : few_at<8, 1, 1, false>(a, st);
+  } else if (rows == 2) {
+    columns == 2 ? few_at<4, 2, 2, false>(a, st) : few_at<4, 2, 1, false>(a, st);
+  } else if (rows == 3) {
+    columns == 2 ? few_at<4, 3, 2, false>(a, st) : few_at<4, 3, 1, false>(a, st);
+  } else {
+    columns == 2 ? few_at<4, 4, 2, false>(a, st) : few_at<4, 4, 1, false>(a, st);
+  }
   return hipGetLastError();
 }
 

@@ -22,7 +22,7 @@ from test_gpu_rows import bf16, dev, f64, host, rows8, values8
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
-EXACT = 16  # rows up to which products are not cut
+EXACT = 64  # rows up to which products are not cut
 
 
 def codes_to(codes, bytes_):

@@ -54,6 +54,22 @@ __device__ __forceinline__ uint2 fp8_block(const float (&x)[8], uint32_t* scale_
   return fp8_codes(x, *scale_byte);
 }
 
+// Eight codes times 2^e (given as a float) as bf16 numbers, which hold them exactly for the scale bytes of
+// fp8_plain.
+template <bool HI>
+__device__ __forceinline__ bf16x2_t fp8_two_bf16(uint32_t w, float scale) {
+  return __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI));
+}
+__device__ __forceinline__ bf16x8_t fp8_as_bf16(uint32_t lo, uint32_t hi, float scale) {
+  const bf16x2_t a = fp8_two_bf16<false>(lo, scale), b = fp8_two_bf16<true>(lo, scale), c = fp8_two_bf16<false>(hi, scale),
+                 d = fp8_two_bf16<true>(hi, scale);
+  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Whether codes under this scale are normal bf16 numbers and finite: they span 2^-9 .. 448.
+__device__ __forceinline__ bool fp8_plain(uint32_t scale_byte) { return scale_byte - 16u < 224u; }
+__device__ __forceinline__ float fp8_power(uint32_t scale_byte) { return __uint_as_float(scale_byte << 23); }
+
 // Where the scale byte of block b of row m lies.
 __device__ __forceinline__ size_t fp8_scale_at(int b, int m, int M) {
   return (static_cast<size_t>(b / 4) * M + m) * 4 + b % 4;

@@ -6,6 +6,8 @@
 
 namespace subspec {
 
+constexpr int kFp8ExactRows = 64;  // up to here products are exact
+
 struct Fp8Args {
   const void* x;          // codes [M][K], or bf16 [M][K] where xs is null
   const uint32_t* xs;     // [fp8_words(K)][M]
@@ -26,7 +28,8 @@ struct Fp8Args {
 struct Fp8Plan {
   int few;                 // few rows: tiles of 16 columns a wavefront; 0: the tiles' kernel
   int waves, splits;       // wavefronts of a workgroup and workgroups that share columns then
-  int rows;                // rows of a tile otherwise
+  int small;               // which of the small tiles; 0: the large ones
+  int rows;                // rows of a large tile
   int workers, rounds, left, sharers;
   size_t code_bytes;       // x's codes and scales, where the call makes them
   size_t workspace_bytes;  // completion counters, codes and scales, partial sums; 0: none
@@ -34,6 +37,7 @@ struct Fp8Plan {
 Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus);
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st);
 hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t st);
+hipError_t launch_fp8_small(const Fp8Args& a, int kind, hipStream_t st);
 hipError_t launch_fp8_pack(const uint8_t* codes, int N, int K, uint8_t* tiles, hipStream_t st);
 
 }  // namespace subspec

@@ -9,20 +9,14 @@
 // the only way around it is 16-bit products, at half the rate and with every code converted.
 #include <algorithm>
 
-#include "fp8_device.h"
-#include "kernels_fp8.h"
+#include "fp8_tile.h"
 
 namespace subspec {
 
 namespace {
 
-typedef int i32x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-
-constexpr int kFp8Waves = 8, kFp8Threads = kFp8Waves * kWave;
-constexpr int kAgent = 16;  // sc1: coherent at agent scope
-
 // A tile of MF * WM blocks of 32 rows and NF * WN blocks of 32 columns; a wavefront takes MF by NF of them.
+// STAGES blocks of k are in LDS or on their way.
 template <int MF, int NF, int WM, int WN, int STAGES>
 struct Tile {
   static_assert(WM * WN == kFp8Waves, "wavefronts of a workgroup");
@@ -39,42 +33,12 @@ struct Tile {
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
-// One load straight into LDS: lane l's SIZE bytes land at byte dst + SIZE * l.  Written as assembly because
-// the compiler, where it sees such loads, waits for all of them before it reads LDS again; it has no register
-// result, and the kernel's own waits order it (a wait state after the write of m0 included).
-__device__ __forceinline__ void copy16(const uint8_t* base, uint32_t offset, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(dst), "v"(offset), "s"(base) : "memory", "m0");
-}
-__device__ __forceinline__ void copy4(const uint32_t* from, uint32_t dst) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(dst), "v"(from) : "memory", "m0");
-}
-
-// s_waitcnt: at most `vm` vector memory operations outstanding, no LDS one.
-constexpr int wait_vm_lds(int vm) { return (vm & 15) | (7 << 4) | ((vm >> 4) << 14); }
-template <int VM>
-__device__ __forceinline__ void wait_and_meet() {
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(wait_vm_lds(VM));
-  asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
-__device__ __forceinline__ i32x8_t codes32(const uint8_t* lo, const uint8_t* hi) {
-  const int4 a = *reinterpret_cast<const int4*>(lo), b = *reinterpret_cast<const int4*>(hi);
-  return i32x8_t{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  return float_to_bf16_bits(lo) | static_cast<uint32_t>(float_to_bf16_bits(hi)) << 16;
-}
-
 // Which worker has block p of the left tiles' `total` blocks: worker w's run starts at floor(w total / sharers).
 __device__ __forceinline__ int sharer_of(long long p, long long total, int sharers) {
   return static_cast<int>(((p + 1) * sharers - 1) / total);
 }
 
-template <int MF, int NF, int WM, int WN, int STAGES>
+template <int MF, int NF, int WM, int WN, int STAGES, bool EXACT>
 __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_fp8_tiles(Fp8Args a) {
   using T = Tile<MF, NF, WM, WN, STAGES>;
   extern __shared__ __align__(16) uint8_t lds[];
@@ -137,9 +101,8 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
     for (int j = 0; j < T::kCopies; ++j) {
       const int i = min(wave + kFp8Waves * j, T::BM / 8 + T::BN / 8 - 1);
-      if (i < T::BM / 8) {  // eight rows of 128 codes, 16 bytes c of row r at place c ^ r: no bank twice when read
-        const int r = lane / 8;
-        offset[j] = static_cast<uint32_t>(min(8 * i + r, a.M - 1 - m0)) * a.K + 16 * (lane % 8 ^ r);
+      if (i < T::BM / 8) {
+        offset[j] = static_cast<uint32_t>(min(8 * i + lane / 8, a.M - 1 - m0)) * a.K + fp8_chunk(lane);
       } else {
         const int u = i - T::BM / 8;
         offset[j] = static_cast<uint32_t>(min(u / 2, a.N / 16 - 1 - n0 / 16)) * 16 * a.K + 1024 * (u % 2) + 16 * lane;
@@ -157,7 +120,8 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
     for (int j = 0; j < T::kCopies; ++j) {
       const int i = min(wave + kFp8Waves * j, T::BM / 8 + T::BN / 8 - 1);
-      copy16(i < T::BM / 8 ? xbase : wbase, offset[j], at + 1024 * i);
+      if (i < T::BM / 8) copy16<false>(xbase, offset[j], at + 1024 * i);
+      else copy16<(EXACT && MF == 1)>(wbase, offset[j], at + 1024 * i);
     }
     copy4(sbase, at + T::kXBytes + T::kWBytes + 256 * min(wave, T::kScaleCopies - 1));
     xbase += 128;
@@ -169,23 +133,14 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   for (; issued < T::kAhead && issued < steps; ++issued) issue();
 
   // --- products
-  const int r = lane % 32, half = lane / 32, wm = wave % WM, wn = wave / WM;
-  uint32_t xat[4];  // 16 bytes 4 s + 2 half + t of row r
-#pragma unroll
-  for (int u = 0; u < 4; ++u) xat[u] = (32 * MF * wm + r) * 128 + 16 * ((4 * (u / 2) + 2 * half + u % 2) ^ (r % 8));
-  const uint32_t wat = T::kXBytes + 32 * NF * wn * 128 + r / 16 * 2048 + 512 * half + 16 * (r % 16);
-  const uint32_t xsat = T::kXBytes + T::kWBytes + 4 * (32 * MF * wm + r), wsat = T::kXBytes + T::kWBytes + 4 * (T::BM + 32 * NF * wn + r);
+  const Fp8Lane at = fp8_lane(lane);
+  const int half = lane / 32, wm = wave % WM, wn = wave / WM;
   f32x16_t acc[NF][MF];
   int step = 0;
   uint32_t slot = 0;
   for (int s = 0; s < segments; ++s) {
     const Segment g = segment(s);
-#pragma unroll
-    for (int i = 0; i < NF; ++i)
-#pragma unroll
-      for (int j = 0; j < MF; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    fp8_clear(acc);
     for (int kb = g.kb0; kb < g.kb1; ++kb, ++step) {
       // Loads complete in order: once the later stages' are all that is outstanding, this stage is in LDS; the
       // stage before it is read by everyone and takes the next copies.
@@ -193,25 +148,9 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
       else wait_and_meet<0>();
       if (issued < steps) issue(), ++issued;
       const uint8_t* st = lds + slot * T::kStage;
-      uint32_t xs[MF], ws[NF];
-#pragma unroll
-      for (int j = 0; j < MF; ++j) xs[j] = st[xsat + 128 * j + kb % 4];
-#pragma unroll
-      for (int i = 0; i < NF; ++i) ws[i] = st[wsat + 128 * i + kb % 4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        i32x8_t wf[NF], xf[MF];
-#pragma unroll
-        for (int i = 0; i < NF; ++i) wf[i] = codes32(st + wat + 4096 * i + 1024 * h, st + wat + 4096 * i + 1024 * h + 256);
-#pragma unroll
-        for (int j = 0; j < MF; ++j) xf[j] = codes32(st + xat[2 * h] + 4096 * j, st + xat[2 * h + 1] + 4096 * j);
-#pragma unroll
-        for (int j = 0; j < MF; ++j)
-#pragma unroll
-          for (int i = 0; i < NF; ++i)
-            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wf[i], xf[j], acc[i][j], 0, 0, 0, static_cast<int>(ws[i]), 0,
-                                                                       static_cast<int>(xs[j]));
-      }
+      const uint8_t* words = st + T::kXBytes + T::kWBytes;
+      fp8_block_products<MF, NF, EXACT>(acc, st + 4096 * MF * wm, st + T::kXBytes + 4096 * NF * wn, words + 128 * MF * wm,
+                                        words + 4 * T::BM + 128 * NF * wn, at, half, kb % 4);
       slot = slot + 1 == STAGES ? 0 : slot + 1;
     }
 
@@ -225,16 +164,7 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
       auto part = [&](int who, int seg) __attribute__((always_inline)) {
         return buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(2 * who + seg) * kPart, kPart);
       };
-      const __amdgpu_buffer_rsrc_t mine = part(w, s);
-#pragma unroll
-      for (int i = 0; i < NF; ++i)
-#pragma unroll
-        for (int j = 0; j < MF; ++j)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            __builtin_amdgcn_raw_buffer_store_b128(
-                __builtin_bit_cast(u32x4_t, f32x4_t{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]}), mine,
-                16 * threadIdx.x, ((i * MF + j) * 4 + q) * 16 * kFp8Threads, kAgent);
+      fp8_store_part(acc, part(w, s), threadIdx.x, kFp8Threads);
       int* last = reinterpret_cast<int*>(lds + static_cast<size_t>(STAGES) * T::kStage);
       wait_and_meet<0>();
       const int w0 = sharer_of(static_cast<long long>(t) * KB, total, a.sharers);
@@ -243,40 +173,12 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
         *last = __hip_atomic_fetch_add(a.count + t, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(w1 - w0);
       __syncthreads();
       if (!*last) continue;
-      for (int who = w0; who <= w1; ++who) {
-        // the tile is the first of a worker's run or its second
-        const __amdgpu_buffer_rsrc_t from_part = part(who, static_cast<int>(who * total / a.sharers / KB) == t ? 0 : 1);
-#pragma unroll
-        for (int i = 0; i < NF; ++i)
-#pragma unroll
-          for (int j = 0; j < MF; ++j)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const f32x4_t v = __builtin_bit_cast(
-                  f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(from_part, 16 * threadIdx.x, ((i * MF + j) * 4 + q) * 16 * kFp8Threads, kAgent));
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = who == w0 ? v[e] : acc[i][j][4 * q + e] + v[e];
-            }
-      }
+      // (the tile is the first of a worker's run or its second)
+      fp8_add_parts(acc, w1 - w0 + 1, [&](int k) { return part(w0 + k, static_cast<int>((w0 + k) * total / a.sharers / KB) == t ? 0 : 1); },
+                    threadIdx.x, kFp8Threads);
       if (threadIdx.x == 0) __hip_atomic_store(a.count + t, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    // A lane holds columns 8 q + 4 half + 0 .. 3 of one row; swapped with the other half's, 8 in a row.
-#pragma unroll
-    for (int j = 0; j < MF; ++j) {
-      const int m = m0 + 32 * (MF * wm + j) + r;
-#pragma unroll
-      for (int i = 0; i < NF; ++i) {
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-          const int n = n0 + 32 * (NF * wn + i) + 16 * p;
-          const f32x16_t& c = acc[i][j];
-          const auto lo = __builtin_amdgcn_permlane32_swap(pack_bf16(c[8 * p], c[8 * p + 1]), pack_bf16(c[8 * p + 4], c[8 * p + 5]), false, false);
-          const auto hi = __builtin_amdgcn_permlane32_swap(pack_bf16(c[8 * p + 2], c[8 * p + 3]), pack_bf16(c[8 * p + 6], c[8 * p + 7]), false, false);
-          if (m < a.M && n < a.N)
-            *reinterpret_cast<uint4*>(a.y + static_cast<size_t>(m) * a.N + n + 8 * half) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
-        }
-      }
-    }
+    fp8_results(acc, a, m0 + 32 * MF * wm, n0 + 32 * NF * wn, lane);
   }
 }
 
@@ -291,51 +193,113 @@ __global__ __launch_bounds__(256) void k_fp8_pack(const uint8_t* codes, int N, i
   *reinterpret_cast<uint4*>(tiles + 16 * t) = *reinterpret_cast<const uint4*>(codes + n * K + k);
 }
 
-constexpr int kFewRows = 64;   // up to here kernels_fp8_few.hip
 constexpr int kColumns = 256;  // of every tile
 
-template <int MF, int NF, int WM, int WN, int STAGES>
+template <int MF, int NF, int WM, int WN, int STAGES, bool EXACT>
 hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
   using T = Tile<MF, NF, WM, WN, STAGES>;
   static_assert(T::BN == kColumns, "columns of a tile");
-  static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_fp8_tiles<MF, NF, WM, WN, STAGES>),
+  static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_fp8_tiles<MF, NF, WM, WN, STAGES, EXACT>),
                                                    hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
   if (set != hipSuccess) return set;
-  hipLaunchKernelGGL((k_fp8_tiles<MF, NF, WM, WN, STAGES>), dim3(a.workers), dim3(kFp8Threads), T::kLds, st, a);
+  hipLaunchKernelGGL((k_fp8_tiles<MF, NF, WM, WN, STAGES, EXACT>), dim3(a.workers), dim3(kFp8Threads), T::kLds, st, a);
   return hipGetLastError();
 }
 
-size_t fp8_row_bytes(int M, int K) {
-  return (static_cast<size_t>(M) * K + static_cast<size_t>(fp8_words(K)) * M * 4 + 255) & ~size_t(255);
+// What the launches cost, in microseconds: a call, a workgroup's stage of k when few and when all compute
+// units have one, a workgroup's start and end, joining parts of K (and their bytes, written and read), and
+// bytes of weights from memory.  Fitted to sweeps of every shape over 60 sizes; the choice below is the
+// cheapest by them.
+constexpr float kCall = 4.f, kTurn = 2.f, kJoin = 1.5f, kJoinBytes = 6.5e6f, kWeightBytes = 5e6f;
+struct SmallCost {
+  int kind, rows, columns, blocks;  // launch_fp8_small's kind; a workgroup's tile and blocks of k a stage
+  float few, all;
+  bool exact;
+};
+constexpr SmallCost kSmall[] = {
+    {1, 32, 64, 4, 0.6f, 0.95f, true},   {2, 64, 64, 4, 1.4f, 1.5f, true},     {3, 64, 128, 2, 1.4f, 1.5f, true},
+    {4, 64, 64, 4, 0.65f, 1.4f, false},  {5, 64, 128, 2, 0.6f, 0.85f, false},  {6, 96, 128, 2, 0.9f, 1.15f, false},
+    {7, 128, 128, 1, 0.5f, 0.66f, false},
+};
+struct LargeCost {
+  int rows;
+  float step;
+  bool exact;
+};
+constexpr LargeCost kLarge[] = {{32, 1.0f, true}, {64, 1.5f, true}, {128, 1.04f, false}, {192, 1.45f, false}, {256, 1.88f, false}};
+
+// At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
+// that already spreads over the compute units, else two, which share the rows' conversion; K cut over the eight
+// wavefronts of a workgroup where it is short, else over four and over workgroups too, as many as stay resident.
+// (1 row: 3584 x 3584 6.0 us with one tile and eight wavefronts, 6.9 with two tiles, 7.1 with four wavefronts;
+// 3584 x 18944 17.6 with two tiles, four wavefronts and four workgroups, 19.6 with one tile and one workgroup.)
+void few_plan(int M, int N, int K, bool rows8, int cus, Fp8Plan* p) {
+  const int tiles = N / 16, KB = K / 128;
+  const bool longer = KB > 64;
+  p->few = M > 16 || (tiles <= cus && !longer) ? 1 : 2;
+  const int sets = (tiles + p->few - 1) / p->few;
+  p->waves = M > 16 || longer || sets > cus ? 4 : 8;
+  p->splits = longer || M > 16 ? std::max(1, std::min((rows8 ? 3 : 2) * cus / sets, std::min(KB / 16, 64))) : 1;
 }
 
 }  // namespace
 
 Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
   Fp8Plan p{};
-  if (M <= kFewRows) {
-    const int tiles = N / 16, units = (K + 255) / 256;
-    p.few = tiles >= 4 * cus ? 2 : 1;
-    p.waves = M > 16 || tiles > cus ? 4 : 8;
-    const int sets = (tiles + p.few - 1) / p.few, rows = (M + 15) / 16;
-    p.splits = std::max(1, std::min({(p.waves == 4 ? 4 : 1) * cus / sets, units / (4 * p.waves), 64}));
-    size_t at = kSplitCounterBytes;
-    if (!rows8 && M > 16) at += p.code_bytes = fp8_row_bytes(M, K);
-    if (p.splits > 1) at += static_cast<size_t>(sets) * p.splits * rows * p.few * kWave * 16;
-    p.workspace_bytes = at > kSplitCounterBytes ? at : 0;
-    return p;
+  const int KB = K / 128;
+  const bool exact = M <= kFp8ExactRows;
+  size_t parts = 0;
+  if (M <= 16 || (exact && static_cast<long long>(N) * K <= 1 << 21)) {
+    few_plan(M, N, K, rows8, cus, &p);
+    if (p.splits > 1) parts = static_cast<size_t>((N / 16 + p.few - 1) / p.few) * p.splits * ((M + 15) / 16) * p.few * kWave * 16;
+  } else {
+    const float memory = static_cast<float>(N) * K / kWeightBytes;
+    float best = 1e30f;
+    for (const SmallCost& c : kSmall) {
+      if (c.exact != exact) continue;
+      const long long tiles = static_cast<long long>((M + c.rows - 1) / c.rows) * ((N + c.columns - 1) / c.columns);
+      if (tiles > 64ll * cus) continue;
+      const int units = (KB + c.blocks - 1) / c.blocks;
+      const int splits = std::max(1, std::min(cus / static_cast<int>(tiles), units));
+      const long long groups = tiles * splits, turns = (groups + cus - 1) / cus;
+      const float step = std::max(c.few, c.all * std::min<long long>(groups, cus) / cus);
+      const size_t bytes = splits > 1 ? static_cast<size_t>(groups) * c.rows * c.columns * 4 : 0;
+      const float cost = kCall + std::max(memory, turns * ((units + splits - 1) / splits * step + kTurn)) + (bytes ? kJoin + 2 * bytes / kJoinBytes : 0.f);
+      if (cost < best) {
+        best = cost;
+        p.small = c.kind;
+        p.splits = splits;
+        parts = bytes;
+      }
+    }
+    for (const LargeCost& c : kLarge) {
+      if (c.exact != exact || (exact && c.rows < M)) continue;
+      const long long tiles = static_cast<long long>((M + c.rows - 1) / c.rows) * ((N + kColumns - 1) / kColumns);
+      const int rounds = static_cast<int>(tiles / cus), left = static_cast<int>(tiles % cus);
+      // The tiles left over whole, in as many equal runs each as there are compute units for, or in runs of all
+      // tiles over all compute units.
+      for (int way = 0; way < (left ? 3 : 1); ++way) {
+        const int sharers = static_cast<int>(std::min<long long>(way == 0 ? left : way == 1 ? cus / left * left : cus, static_cast<long long>(left) * KB));
+        if (way && sharers <= left) continue;
+        const long long steps = static_cast<long long>(rounds) * KB + (left ? (static_cast<long long>(left) * KB + sharers - 1) / sharers : 0);
+        const size_t runs = sharers > left ? static_cast<size_t>(sharers) * 2 : 0;  // their places in the workspace
+        const float moved = sharers <= left ? 0.f : (sharers % left ? sharers + left : sharers) * 2.f * c.rows * kColumns * 4;
+        const float cost = kCall + std::max(memory, steps * c.step) + (runs ? kJoin + moved / kJoinBytes : 0.f);
+        if (cost < best) {
+          best = cost;
+          p.small = 0;
+          p.rows = c.rows;
+          p.rounds = rounds;
+          p.left = left;
+          p.sharers = sharers;
+          p.workers = rounds ? cus : sharers;
+          parts = runs * c.rows * kColumns * 4;
+        }
+      }
+    }
   }
-  p.rows = M <= 128 ? 128 : 256;
-  const long long tiles = static_cast<long long>((M + p.rows - 1) / p.rows) * ((N + kColumns - 1) / kColumns);
-  const long long KB = K / 128;
-  p.rounds = static_cast<int>(tiles / cus);
-  p.left = static_cast<int>(tiles % cus);
-  p.sharers = static_cast<int>(std::min<long long>(cus, p.left * KB));
-  p.workers = p.rounds ? cus : p.sharers;
-  size_t at = kSplitCounterBytes;
-  if (!rows8) at += p.code_bytes = fp8_row_bytes(M, K);
-  if (p.sharers > p.left) at += static_cast<size_t>(p.sharers) * 2 * p.rows * kColumns * 4;
-  p.workspace_bytes = at > kSplitCounterBytes ? at : 0;
+  if (!rows8 && !(p.few && M <= 16)) p.code_bytes = (static_cast<size_t>(M) * K + static_cast<size_t>(fp8_words(K)) * M * 4 + 255) & ~size_t(255);
+  if (p.code_bytes + parts) p.workspace_bytes = kSplitCounterBytes + p.code_bytes + parts;
   return p;
 }
 
@@ -357,6 +321,10 @@ hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipSt
     a.splits = p.splits;
     return launch_fp8_few(a, p.few, p.waves, st);
   }
+  if (p.small) {
+    a.splits = p.splits;
+    return launch_fp8_small(a, p.small, st);
+  }
   a.tiles_m = (a.M + p.rows - 1) / p.rows;
   a.tiles_n = (a.N + kColumns - 1) / kColumns;
   a.workers = p.workers;
@@ -364,8 +332,11 @@ hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipSt
   a.left = p.left;
   a.sharers = p.sharers;
   switch (p.rows) {
-    case 128: return tiles_at<4, 1, 1, 8, 3>(a, st);
-    default: return tiles_at<4, 2, 2, 4, 2>(a, st);
+    case 32: return tiles_at<1, 1, 1, 8, 4, true>(a, st);
+    case 64: return tiles_at<2, 1, 1, 8, 3, true>(a, st);
+    case 128: return tiles_at<2, 2, 2, 4, 3, false>(a, st);
+    case 192: return tiles_at<3, 2, 2, 4, 2, false>(a, st);
+    default: return tiles_at<4, 2, 2, 4, 2, false>(a, st);
   }
 }
 

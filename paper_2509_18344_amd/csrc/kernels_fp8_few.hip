@@ -1,7 +1,6 @@
 // The product in 8-bit floating point for few rows, where the weights' bytes are all that counts:
-// codes become bf16 numbers on the way (exactly) and meet in the 16-bit matrix instruction, whose products
-// are exact and whose sums are in fp32, a block of 128 k at a time; the block's two powers of two are
-// applied to its sum.  (The 8-bit matrix instruction would cut products to 13 bits, and its rate is not
+// scaled codes become bf16 numbers on the way (exactly) and meet in the 16-bit matrix instruction, whose
+// products are exact and whose sums are in fp32.  (The 8-bit matrix instruction would cut products to 13 bits, and its rate is not
 // needed here: at 5 TB/s a SIMD has about 1000 cycles for a tile of 16 columns and 128 k.)
 //
 // A wavefront takes CT tiles of 16 columns and a run of K, its weights straight from memory to registers, a
@@ -18,16 +17,6 @@ namespace {
 
 constexpr int kUnit = 2;    // blocks that a wavefront loads at once, one unit ahead of the products
 constexpr int kAgent = 16;  // sc1: coherent at agent scope
-
-// Two codes (the low or the high half of w) as bf16 numbers.
-template <bool HI>
-__device__ __forceinline__ bf16x2_t two_bf16(uint32_t w) {
-  return __builtin_bit_cast(bf16x2_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, HI));
-}
-__device__ __forceinline__ bf16x8_t eight_bf16(uint32_t lo, uint32_t hi) {
-  const bf16x2_t a = two_bf16<false>(lo), b = two_bf16<true>(lo), c = two_bf16<false>(hi), d = two_bf16<true>(hi);
-  return bf16x8_t{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 
 __device__ __forceinline__ uint32_t max_across_rows(uint32_t v) {  // over the lanes l, l ^ 16, l ^ 32, l ^ 48
   const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
@@ -60,9 +49,13 @@ __device__ __forceinline__ XBlock<FUSED> load_x(const uint8_t* row, int kb) {
   return b;
 }
 
-// The block's codes as four operands of the matrix instruction, and the scale byte.
+// The block's codes, 32 a lane, and (of bf16 rows) its scale byte.
+struct Codes {
+  uint32_t v[8];
+};
 template <bool FUSED>
-__device__ __forceinline__ void x_operands(const XBlock<FUSED>& b, bf16x8_t (&out)[4], uint32_t* byte) {
+__device__ __forceinline__ Codes x_codes(const XBlock<FUSED>& b, uint32_t* byte) {
+  Codes out;
   if constexpr (FUSED) {
     // Magnitudes of pairs as 16-bit whole numbers, which order as the numbers do.
     typedef unsigned short u16x2_t __attribute__((ext_vector_type(2)));
@@ -87,27 +80,32 @@ __device__ __forceinline__ void x_operands(const XBlock<FUSED>& b, bf16x8_t (&ou
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const uint2 c = fp8_codes(x[u], *byte);
-        out[u] = eight_bf16(c.x, c.y);
+        out.v[2 * u] = c.x;
+        out.v[2 * u + 1] = c.y;
       }
-      return;
+      return out;
     }
     *byte = fp8_scale_byte(__uint_as_float(most << 16));
-    const float scale = __uint_as_float(*byte << 23);  // 2^e
+    const float scale = fp8_power(*byte);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < 8; ++u) {
       typedef short s16x2_t __attribute__((ext_vector_type(2)));
-      const uint32_t w[4] = {b.v[u][0], b.v[u][1], b.v[u][2], b.v[u][3]};
-      s16x2_t lo = {0, 0}, hi = {0, 0};
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2_t, w[0]), scale, false);
-      lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2_t, w[1]), scale, true);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, w[2]), scale, false);
-      hi = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(hi, __builtin_bit_cast(bf16x2_t, w[3]), scale, true);
-      out[u] = eight_bf16(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
+      const uint32_t w[2] = {b.v[u / 2][2 * (u % 2)], b.v[u / 2][2 * (u % 2) + 1]};
+      s16x2_t c = {0, 0};
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2_t, w[0]), scale, false);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(c, __builtin_bit_cast(bf16x2_t, w[1]), scale, true);
+      out.v[u] = __builtin_bit_cast(uint32_t, c);
     }
   } else {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) out[u] = eight_bf16(b.v[u / 2][2 * (u % 2)], b.v[u / 2][2 * (u % 2) + 1]);
+    for (int u = 0; u < 8; ++u) out.v[u] = b.v[u / 4][u % 4];
   }
+  return out;
+}
+
+__device__ __forceinline__ void operands(const Codes& c, float scale, bf16x8_t (&out)[4]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) out[u] = fp8_as_bf16(c.v[2 * u], c.v[2 * u + 1], scale);
 }
 
 // MT tiles of 16 rows, CT of 16 columns a wavefront.
@@ -135,11 +133,11 @@ __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
   for (int c = 0; c < CT; ++c) {
     const int tile = min(set * CT + c, a.N / 16 - 1);
     wt[c] = a.w + static_cast<size_t>(tile) * KB * 2048 + 16 * lane;
-    wst[c] = a.ws + 16 * tile + 4 * q;
+    wst[c] = a.ws + 16 * tile + lane % 16;
   }
   struct Weights {
     u32x4_t w[CT][kUnit][2];
-    u32x4_t s[CT];
+    uint32_t s[CT];
   };
   struct Rows {
     XBlock<FUSED> b[MT];
@@ -154,7 +152,7 @@ __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
         r.w[c][j][0] = __builtin_nontemporal_load(p);
         r.w[c][j][1] = __builtin_nontemporal_load(p + 64);
       }
-      r.s[c] = *reinterpret_cast<const u32x4_t*>(wst[c] + static_cast<size_t>(kUnit * g / 4) * a.N);
+      r.s[c] = wst[c][static_cast<size_t>(kUnit * g / 4) * a.N];
     }
   };
   auto load_rows = [&](int kb, Rows& r) __attribute__((always_inline)) {
@@ -185,24 +183,45 @@ __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
       const Rows x = rows;
       if (kb + 1 < kb1) load_rows(kb + 1, rows);
       const int shift = 8 * (kb % 4);
+      Codes xc[MT];
+      uint32_t xb[MT], wb[CT];
+      bool plain = true;
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+        xb[t] = FUSED ? 0u : x.s[t] >> shift & 255u;
+        xc[t] = x_codes<FUSED>(x.b[t], &xb[t]);
+        plain &= fp8_plain(xb[t]);
+      }
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        wb[c] = now.s[c] >> shift & 255u;
+        plain &= fp8_plain(wb[c]);
+      }
+      plain = __all(plain);
       bf16x8_t w[CT][4];
 #pragma unroll
-      for (int c = 0; c < CT; ++c)
+      for (int c = 0; c < CT; ++c) {
+        Codes wc;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) w[c][u] = eight_bf16(now.w[c][j][u / 2][2 * (u % 2)], now.w[c][j][u / 2][2 * (u % 2) + 1]);
+        for (int u = 0; u < 8; ++u) wc.v[u] = now.w[c][j][u / 4][u % 4];
+        operands(wc, plain ? fp8_power(wb[c]) : 1.f, w[c]);
+      }
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
         bf16x8_t xo[4];
-        uint32_t xs = FUSED ? 0u : x.s[t] >> shift & 255u;
-        x_operands<FUSED>(x.b[t], xo, &xs);
+        operands(xc[t], plain ? fp8_power(xb[t]) : 1.f, xo);
 #pragma unroll
         for (int c = 0; c < CT; ++c) {
-          f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+          f32x4_t s = plain ? acc[t][c] : f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int u = 0; u < 4; ++u) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c][u], xo[u], s, 0, 0, 0);
-          // this lane's row of x, and four columns
+          if (plain) {
+            acc[t][c] = s;
+          } else {  // a scale so far from 1 that bf16 would not hold the codes: this lane's row of x and four columns afterwards
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[t][c][e] += ldexpf(s[e], static_cast<int>(xs + (now.s[c][e] >> shift & 255u)) - 254);
+            for (int e = 0; e < 4; ++e)
+              acc[t][c][e] += ldexpf(s[e], static_cast<int>(xb[t] + __shfl(wb[c], 4 * q + e)) - 254);
+          }
         }
       }
     }
@@ -277,15 +296,15 @@ hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t 
   const int rows = (a.M + 15) / 16;
   const bool fused = !a.xs;
   if (rows == 1) {
-    if (columns == 2) fused ? few_at<4, 1, 2, true>(a, st) : few_at<4, 1, 2, false>(a, st);
-    else if (waves == 4) fused ? few_at<4, 1, 1, true>(a, st) : few_at<4, 1, 1, false>(a, st);
+    if (columns == 2 && waves == 8) fused ? few_at<8, 1, 2, true>(a, st) : few_at<8, 1, 2, false>(a, st);
+    else if (columns == 2) fused ? few_at<4, 1, 2, true>(a, st) : few_at<4, 1, 2, false>(a, st);
     else fused ? few_at<8, 1, 1, true>(a, st) : few_at<8, 1, 1, false>(a, st);
   } else if (rows == 2) {
-    columns == 2 ? few_at<4, 2, 2, false>(a, st) : few_at<4, 2, 1, false>(a, st);
+    few_at<4, 2, 1, false>(a, st);
   } else if (rows == 3) {
-    columns == 2 ? few_at<4, 3, 2, false>(a, st) : few_at<4, 3, 1, false>(a, st);
+    few_at<4, 3, 1, false>(a, st);
   } else {
-    columns == 2 ? few_at<4, 4, 2, false>(a, st) : few_at<4, 4, 1, false>(a, st);
+    few_at<4, 4, 1, false>(a, st);
   }
   return hipGetLastError();
 }

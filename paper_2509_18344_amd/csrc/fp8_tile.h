@@ -54,9 +54,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return float_to_bf16_bits(lo) | static_cast<uint32_t>(float_to_bf16_bits(hi)) << 16;
 }
 
-// A block of k in LDS: eight rows of x in 1024 bytes, 16 bytes c of row r at place c ^ (r % 8) of its 128 (no
-// bank twice when a wavefront reads them), the weight tiles as they are in memory, and the scale words.
-__device__ __forceinline__ uint32_t fp8_chunk(int lane) { return 16 * (lane % 8 ^ lane / 8); }  // of row lane / 8, to place lane % 8
+// A block of k in LDS: eight rows of x in 1024 bytes, 16 bytes c of row r at place c ^ (r / 2 % 8) of its 128 (no
+// bank twice in the 16 rows that are read at once), the weight tiles as they are in memory, and the scale words.
+// What lane `lane` of copy i (rows 8 i ..) takes to place lane % 8 of row lane / 8.
+__device__ __forceinline__ uint32_t fp8_chunk(int lane, int i) { return 16 * (lane % 8 ^ (4 * (i % 2) + lane / 16)); }
 
 // Where a lane reads: 32 rows of either side start at `x` and `w`, words at `xs` and `ws`.
 struct Fp8Lane {
@@ -67,7 +68,7 @@ __device__ __forceinline__ Fp8Lane fp8_lane(int lane) {
   const int r = lane % 32, half = lane / 32;
   Fp8Lane l;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) l.x[u] = r * 128 + 16 * ((4 * (u / 2) + 2 * half + u % 2) ^ (r % 8));
+  for (int u = 0; u < 4; ++u) l.x[u] = r * 128 + 16 * ((4 * (u / 2) + 2 * half + u % 2) ^ (r / 2 % 8));
   l.w = r / 16 * 2048 + 512 * half + 16 * (r % 16);
   l.s = 4 * r;
   return l;
@@ -167,6 +168,49 @@ __device__ __forceinline__ void fp8_clear(f32x16_t (&acc)[NF][MF]) {
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 }
 
+// Which worker has block p of the left tiles' `total` blocks: worker w's run starts at floor(w total / sharers).
+__device__ __forceinline__ int sharer_of(long long p, long long total, int sharers) {
+  return static_cast<int>(((p + 1) * sharers - 1) / total);
+}
+
+// A worker's segments: up to two cut tiles, then whole ones.
+struct Fp8Segment {
+  int tile, kb0, kb1;
+};
+struct Fp8Work {
+  long long total, from, to;  // blocks of the left tiles; this worker's
+  int KB, w, first, cut, segments, left0, step;
+
+  __device__ __forceinline__ explicit Fp8Work(const Fp8Args& a) : KB(a.K / 128), left0(a.rounds * a.workers), step(a.workers) {
+    // Workgroups b, b + 8, .. run on one XCD: it takes neighbouring workers, so that its L2 serves tiles of the
+    // same rows and columns.
+    const int b = blockIdx.x, per = a.workers / 8;
+    w = a.workers % 8 ? b : (b % 8) * per + b / 8;
+    total = static_cast<long long>(a.left) * KB;
+    from = to = 0;
+    if (w < a.sharers) from = w * total / a.sharers, to = (w + 1) * total / a.sharers;
+    first = static_cast<int>(from / KB);
+    cut = to == from ? 0 : (to - 1) / KB > first ? 2 : 1;
+    segments = cut + a.rounds;
+  }
+  __device__ __forceinline__ Fp8Segment segment(int s) const {
+    if (s >= cut) return {w + (s - cut) * step, 0, KB};
+    const int t = first + s;
+    const long long at = static_cast<long long>(t) * KB;
+    return {left0 + t, static_cast<int>(max(from, at) - at), static_cast<int>(min(to, at + KB) - at)};
+  }
+  __device__ __forceinline__ int blocks() const {
+    return static_cast<int>(to - from) + (segments - cut) * KB;
+  }
+};
+
+// Tiles in bands of eight along the rows, columns inside: neighbouring workers share either.
+__device__ __forceinline__ void fp8_place(const Fp8Args& a, int tile, int rows, int columns, int* m0, int* n0) {
+  const int band = tile / (8 * a.tiles_n), rest = tile - band * 8 * a.tiles_n, high = min(8, a.tiles_m - 8 * band);
+  *n0 = rest / high * columns;
+  *m0 = (8 * band + rest % high) * rows;
+}
+
 // Results of rows m0 .. and columns n0 .. : a lane's four columns of a row, swapped with the other half's, are
 // eight in a row.
 template <int MF, int NF>
@@ -231,6 +275,30 @@ __device__ __forceinline__ void fp8_add_parts(f32x16_t (&acc)[NF][MF], int count
           for (int e = 0; e < 16; ++e) acc[i][j][e] += v[o][j][e / 4][e % 4];
     }
   }
+}
+
+// A cut tile's sums, called by the whole workgroup.  Every worker of the tile stores its own with agent-scope
+// stores and counts itself in once they are acknowledged; the last, for which this returns true, has the sum in
+// the order of k.
+template <int MF, int NF>
+__device__ __forceinline__ bool fp8_join(f32x16_t (&acc)[NF][MF], const Fp8Args& a, const Fp8Work& work, int s, int tile, uint32_t part_bytes, int* last) {
+  const int t = tile - work.left0;
+  auto part = [&](int who, int seg) __attribute__((always_inline)) {
+    return buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(2 * who + seg) * part_bytes, part_bytes);
+  };
+  fp8_store_part(acc, part(work.w, s), threadIdx.x, kFp8Threads);
+  wait_and_meet<0>();
+  const int w0 = sharer_of(static_cast<long long>(t) * work.KB, work.total, a.sharers);
+  const int w1 = sharer_of(static_cast<long long>(t) * work.KB + work.KB - 1, work.total, a.sharers);
+  if (threadIdx.x == 0)
+    *last = __hip_atomic_fetch_add(a.count + t, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(w1 - w0);
+  __syncthreads();
+  if (!*last) return false;
+  // (the tile is the first of a worker's run or its second)
+  fp8_add_parts(acc, w1 - w0 + 1, [&](int k) { return part(w0 + k, static_cast<int>((w0 + k) * work.total / a.sharers / work.KB) == t ? 0 : 1); },
+                threadIdx.x, kFp8Threads);
+  if (threadIdx.x == 0) __hip_atomic_store(a.count + t, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
 }
 
 }  // namespace subspec

@@ -33,52 +33,13 @@ struct Tile {
   static_assert(kLds <= 160 * 1024, "LDS of a compute unit");
 };
 
-// Which worker has block p of the left tiles' `total` blocks: worker w's run starts at floor(w total / sharers).
-__device__ __forceinline__ int sharer_of(long long p, long long total, int sharers) {
-  return static_cast<int>(((p + 1) * sharers - 1) / total);
-}
-
 template <int MF, int NF, int WM, int WN, int STAGES, bool EXACT>
 __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_fp8_tiles(Fp8Args a) {
   using T = Tile<MF, NF, WM, WN, STAGES>;
   extern __shared__ __align__(16) uint8_t lds[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int KB = a.K / 128;
-  // Workgroups b, b + 8, .. run on one XCD: it takes neighbouring workers, so that its L2 serves tiles of the
-  // same rows and columns.
-  const int b = blockIdx.x, per = a.workers / 8, w = a.workers % 8 ? b : (b % 8) * per + b / 8;
-
-  // --- this worker's segments: up to two cut tiles, then whole ones
-  const long long total = static_cast<long long>(a.left) * KB;
-  long long from = 0, to = 0;
-  if (w < a.sharers) from = w * total / a.sharers, to = (w + 1) * total / a.sharers;
-  const int first = static_cast<int>(from / KB), cut = to == from ? 0 : (to - 1) / KB > first ? 2 : 1;
-  const int segments = cut + a.rounds;
-  struct Segment {
-    int tile, kb0, kb1;
-  };
-  auto segment = [&](int s) __attribute__((always_inline)) {
-    Segment g;
-    if (s >= cut) {
-      g = {w + (s - cut) * a.workers, 0, KB};
-    } else {
-      const int t = first + s;
-      const long long at = static_cast<long long>(t) * KB;
-      g = {a.rounds * a.workers + t, static_cast<int>(max(from, at) - at), static_cast<int>(min(to, at + KB) - at)};
-    }
-    return g;
-  };
-  // Tiles in bands of eight along the rows, columns inside: neighbouring workers share either.
-  auto place = [&](int tile, int* m0, int* n0) __attribute__((always_inline)) {
-    const int band = tile / (8 * a.tiles_n), rest = tile - band * 8 * a.tiles_n, high = min(8, a.tiles_m - 8 * band);
-    *n0 = rest / high * T::BN;
-    *m0 = (8 * band + rest % high) * T::BM;
-  };
-  int steps = 0;
-  for (int s = 0; s < segments; ++s) {
-    const Segment g = segment(s);
-    steps += g.kb1 - g.kb0;
-  }
+  const Fp8Work work(a);
+  const int steps = work.blocks();
   if (!steps) return;
 
   // --- copies into the ring of stages
@@ -90,11 +51,11 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   long long sstep = 0;
   uint32_t offset[T::kCopies];
   auto open = [&]() __attribute__((always_inline)) {
-    const Segment g = segment(++iseg);
+    const Fp8Segment g = work.segment(++iseg);
     ikb = g.kb0;
     iend = g.kb1;
     int m0, n0;
-    place(g.tile, &m0, &n0);
+    fp8_place(a, g.tile, T::BM, T::BN, &m0, &n0);
     xbase = static_cast<const uint8_t*>(a.x) + static_cast<size_t>(m0) * a.K + 128ll * ikb;
     wbase = a.w + static_cast<size_t>(n0) * a.K + 2048ll * ikb;
     // Rows and columns past the last: that one again (their results go nowhere).
@@ -102,7 +63,7 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
     for (int j = 0; j < T::kCopies; ++j) {
       const int i = min(wave + kFp8Waves * j, T::BM / 8 + T::BN / 8 - 1);
       if (i < T::BM / 8) {
-        offset[j] = static_cast<uint32_t>(min(8 * i + lane / 8, a.M - 1 - m0)) * a.K + fp8_chunk(lane);
+        offset[j] = static_cast<uint32_t>(min(8 * i + lane / 8, a.M - 1 - m0)) * a.K + fp8_chunk(lane, i);
       } else {
         const int u = i - T::BM / 8;
         offset[j] = static_cast<uint32_t>(min(u / 2, a.N / 16 - 1 - n0 / 16)) * 16 * a.K + 1024 * (u % 2) + 16 * lane;
@@ -138,8 +99,8 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   f32x16_t acc[NF][MF];
   int step = 0;
   uint32_t slot = 0;
-  for (int s = 0; s < segments; ++s) {
-    const Segment g = segment(s);
+  for (int s = 0; s < work.segments; ++s) {
+    const Fp8Segment g = work.segment(s);
     fp8_clear(acc);
     for (int kb = g.kb0; kb < g.kb1; ++kb, ++step) {
       // Loads complete in order: once the later stages' are all that is outstanding, this stage is in LDS; the
@@ -155,29 +116,10 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
     }
 
     int m0, n0;
-    place(g.tile, &m0, &n0);
-    if (g.kb1 - g.kb0 < KB) {
-      // Partial sums in the accumulators' order.  Every worker of the tile stores its own with agent-scope
-      // stores and counts itself in once they are acknowledged; the last adds them in the order of k.
-      const int t = g.tile - a.rounds * a.workers;
-      constexpr uint32_t kPart = T::BM * T::BN * 4;
-      auto part = [&](int who, int seg) __attribute__((always_inline)) {
-        return buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(2 * who + seg) * kPart, kPart);
-      };
-      fp8_store_part(acc, part(w, s), threadIdx.x, kFp8Threads);
-      int* last = reinterpret_cast<int*>(lds + static_cast<size_t>(STAGES) * T::kStage);
-      wait_and_meet<0>();
-      const int w0 = sharer_of(static_cast<long long>(t) * KB, total, a.sharers);
-      const int w1 = sharer_of(static_cast<long long>(t) * KB + KB - 1, total, a.sharers);
-      if (threadIdx.x == 0)
-        *last = __hip_atomic_fetch_add(a.count + t, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == static_cast<unsigned>(w1 - w0);
-      __syncthreads();
-      if (!*last) continue;
-      // (the tile is the first of a worker's run or its second)
-      fp8_add_parts(acc, w1 - w0 + 1, [&](int k) { return part(w0 + k, static_cast<int>((w0 + k) * total / a.sharers / KB) == t ? 0 : 1); },
-                    threadIdx.x, kFp8Threads);
-      if (threadIdx.x == 0) __hip_atomic_store(a.count + t, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
+    fp8_place(a, g.tile, T::BM, T::BN, &m0, &n0);
+    if (g.kb1 - g.kb0 < work.KB &&
+        !fp8_join(acc, a, work, s, g.tile, T::BM * T::BN * 4, reinterpret_cast<int*>(lds + static_cast<size_t>(STAGES) * T::kStage)))
+      continue;
     fp8_results(acc, a, m0 + 32 * MF * wm, n0 + 32 * NF * wn, lane);
   }
 }
@@ -206,27 +148,30 @@ hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// What the launches cost, in microseconds: a call, a workgroup's stage of k when few and when all compute
-// units have one, a workgroup's start and end, joining parts of K (and their bytes, written and read), and
-// bytes of weights from memory.  Fitted to sweeps of every shape over 60 sizes; the choice below is the
-// cheapest by them.
-constexpr float kCall = 4.f, kTurn = 2.f, kJoin = 1.5f, kJoinBytes = 6.5e6f, kWeightBytes = 5e6f;
+// What the launches cost, in microseconds: a call; a workgroup's stage of k when few compute units have one and
+// when all do, and its start and end; joining parts of K, first in a launch or ahead of whole tiles, and their
+// bytes, written and read, cheaper while they stay in the last cache; bytes of weights from memory.  Fitted to
+// sweeps of every shape over some 60 sizes: the choice below, the cheapest by them, lost 4 % to the best.
+constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 1.5f, kJoinAhead = 5.f, kJoinBytes = 6e6f, kJoinCached = 1e8f, kWeightBytes = 5.2e6f;
+float join_cost(float bytes, bool ahead) {
+  return (ahead ? kJoinAhead : kJoin) + (bytes + std::max(0.f, bytes - kJoinCached)) / kJoinBytes;
+}
 struct SmallCost {
   int kind, rows, columns, blocks;  // launch_fp8_small's kind; a workgroup's tile and blocks of k a stage
   float few, all;
   bool exact;
 };
 constexpr SmallCost kSmall[] = {
-    {1, 32, 64, 4, 0.6f, 0.95f, true},   {2, 64, 64, 4, 1.4f, 1.5f, true},     {3, 64, 128, 2, 1.4f, 1.5f, true},
-    {4, 64, 64, 4, 0.65f, 1.4f, false},  {5, 64, 128, 2, 0.6f, 0.85f, false},  {6, 96, 128, 2, 0.9f, 1.15f, false},
-    {7, 128, 128, 1, 0.5f, 0.66f, false},
+    {1, 32, 64, 4, 0.6f, 0.95f, true},   {2, 64, 64, 4, 1.45f, 1.6f, true},     {3, 64, 128, 2, 1.4f, 1.5f, true},
+    {4, 64, 64, 4, 0.65f, 1.4f, false},  {5, 64, 128, 2, 0.6f, 0.85f, false},  {6, 96, 128, 2, 0.9f, 1.1f, false},
+    {7, 128, 128, 1, 0.56f, 0.66f, false},
 };
 struct LargeCost {
   int rows;
   float step;
   bool exact;
 };
-constexpr LargeCost kLarge[] = {{32, 1.0f, true}, {64, 1.5f, true}, {128, 1.04f, false}, {192, 1.45f, false}, {256, 1.88f, false}};
+constexpr LargeCost kLarge[] = {{32, 1.0f, true}, {64, 1.5f, true}, {128, 1.05f, false}, {192, 1.4f, false}, {256, 1.8f, false}};
 
 // At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
 // that already spreads over the compute units, else two, which share the rows' conversion; K cut over the eight
@@ -264,7 +209,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
       const long long groups = tiles * splits, turns = (groups + cus - 1) / cus;
       const float step = std::max(c.few, c.all * std::min<long long>(groups, cus) / cus);
       const size_t bytes = splits > 1 ? static_cast<size_t>(groups) * c.rows * c.columns * 4 : 0;
-      const float cost = kCall + std::max(memory, turns * ((units + splits - 1) / splits * step + kTurn)) + (bytes ? kJoin + 2 * bytes / kJoinBytes : 0.f);
+      const float cost = kCall + std::max(memory, turns * ((units + splits - 1) / splits * step + kTurn)) + (bytes ? join_cost(2.f * bytes, false) : 0.f);
       if (cost < best) {
         best = cost;
         p.small = c.kind;
@@ -284,7 +229,8 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
         const long long steps = static_cast<long long>(rounds) * KB + (left ? (static_cast<long long>(left) * KB + sharers - 1) / sharers : 0);
         const size_t runs = sharers > left ? static_cast<size_t>(sharers) * 2 : 0;  // their places in the workspace
         const float moved = sharers <= left ? 0.f : (sharers % left ? sharers + left : sharers) * 2.f * c.rows * kColumns * 4;
-        const float cost = kCall + std::max(memory, steps * c.step) + (runs ? kJoin + moved / kJoinBytes : 0.f);
+        const int ends = rounds + (left ? 1 + (sharers % left != 0) : 0);
+        const float cost = kCall + std::max(memory, steps * c.step) + ends * kEnd + (runs ? join_cost(moved, rounds > 0) : 0.f);
         if (cost < best) {
           best = cost;
           p.small = 0;

@@ -49,7 +49,7 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   for (int j = 0; j < T::kCopies; ++j) {
     const int i = (wave + kFp8Waves * j) % T::kRuns;
     if (i < T::BM / 8) {
-      offset[j] = static_cast<uint32_t>(min(8 * i + lane / 8, a.M - 1 - m0)) * a.K + fp8_chunk(lane);
+      offset[j] = static_cast<uint32_t>(min(8 * i + lane / 8, a.M - 1 - m0)) * a.K + fp8_chunk(lane, i);
     } else {
       const int u = i - T::BM / 8;
       offset[j] = static_cast<uint32_t>(min(u / 2, a.N / 16 - 1 - n0 / 16)) * 16 * a.K + 1024 * (u % 2) + 16 * lane;

@@ -150,27 +150,29 @@ hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
 
 // What the launches cost, in microseconds: a call; a workgroup's stage of k when few compute units have one and
 // when all do, and its start and end; joining parts of K, first in a launch or ahead of whole tiles, and their
-// bytes, written and read, cheaper while they stay in the last cache; bytes of weights from memory.  Fitted to
+// bytes, written and read, cheaper while they stay in the last cache; a kind's bytes of weights from memory.  Fitted to
 // sweeps of every shape over some 60 sizes: the choice below, the cheapest by them, lost 4 % to the best.
-constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 1.5f, kJoinAhead = 5.f, kJoinBytes = 6e6f, kJoinCached = 1e8f, kWeightBytes = 5.2e6f;
+constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 1.5f, kJoinAhead = 5.f, kJoinBytes = 6e6f, kJoinCached = 1e8f;
 float join_cost(float bytes, bool ahead) {
   return (ahead ? kJoinAhead : kJoin) + (bytes + std::max(0.f, bytes - kJoinCached)) / kJoinBytes;
 }
 struct SmallCost {
   int kind, rows, columns, blocks;  // launch_fp8_small's kind; a workgroup's tile and blocks of k a stage
-  float few, all;
+  float few, all, rate;
   bool exact;
+  int resident;                     // workgroups a compute unit
 };
 constexpr SmallCost kSmall[] = {
-    {1, 32, 64, 4, 0.6f, 0.95f, true},   {2, 64, 64, 4, 1.45f, 1.6f, true},     {3, 64, 128, 2, 1.4f, 1.5f, true},
-    {4, 64, 64, 4, 0.65f, 1.4f, false},  {5, 64, 128, 2, 0.6f, 0.85f, false},  {6, 96, 128, 2, 0.9f, 1.1f, false},
-    {7, 128, 128, 1, 0.56f, 0.66f, false},
+    {1, 32, 64, 4, 0.6f, 0.95f, 4.9e6f, true, 1},  {2, 64, 64, 4, 1.45f, 1.6f, 4.9e6f, true, 1},  {3, 64, 128, 2, 1.4f, 1.5f, 4.9e6f, true, 1},
+    {8, 32, 64, 2, 0.6f, 1.f, 5.4e6f, true, 2},    {4, 64, 64, 4, 0.65f, 1.4f, 4.9e6f, false, 1}, {5, 64, 128, 2, 0.6f, 0.85f, 4.9e6f, false, 1},
+    {6, 96, 128, 2, 0.9f, 1.1f, 4.9e6f, false, 1}, {7, 128, 128, 1, 0.56f, 0.66f, 4.9e6f, false, 1},
 };
 struct LargeCost {
   int rows;
   float step;
   bool exact;
 };
+constexpr float kLargeRate = 5.2e6f;
 constexpr LargeCost kLarge[] = {{32, 1.0f, true}, {64, 1.5f, true}, {128, 1.05f, false}, {192, 1.4f, false}, {256, 1.8f, false}};
 
 // At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
@@ -198,7 +200,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
     few_plan(M, N, K, rows8, cus, &p);
     if (p.splits > 1) parts = static_cast<size_t>((N / 16 + p.few - 1) / p.few) * p.splits * ((M + 15) / 16) * p.few * kWave * 16;
   } else {
-    const float memory = static_cast<float>(N) * K / kWeightBytes;
+    const float weights = static_cast<float>(N) * K;
     float best = 1e30f;
     for (const SmallCost& c : kSmall) {
       if (c.exact != exact) continue;
@@ -206,10 +208,12 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
       if (tiles > 64ll * cus) continue;
       const int units = (KB + c.blocks - 1) / c.blocks;
       const int splits = std::max(1, std::min(cus / static_cast<int>(tiles), units));
-      const long long groups = tiles * splits, turns = (groups + cus - 1) / cus;
+      const long long groups = tiles * splits;
+      // (of two workgroups a compute unit the one goes on while the other starts or ends)
+      const float turns = c.resident == 1 ? static_cast<float>((groups + cus - 1) / cus) : std::max(1.f, groups / (2.f * cus));
       const float step = std::max(c.few, c.all * std::min<long long>(groups, cus) / cus);
       const size_t bytes = splits > 1 ? static_cast<size_t>(groups) * c.rows * c.columns * 4 : 0;
-      const float cost = kCall + std::max(memory, turns * ((units + splits - 1) / splits * step + kTurn)) + (bytes ? join_cost(2.f * bytes, false) : 0.f);
+      const float cost = kCall + std::max(weights / c.rate, turns * ((units + splits - 1) / splits * step + kTurn)) + (bytes ? join_cost(2.f * bytes, false) : 0.f);
       if (cost < best) {
         best = cost;
         p.small = c.kind;
@@ -230,7 +234,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
         const size_t runs = sharers > left ? static_cast<size_t>(sharers) * 2 : 0;  // their places in the workspace
         const float moved = sharers <= left ? 0.f : (sharers % left ? sharers + left : sharers) * 2.f * c.rows * kColumns * 4;
         const int ends = rounds + (left ? 1 + (sharers % left != 0) : 0);
-        const float cost = kCall + std::max(memory, steps * c.step) + ends * kEnd + (runs ? join_cost(moved, rounds > 0) : 0.f);
+        const float cost = kCall + std::max(weights / kLargeRate, steps * c.step) + ends * kEnd + (runs ? join_cost(moved, rounds > 0) : 0.f);
         if (cost < best) {
           best = cost;
           p.small = 0;

@@ -1,5 +1,5 @@
 // The product in 8-bit floating point where tiles are few: a workgroup takes one smaller tile, or a run of its
-// K, and its wavefronts cut every stage's blocks of k among them too, so that a short tile still keeps eight
+// K, and its wavefronts cut every stage's blocks of k among them too, so that a short tile still keeps all its
 // wavefronts busy and most of the sums over K meet in LDS.
 #include <algorithm>
 
@@ -9,17 +9,17 @@ namespace subspec {
 
 namespace {
 
-// WM by WN by WK wavefronts: MF blocks of 32 rows and NF of 32 columns each, one of WK blocks of k of a stage.
+// WM by WN by WK wavefronts, four or eight: MF blocks of 32 rows and NF of 32 columns each, one of WK blocks of k of a stage.
 template <int MF, int NF, int WM, int WN, int WK, int STAGES>
 struct SmallTile {
-  static_assert(WM * WN * WK == kFp8Waves, "wavefronts of a workgroup");
+  static constexpr int WAVES = WM * WN * WK, THREADS = WAVES * kWave;
   static constexpr int BM = 32 * MF * WM, BN = 32 * NF * WN;
   static constexpr int kXBytes = BM * 128, kWBytes = BN * 128, kWords = (BM + BN + kWave - 1) / kWave;
   static constexpr int kBlock = kXBytes + kWBytes + 256 * kWords;  // codes and scale words of a block of k
   static constexpr int kStage = WK * kBlock;
   static constexpr int kRuns = BM / 8 + BN / 8;  // 1024-byte copies of a block
-  static constexpr int kCopies = WK * kRuns / kFp8Waves, kWordCopies = (WK * kWords + kFp8Waves - 1) / kFp8Waves;
-  static_assert(WK * kRuns % kFp8Waves == 0, "copies of a stage");
+  static constexpr int kCopies = WK * kRuns / WAVES, kWordCopies = (WK * kWords + WAVES - 1) / WAVES;
+  static_assert(WK * kRuns % WAVES == 0, "copies of a stage");
   static constexpr int kLoads = kCopies + kWordCopies, kAhead = STAGES - 1;
   static_assert(kAhead * kLoads < 64, "vmcnt has six bits");
   static constexpr size_t kSums = static_cast<size_t>(WK - 1) * BM * BN * 4;
@@ -28,7 +28,7 @@ struct SmallTile {
 };
 
 template <int MF, int NF, int WM, int WN, int WK, int STAGES, bool EXACT>
-__global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 4))) void k_fp8_small(Fp8Args a) {
+__global__ __launch_bounds__(WM * WN * WK * kWave) __attribute__((amdgpu_waves_per_eu(2, 4))) void k_fp8_small(Fp8Args a) {
   using T = SmallTile<MF, NF, WM, WN, WK, STAGES>;
   extern __shared__ __align__(16) uint8_t lds[];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   uint32_t offset[T::kCopies];
 #pragma unroll
   for (int j = 0; j < T::kCopies; ++j) {
-    const int i = (wave + kFp8Waves * j) % T::kRuns;
+    const int i = (wave + T::WAVES * j) % T::kRuns;
     if (i < T::BM / 8) {
       offset[j] = static_cast<uint32_t>(min(8 * i + lane / 8, a.M - 1 - m0)) * a.K + fp8_chunk(lane, i);
     } else {
@@ -59,7 +59,7 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   uint32_t sstep[T::kWordCopies];
 #pragma unroll
   for (int j = 0; j < T::kWordCopies; ++j) {
-    const int v = kWave * (min(wave + kFp8Waves * j, WK * T::kWords - 1) % T::kWords) + lane;
+    const int v = kWave * (min(wave + T::WAVES * j, WK * T::kWords - 1) % T::kWords) + lane;
     const bool of_x = v < T::BM;
     sbase[j] = of_x ? a.xs + min(m0 + v, a.M - 1) : a.ws + min(n0 + min(v - T::BM, T::BN - 1), a.N - 1);
     sstep[j] = of_x ? a.M : a.N;
@@ -68,13 +68,13 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
     const uint32_t to = ring + slot * T::kStage;
 #pragma unroll
     for (int j = 0; j < T::kCopies; ++j) {
-      const int c = wave + kFp8Waves * j, k = c / T::kRuns, i = c % T::kRuns, kb = min(unit * WK + k, KB - 1);
+      const int c = wave + T::WAVES * j, k = c / T::kRuns, i = c % T::kRuns, kb = min(unit * WK + k, KB - 1);
       if (i < T::BM / 8) copy16<false>(xbase + 128ll * kb, offset[j], to + k * T::kBlock + 1024 * i);
       else copy16<(EXACT && MF == 1)>(wbase + 2048ll * kb, offset[j], to + k * T::kBlock + 1024 * i);
     }
 #pragma unroll
     for (int j = 0; j < T::kWordCopies; ++j) {
-      const int c = min(wave + kFp8Waves * j, WK * T::kWords - 1), k = c / T::kWords, kb = min(unit * WK + k, KB - 1);
+      const int c = min(wave + T::WAVES * j, WK * T::kWords - 1), k = c / T::kWords, kb = min(unit * WK + k, KB - 1);
       copy4(sbase[j] + static_cast<size_t>(kb / 4) * sstep[j], to + k * T::kBlock + T::kXBytes + T::kWBytes + 256 * (c % T::kWords));
     }
   };
@@ -161,7 +161,7 @@ hipError_t small_at(Fp8Args a, hipStream_t st) {
   if (set != hipSuccess) return set;
   a.tiles_m = (a.M + T::BM - 1) / T::BM;
   a.tiles_n = (a.N + T::BN - 1) / T::BN;
-  hipLaunchKernelGGL((k_fp8_small<MF, NF, WM, WN, WK, STAGES, EXACT>), dim3(a.tiles_m * a.tiles_n * a.splits), dim3(kFp8Threads), T::kLds, st, a);
+  hipLaunchKernelGGL((k_fp8_small<MF, NF, WM, WN, WK, STAGES, EXACT>), dim3(a.tiles_m * a.tiles_n * a.splits), dim3(T::THREADS), T::kLds, st, a);
   return hipGetLastError();
 }
 
@@ -175,7 +175,8 @@ hipError_t launch_fp8_small(const Fp8Args& a, int kind, hipStream_t st) {
     case 4: return small_at<2, 1, 1, 2, 4, 2, false>(a, st);  // 64 x 64
     case 5: return small_at<2, 1, 1, 4, 2, 3, false>(a, st);  // 64 x 128
     case 6: return small_at<3, 1, 1, 4, 2, 2, false>(a, st);  // 96 x 128
-    default: return small_at<2, 1, 2, 4, 1, 4, false>(a, st);  // 128 x 128
+    case 7: return small_at<2, 1, 2, 4, 1, 4, false>(a, st);  // 128 x 128
+    default: return small_at<1, 1, 1, 2, 2, 3, true>(a, st);   // 32 x 64, four wavefronts, two workgroups a compute unit
   }
 }
 

@@ -105,6 +105,7 @@ def load_library():
         "subspec_fp8_pack": (I, [P, I, I, P, P]),
         "subspec_fp8_linear": (I, [P, P, P, P, I, I, I, P, P]),
         "subspec_fp8_linear_workspace_bytes": (S, [I, I, I, I]),
+        "subspec_fp8_linear_plan": (I, [I, I, I, P, P, P, P, P]),
         "subspec_prefetch_create": (I, [S, I, ctypes.POINTER(ctypes.c_void_p)]),
         "subspec_prefetch_destroy": (I, [P]),
         "subspec_prefetch_begin": (I, [P, P, S, ctypes.POINTER(ctypes.c_longlong)]),
@@ -459,7 +460,7 @@ def subspec_tree_verify_workspace_bytes(N, V) -> int:
 
 def _scales(t, words):
     """Kind and least elements of `words` scale words: words, or their bytes in order, [words / rows][rows][4]."""
-    if getattr(getattr(t, "dtype", None), "itemsize", 4) == 1:
+    if t is not None and getattr(getattr(t, "dtype", None), "itemsize", 4) == 1:
         return "e8m0", 4 * words
     return "i32", words
 
@@ -507,6 +508,13 @@ def subspec_fp8_linear(x, x_scales, w, w_scales, M, N, K, y, stream=None) -> int
 
 def subspec_fp8_linear_workspace_bytes(M, N, K, rows8) -> int:
     return int(load_library().subspec_fp8_linear_workspace_bytes(M, N, K, int(rows8)))
+
+
+def subspec_fp8_linear_plan(M, N, K):
+    """(kernel, rows, columns, workgroups, sharing) of the launch."""
+    v = [ctypes.c_int() for _ in range(5)]
+    _check("subspec_fp8_linear_plan", load_library().subspec_fp8_linear_plan(M, N, K, *map(ctypes.byref, v)))
+    return tuple(x.value for x in v)
 
 
 class Prefetcher:

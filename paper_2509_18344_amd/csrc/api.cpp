@@ -1485,6 +1485,19 @@ size_t subspec_fp8_linear_workspace_bytes(int M, int N, int K, int rows8) {
   return subspec::fp8_plan(M, N, K, rows8 != 0, device_cus()).workspace_bytes;
 }
 
+int subspec_fp8_linear_plan(int M, int N, int K, int* kernel, int* rows, int* columns, int* workgroups, int* sharing) {
+  if (!kernel || !rows || !columns || !workgroups || !sharing) return fail(SUBSPEC_EINVAL, "null pointer argument");
+  const int rc = fp8_linear_check(M, N, K);
+  if (rc) return rc;
+  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, true, device_cus());
+  *kernel = p.few ? 0 : p.small ? 1 : 2;
+  *rows = p.tile_rows;
+  *columns = p.tile_columns;
+  *workgroups = p.groups;
+  *sharing = p.sharing;
+  return SUBSPEC_OK;
+}
+
 int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K,
                        void* y, hipStream_t stream) {
   if (!x || !w || !w_scales || !y) return fail(SUBSPEC_EINVAL, "fp8_linear: null pointer argument");

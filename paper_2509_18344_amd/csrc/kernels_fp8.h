@@ -31,6 +31,7 @@ struct Fp8Plan {
   int small;               // which of the small tiles; 0: the large ones
   int rows;                // rows of a large tile
   int workers, rounds, left, sharers;
+  int tile_rows, tile_columns, groups, sharing;  // the launch described: tile, workgroups, most that share a tile's K
   size_t code_bytes;       // x's codes and scales, where the call makes them
   size_t workspace_bytes;  // completion counters, codes and scales, partial sums; 0: none
 };

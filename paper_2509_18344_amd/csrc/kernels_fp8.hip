@@ -124,15 +124,14 @@ __global__ __launch_bounds__(kFp8Threads) __attribute__((amdgpu_waves_per_eu(2, 
   }
 }
 
-// A thread moves 16 codes of one column: slice `lane` of half h of tile (nt, kb).
-__global__ __launch_bounds__(256) void k_fp8_pack(const uint8_t* codes, int N, int K, uint8_t* tiles) {
-  const size_t t = static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (16 * t >= static_cast<size_t>(N) * K) return;
-  const int lane = t % 64, half = t / 64 % 2;
-  const size_t tile = t / 128;
-  const int KB = K / 128;
-  const size_t n = tile / KB * 16 + lane % 16, k = tile % KB * 128 + 64 * half + 16 * (lane / 16);
-  *reinterpret_cast<uint4*>(tiles + 16 * t) = *reinterpret_cast<const uint4*>(codes + n * K + k);
+// A thread moves 16 codes of one column: slice `lane` of half h of tile (nt, kb), two tiles a workgroup.
+__global__ __launch_bounds__(256) void k_fp8_pack(const uint8_t* codes, int K, uint8_t* tiles) {
+  const int nt = blockIdx.x, KB = K / 128, kb = blockIdx.y * 2 + threadIdx.x / 128;
+  if (kb >= KB) return;
+  const int lane = threadIdx.x % 64, half = threadIdx.x / 64 % 2;
+  const size_t n = static_cast<size_t>(nt) * 16 + lane % 16, k = static_cast<size_t>(kb) * 128 + 64 * half + 16 * (lane / 16);
+  *reinterpret_cast<uint4*>(tiles + (static_cast<size_t>(nt) * KB + kb) * 2048 + 1024 * half + 16 * lane) =
+      *reinterpret_cast<const uint4*>(codes + n * K + k);
 }
 
 constexpr int kColumns = 256;  // of every tile
@@ -141,52 +140,53 @@ template <int MF, int NF, int WM, int WN, int STAGES, bool EXACT>
 hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
   using T = Tile<MF, NF, WM, WN, STAGES>;
   static_assert(T::BN == kColumns, "columns of a tile");
-  static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_fp8_tiles<MF, NF, WM, WN, STAGES, EXACT>),
-                                                   hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
-  if (set != hipSuccess) return set;
   hipLaunchKernelGGL((k_fp8_tiles<MF, NF, WM, WN, STAGES, EXACT>), dim3(a.workers), dim3(kFp8Threads), T::kLds, st, a);
   return hipGetLastError();
 }
 
 // What the launches cost, in microseconds: a call; a workgroup's stage of k when few compute units have one and
-// when all do, and its start and end; joining parts of K, first in a launch or ahead of whole tiles, and their
-// bytes, written and read, cheaper while they stay in the last cache; a kind's bytes of weights from memory.  Fitted to
-// sweeps of every shape over some 60 sizes: the choice below, the cheapest by them, lost 4 % to the best.
-constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 1.5f, kJoinAhead = 5.f, kJoinBytes = 6e6f, kJoinCached = 1e8f;
-float join_cost(float bytes, bool ahead) {
-  return (ahead ? kJoinAhead : kJoin) + (bytes + std::max(0.f, bytes - kJoinCached)) / kJoinBytes;
+// when all do, its end, and a start after another's end; joining parts of K, first in a launch or ahead of whole
+// tiles: trips to memory one after the other, and bytes, written and read, cheaper while they stay in the last
+// cache; a kind's bytes of weights from memory.  Fitted to sweeps of every shape over some 60 sizes: the choice
+// below, the cheapest by them, lost 4 % to the best.
+constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 0.5f, kJoinAhead = 2.f, kTrip = 0.8f, kJoinBytes = 7e6f, kJoinCached = 1e8f;
+float join_cost(float bytes, int sharing, int at_once, int passes, bool ahead) {
+  return (ahead ? kJoinAhead : kJoin) + kTrip * passes * ((sharing + at_once - 1) / at_once) + (bytes + std::max(0.f, bytes - kJoinCached)) / kJoinBytes;
 }
 struct SmallCost {
   int kind, rows, columns, blocks;  // launch_fp8_small's kind; a workgroup's tile and blocks of k a stage
   float few, all, rate;
   bool exact;
   int resident;                     // workgroups a compute unit
+  int at_once;                      // parts that are added at once
 };
 constexpr SmallCost kSmall[] = {
-    {1, 32, 64, 4, 0.6f, 0.95f, 4.9e6f, true, 1},  {2, 64, 64, 4, 1.45f, 1.6f, 4.9e6f, true, 1},  {3, 64, 128, 2, 1.4f, 1.5f, 4.9e6f, true, 1},
-    {8, 32, 64, 2, 0.6f, 1.f, 5.4e6f, true, 2},    {4, 64, 64, 4, 0.65f, 1.4f, 4.9e6f, false, 1}, {5, 64, 128, 2, 0.6f, 0.85f, 4.9e6f, false, 1},
-    {6, 96, 128, 2, 0.9f, 1.1f, 4.9e6f, false, 1}, {7, 128, 128, 1, 0.56f, 0.66f, 4.9e6f, false, 1},
+    {1, 32, 64, 4, 0.6f, 0.95f, 4.9e6f, true, 1, 8},  {2, 64, 64, 4, 1.45f, 1.6f, 4.9e6f, true, 1, 4},  {3, 64, 128, 2, 1.4f, 1.5f, 4.9e6f, true, 1, 4},
+    {8, 32, 64, 2, 0.6f, 1.f, 5.4e6f, true, 2, 8},    {4, 64, 64, 4, 0.65f, 1.4f, 4.9e6f, false, 1, 4}, {5, 64, 128, 2, 0.6f, 0.85f, 4.9e6f, false, 1, 4},
+    {6, 96, 128, 2, 0.9f, 1.1f, 4.9e6f, false, 1, 2}, {7, 128, 128, 1, 0.56f, 0.66f, 4.9e6f, false, 1, 4},
 };
 struct LargeCost {
   int rows;
   float step;
   bool exact;
+  int at_once, passes;  // parts that are added at once, passes over them
 };
 constexpr float kLargeRate = 5.2e6f;
-constexpr LargeCost kLarge[] = {{32, 1.0f, true}, {64, 1.5f, true}, {128, 1.05f, false}, {192, 1.4f, false}, {256, 1.8f, false}};
+constexpr LargeCost kLarge[] = {{32, 1.0f, true, 8, 1}, {64, 1.5f, true, 4, 1}, {128, 1.05f, false, 1, 2}, {192, 1.4f, false, 1, 2}, {256, 1.8f, false, 1, 2}};
 
 // At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
 // that already spreads over the compute units, else two, which share the rows' conversion; K cut over the eight
 // wavefronts of a workgroup where it is short, else over four and over workgroups too, as many as stay resident.
 // (1 row: 3584 x 3584 6.0 us with one tile and eight wavefronts, 6.9 with two tiles, 7.1 with four wavefronts;
 // 3584 x 18944 17.6 with two tiles, four wavefronts and four workgroups, 19.6 with one tile and one workgroup.)
-void few_plan(int M, int N, int K, bool rows8, int cus, Fp8Plan* p) {
+// The same for bf16 rows, so that they give the bits of their 8-bit rows.
+void few_plan(int M, int N, int K, int cus, Fp8Plan* p) {
   const int tiles = N / 16, KB = K / 128;
   const bool longer = KB > 64;
   p->few = M > 16 || (tiles <= cus && !longer) ? 1 : 2;
   const int sets = (tiles + p->few - 1) / p->few;
   p->waves = M > 16 || longer || sets > cus ? 4 : 8;
-  p->splits = longer || M > 16 ? std::max(1, std::min((rows8 ? 3 : 2) * cus / sets, std::min(KB / 16, 64))) : 1;
+  p->splits = longer || M > 16 ? std::max(1, std::min(3 * cus / sets, std::min(KB / 16, 64))) : 1;
 }
 
 }  // namespace
@@ -197,7 +197,11 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
   const bool exact = M <= kFp8ExactRows;
   size_t parts = 0;
   if (M <= 16 || (exact && static_cast<long long>(N) * K <= 1 << 21)) {
-    few_plan(M, N, K, rows8, cus, &p);
+    few_plan(M, N, K, cus, &p);
+    p.tile_rows = 16 * ((M + 15) / 16);
+    p.tile_columns = 16 * p.few;
+    p.groups = (N / 16 + p.few - 1) / p.few * p.splits;
+    p.sharing = p.splits;
     if (p.splits > 1) parts = static_cast<size_t>((N / 16 + p.few - 1) / p.few) * p.splits * ((M + 15) / 16) * p.few * kWave * 16;
   } else {
     const float weights = static_cast<float>(N) * K;
@@ -213,11 +217,16 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
       const float turns = c.resident == 1 ? static_cast<float>((groups + cus - 1) / cus) : std::max(1.f, groups / (2.f * cus));
       const float step = std::max(c.few, c.all * std::min<long long>(groups, cus) / cus);
       const size_t bytes = splits > 1 ? static_cast<size_t>(groups) * c.rows * c.columns * 4 : 0;
-      const float cost = kCall + std::max(weights / c.rate, turns * ((units + splits - 1) / splits * step + kTurn)) + (bytes ? join_cost(2.f * bytes, false) : 0.f);
+      const float cost = kCall + std::max(weights / c.rate, turns * ((units + splits - 1) / splits * step) + (turns - 1) * kTurn + kEnd) +
+                         (bytes ? join_cost(2.f * bytes, splits, c.at_once, 1, false) : 0.f);
       if (cost < best) {
         best = cost;
         p.small = c.kind;
         p.splits = splits;
+        p.tile_rows = c.rows;
+        p.tile_columns = c.columns;
+        p.groups = static_cast<int>(groups);
+        p.sharing = splits;
         parts = bytes;
       }
     }
@@ -233,8 +242,9 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
         const long long steps = static_cast<long long>(rounds) * KB + (left ? (static_cast<long long>(left) * KB + sharers - 1) / sharers : 0);
         const size_t runs = sharers > left ? static_cast<size_t>(sharers) * 2 : 0;  // their places in the workspace
         const float moved = sharers <= left ? 0.f : (sharers % left ? sharers + left : sharers) * 2.f * c.rows * kColumns * 4;
+        const int sharing = runs ? (sharers + left - 1) / left + (sharers % left != 0) : 1;
         const int ends = rounds + (left ? 1 + (sharers % left != 0) : 0);
-        const float cost = kCall + std::max(weights / kLargeRate, steps * c.step) + ends * kEnd + (runs ? join_cost(moved, rounds > 0) : 0.f);
+        const float cost = kCall + std::max(weights / kLargeRate, steps * c.step) + ends * kEnd + (runs ? join_cost(moved, sharing, c.at_once, c.passes, rounds > 0) : 0.f);
         if (cost < best) {
           best = cost;
           p.small = 0;
@@ -243,6 +253,10 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
           p.left = left;
           p.sharers = sharers;
           p.workers = rounds ? cus : sharers;
+          p.tile_rows = c.rows;
+          p.tile_columns = kColumns;
+          p.groups = p.workers;
+          p.sharing = sharing;
           parts = runs * c.rows * kColumns * 4;
         }
       }
@@ -291,8 +305,7 @@ hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipSt
 }
 
 hipError_t launch_fp8_pack(const uint8_t* codes, int N, int K, uint8_t* tiles, hipStream_t st) {
-  const size_t threads = static_cast<size_t>(N) * K / 16;
-  hipLaunchKernelGGL(k_fp8_pack, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, codes, N, K, tiles);
+  hipLaunchKernelGGL(k_fp8_pack, dim3(N / 16, (K / 128 + 1) / 2), dim3(256), 0, st, codes, K, tiles);
   return hipGetLastError();
 }
 

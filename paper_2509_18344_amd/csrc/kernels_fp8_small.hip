@@ -156,9 +156,6 @@ __global__ __launch_bounds__(WM * WN * WK * kWave) __attribute__((amdgpu_waves_p
 template <int MF, int NF, int WM, int WN, int WK, int STAGES, bool EXACT>
 hipError_t small_at(Fp8Args a, hipStream_t st) {
   using T = SmallTile<MF, NF, WM, WN, WK, STAGES>;
-  static const hipError_t set = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_fp8_small<MF, NF, WM, WN, WK, STAGES, EXACT>),
-                                                   hipFuncAttributeMaxDynamicSharedMemorySize, T::kLds);
-  if (set != hipSuccess) return set;
   a.tiles_m = (a.M + T::BM - 1) / T::BM;
   a.tiles_n = (a.N + T::BN - 1) / T::BN;
   hipLaunchKernelGGL((k_fp8_small<MF, NF, WM, WN, WK, STAGES, EXACT>), dim3(a.tiles_m * a.tiles_n * a.splits), dim3(T::THREADS), T::kLds, st, a);

@@ -1,6 +1,7 @@
 """Building substitute weights on the GPU with the library: quantize (subspec_quantize)
 and pack (subspec_qpack) one projection, or several that share their input and are
-fused along N (q|k|v, gate|up), plus the per-layer launch list of a decoder layer."""
+fused along N (q|k|v, gate|up), the per-layer launch list of a decoder layer, and weights in
+8-bit floating point."""
 from __future__ import annotations
 
 from . import _binding as b
@@ -25,6 +26,20 @@ def fused(ws, bits: int, group: int) -> dict:
     the result equals the separate projections side by side)."""
     import torch
     return quantize_pack(torch.cat(list(ws), dim=0), bits, group)
+
+
+def fp8_weight(w, stream=None) -> dict:
+    """w: bfloat16 device tensor [N][K] -> weight tiles and scales for subspec_fp8_linear."""
+    import torch
+    N, K = w.shape
+    codes = torch.empty((N, K), dtype=torch.uint8, device=w.device)
+    scales = torch.empty(((K + 511) // 512, N), dtype=torch.int32, device=w.device)
+    b.subspec_fp8_rows(w, N, K, codes, scales, stream)
+    tiles = torch.empty(N * K, dtype=torch.uint8, device=w.device)
+    b.subspec_fp8_pack(codes, N, K, tiles, stream)
+    if stream is not None and stream != torch.cuda.current_stream(w.device):
+        codes.record_stream(stream)  # goes back to the allocator while the stream still reads it
+    return {"w": tiles, "w_scales": scales, "N": N, "K": K}
 
 
 def layer_launches(packed, xs, ys):

@@ -54,13 +54,14 @@ def _powers(codes, bytes_):
     return np.where(codes & 127, p, 0.0)
 
 
-def check(y, x8, w8, what=""):
+def check(y, x8, w8, what="", rows=None):
     """y (bf16 on the GPU) against the product of 8-bit rows, (codes, scale bytes) each."""
     xv, wv = oracle.fp8_values(*x8), oracle.fp8_values(*w8)
     K = xv.shape[1]
+    exact = (rows or len(xv)) <= EXACT
     ref, wabs = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
     px, pw = (_powers(*r).reshape(len(r[0]), K // 8, 8).max(-1) for r in (x8, w8))
-    cut = 8 * 2.0 ** -13 * (px @ pw.T) * (len(xv) > EXACT)
+    cut = 8 * 2.0 ** -13 * (px @ pw.T) * (not exact)
     err, tol = np.abs(f64(host(y)) - ref), 2.0 ** -8 * (np.abs(ref) + cut) + cut + (K / 128 + 32) * 2.0 ** -23 * wabs
     assert np.all(err <= tol), (what, float((err / np.maximum(tol, 1e-300)).max()), np.argwhere(err > tol)[:4].tolist())
 
@@ -76,6 +77,67 @@ SHAPES = [(1, 16, 128), (1, 3584, 3584), (1, 48, 27648), (2, 16, 256), (3, 208, 
           (13, 16, 18944), (16, 272, 512), (17, 272, 512), (31, 80, 1024), (33, 528, 1280), (48, 16, 4096), (49, 3584, 896), (64, 256, 2176), (65, 272, 640),
           (96, 144, 128), (127, 128, 1920), (128, 1024, 512), (129, 400, 768), (200, 16, 5120), (255, 256, 256), (257, 272, 384), (289, 1168, 1152),
           (300, 4112, 128), (512, 512, 1024), (600, 784, 640), (1000, 2064, 896), (1025, 528, 384), (2049, 272, 256)]
+
+
+# every kind of launch: (kernel, rows, columns of a tile, K shared by workgroups, more than one tile a workgroup or two
+# workgroups a compute unit), as tests/test_library_fp8_cpu.py holds the plan to
+KINDS = {
+    (18, 368, 5888): (1, 32, 64, True, False), (19, 6224, 384): (1, 32, 64, False, False), (20, 17008, 384): (1, 32, 64, False, True),
+    (34, 2528, 1664): (1, 64, 64, True, False), (33, 8208, 384): (1, 64, 64, False, False), (35, 18976, 256): (1, 64, 128, False, False),
+    (34, 9024, 3712): (1, 64, 128, True, False), (18, 16448, 4864): (2, 32, 256, True, False), (34, 19536, 7808): (2, 64, 256, True, False),
+    (40, 70000, 384): (2, 64, 256, False, True), (66, 16, 384): (1, 64, 64, False, False), (67, 16, 896): (1, 64, 64, True, False),
+    (65, 16, 256): (1, 64, 128, False, False), (66, 16, 640): (1, 64, 128, True, False), (69, 18272, 256): (1, 96, 128, False, False),
+    (67, 8352, 6016): (1, 96, 128, True, False), (66, 16, 128): (1, 128, 128, False, False), (2267, 272, 6784): (1, 128, 128, True, False),
+    (130, 17312, 256): (2, 128, 256, False, False), (275, 33024, 128): (2, 128, 256, False, True), (198, 39200, 4736): (2, 128, 256, True, True),
+    (400, 16512, 128): (2, 192, 256, False, False), (514, 27152, 128): (2, 192, 256, False, True), (144, 18000, 5248): (2, 192, 256, True, False),
+    (516, 26448, 2560): (2, 192, 256, True, True), (579, 16480, 128): (2, 256, 256, False, False), (786, 26256, 128): (2, 256, 256, False, True),
+    (1175, 15008, 6016): (2, 256, 256, True, True),
+}
+
+
+def check_some(y, x8, w8, what=""):
+    """check() of about 200 rows and columns, the ends of every tile's among them."""
+    M, N = y.shape
+    pick = lambda n: np.unique(np.r_[np.arange(min(n, 35)), np.arange(max(0, n - 70), n), np.arange(31, n, max(32, n // 64 // 32 * 32)),  # noqa: E731
+                                     np.arange(32, n, max(32, n // 64 // 32 * 32))])
+    m, n = pick(M), pick(N)
+    check(y[torch.from_numpy(m).to(DEV)][:, torch.from_numpy(n).to(DEV)], tuple(a[m] for a in x8), tuple(a[n] for a in w8), what, M)
+
+
+def _tiled_weight(rng, N, K, spread=3):
+    """Rows of a weight that repeat after an odd number of them, and its tiles and scales on the GPU."""
+    c, b = _random_rows(rng, min(N, 131), K, spread)
+    at = np.arange(N) * 37 % len(c)
+    return c[at], b[at]
+
+
+@pytest.mark.parametrize("M,N,K", KINDS)
+def test_every_kind_of_launch(M, N, K):
+    rng = np.random.default_rng([63, M, N, K])
+    x8, w8 = _random_rows(rng, M, K), _tiled_weight(rng, N, K)
+    t, ws = weight(*w8)
+    x = codes_to(*x8)
+    y = linear(*x, t, ws, M, N, K)
+    check_some(y, x8, w8)
+    for _ in range(2):  # and the counters are as they were
+        assert torch.equal(linear(*x, t, ws, M, N, K).view(torch.int16), y.view(torch.int16))
+
+
+@pytest.mark.parametrize("M,N,K", [k for k in KINDS if k[2] >= 384 and k[0] * k[1] < 2 ** 23])
+def test_every_kind_over_all_scales_and_with_nan(M, N, K):
+    rng = np.random.default_rng([64, M, N, K])
+    x8, w8 = _random_rows(rng, M, K), _tiled_weight(rng, N, K)
+    p = np.array([-126, 0, 120, -100, 7, 60, -60, 1, 100])[np.arange(K // 128) % 9]
+    x8, w8 = (x8[0].copy(), np.broadcast_to(127 + p, x8[1].shape)), (w8[0].copy(), np.broadcast_to(127 - p, w8[1].shape))
+    x, (t, ws) = codes_to(*x8), weight(*w8)
+    y = linear(*x, t, ws, M, N, K)
+    check_some(y, x8, w8)
+    x8[0][M // 2, K - 1], w8[0][N - 3, 0] = 0xFF, 0x7F
+    x, (t, ws) = codes_to(*x8), weight(*w8)
+    z = linear(*x, t, ws, M, N, K)
+    nan = torch.isnan(z)
+    assert bool(nan[M // 2].all()) and bool(nan[:, N - 3].all()) and int(nan.sum()) == M + N - 1
+    assert torch.equal(torch.where(nan, 0, z), torch.where(nan, 0, y))
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -107,7 +169,7 @@ def test_fp8_linear_of_whole_numbers_is_exact(M, N, K):
     assert np.array_equal(f64(host(y))[small], ref[small])
 
 
-@pytest.mark.parametrize("M,N,K", [(1, 3584, 3584), (5, 272, 27648), (16, 512, 640), (17, 512, 640), (49, 1024, 2176), (100, 272, 5120), (289, 528, 1152), (700, 1040, 512)])
+@pytest.mark.parametrize("M,N,K", [(1, 3584, 3584), (5, 272, 27648), (3, 5120, 16384), (16, 512, 640), (17, 512, 640), (49, 1024, 2176), (100, 272, 5120), (289, 528, 1152), (700, 1040, 512)])
 def test_bf16_rows_give_the_bits_of_their_8_bit_rows(M, N, K):
     rng = np.random.default_rng([52, M, N, K])
     x = rng.standard_normal((M, K)) * np.repeat(np.exp2(rng.integers(-4, 5, (M, K // 128))), 128, 1)
@@ -190,6 +252,23 @@ def test_pack_is_the_oracles_order(N, K):
     assert np.array_equal(t[: N * K].cpu().numpy(), oracle.weight_tiles(c)) and bool((t[N * K:] == 0x5A).all())
 
 
+@pytest.mark.parametrize("other", [False, True])
+def test_prepared_weight(other):
+    from paper_2509_18344_amd import prepare
+    N, K, M = 272, 640, 5
+    rng = np.random.default_rng(62)
+    w, x = bf16(rng.standard_normal((N, K))), bf16(rng.standard_normal((M, K)))
+    wd, xd = dev(w), dev(x)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream() if other else None
+    p = prepare.fp8_weight(wd, s)
+    if other:
+        s.synchronize()
+    wc, wb = oracle.fp8_rows(f64(w))
+    assert np.array_equal(p["w"].cpu().numpy(), oracle.weight_tiles(wc))
+    check(linear(xd, None, p["w"], p["w_scales"], M, p["N"], p["K"]), oracle.fp8_rows(f64(x)), (wc, wb))
+
+
 def test_results_past_2_31_elements():
     M, N, K = 32800, 65552, 128  # 2.15e9 results
     rng = np.random.default_rng(56)
@@ -202,7 +281,7 @@ def test_results_past_2_31_elements():
     ss.subspec_fp8_linear(x, xs, t, ws, M, N, K, y)
     rows = np.r_[0:3, M // 2, M - 40:M]
     for cols in (slice(-300, None), slice(300)):
-        check(y[torch.from_numpy(rows).to(DEV)][:, cols], (xc[xr[rows]], xb[xr[rows]]), (wc[wr[cols]], wb[wr[cols]]))
+        check(y[torch.from_numpy(rows).to(DEV)][:, cols], (xc[xr[rows]], xb[xr[rows]]), (wc[wr[cols]], wb[wr[cols]]), "", M)
 
 
 def test_weights_past_2_32_bytes():

@@ -104,6 +104,28 @@ def test_fp8_linear_workspace():
     assert ss.subspec_fp8_linear_workspace_bytes(4096, 512, 1280, 2) == 0
 
 
+def test_every_kind_of_launch_is_reached():
+    from test_gpu_fp8 import KINDS
+    for (M, N, K), (kernel, rows, columns, shared, several) in KINDS.items():
+        k, r, c, groups, sharing = ss.subspec_fp8_linear_plan(M, N, K)
+        assert (k, r, c, sharing > 1) == (kernel, rows, columns, shared), (M, N, K)
+        tiles = -(-M // rows) * -(-N // columns)
+        assert (groups > 256 if k == 1 else tiles > groups) == several, (M, N, K, groups)
+        assert groups <= tiles * sharing
+    kinds = {v[:3] for v in KINDS.values()}
+    rng = np.random.default_rng(0)
+    for _ in range(3000):  # and no other is
+        M, N, K = (int(np.exp(rng.uniform(np.log(lo), np.log(hi)))) for lo, hi in ((1, 5000), (1, 4000), (1, 220)))
+        p = ss.subspec_fp8_linear_plan(M, 16 * N, 128 * K)
+        assert p[:3] in kinds if p[0] else p[1] == (M + 15) // 16 * 16 and M <= 64 and p[2] in (16, 32), (M, N, K, p)
+
+
+@pytest.mark.parametrize("shape", [(0, 16, 128), (1, 24, 128), (1, 16, 192), (1 << 20, 1 << 21, 128)])
+def test_fp8_linear_plan_refusals(shape):
+    with refused("EUNSUPPORTED"):
+        ss.subspec_fp8_linear_plan(*shape)
+
+
 # --- what the binding checks ----------------------------------------------------------------
 
 M, K, I, N = 3, 640, 384, 48

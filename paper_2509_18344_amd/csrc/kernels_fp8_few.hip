@@ -300,7 +300,7 @@ hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t 
     else if (columns == 2) fused ? few_at<4, 1, 2, true>(a, st) : few_at<4, 1, 2, false>(a, st);
     else fused ? few_at<8, 1, 1, true>(a, st) : few_at<8, 1, 1, false>(a, st);
   } else if (rows == 2) {
-    few_at<4, 2, 1, false>(a, st);
+    fused ? few_at<4, 2, 1, true>(a, st) : few_at<4, 2, 1, false>(a, st);
   } else if (rows == 3) {
     few_at<4, 3, 1, false>(a, st);
   } else {

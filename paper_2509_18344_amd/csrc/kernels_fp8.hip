@@ -186,7 +186,7 @@ void few_plan(int M, int N, int K, int cus, Fp8Plan* p) {
   p->few = M > 16 || (tiles <= cus && !longer) ? 1 : 2;
   const int sets = (tiles + p->few - 1) / p->few;
   p->waves = M > 16 || longer || sets > cus ? 4 : 8;
-  p->splits = longer || M > 16 ? std::max(1, std::min(3 * cus / sets, std::min(KB / 16, 64))) : 1;
+  p->splits = longer || M > 16 ? std::max(1, std::min(2 * cus / sets, std::min(KB / 16, 64))) : 1;
 }
 
 }  // namespace

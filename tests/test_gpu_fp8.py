@@ -353,59 +353,3 @@ def test_two_layers_mlps_one_after_the_other(M):
         s = _mlp_steps_check(l, M, out, x, res)
         assert np.all(np.abs(f64(host(rd)) - s) <= 2.0 ** -8 * np.abs(s) * 1.001)
         xd, x, res = y.clone(), host(y), host(rd)
-
-
-@pytest.mark.parametrize("M", [1, 13, 200])
-def test_mlp_on_another_stream_captured_and_replayed(M):
-    rng = np.random.default_rng([59, M])
-    l = _layer(rng, 768, 640)
-    xs = [bf16(rng.standard_normal((M, 768))) for _ in range(4)]
-    res = bf16(4 * rng.standard_normal((M, 768)))
-    out = _mlp_buffers(l, M)
-    want = []
-    for x in xs:
-        want.append(host(_mlp(l, dev(x), dev(res), M, out)))
-    s = torch.cuda.Stream()
-    rd, xd = dev(res), dev(xs[1])
-    s.wait_stream(torch.cuda.current_stream())
-    y = _mlp(l, xd, rd, M, out, s)
-    s.synchronize()
-    assert np.array_equal(host(y), want[1])
-    need = max(ss.subspec_fp8_linear_workspace_bytes(M, n, k, 1) for n, k in ((1280, 768), (768, 640)))
-    ss.subspec_reserve(max(need, 1))
-    allocations = ss.subspec_workspace_info()["allocations"]
-    g = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(g):
-        _mlp(l, xd, rd, M, out)
-    for x, w in zip(xs, want):
-        xd.copy_(dev(x))
-        rd.copy_(dev(res))
-        out["y"].zero_()
-        g.replay()
-        torch.cuda.synchronize()
-        assert np.array_equal(host(out["y"]), w)
-        assert np.array_equal(host(_mlp(l, dev(x), dev(res), M, _mlp_buffers(l, M))), w)  # eager between replays
-    assert ss.subspec_workspace_info()["allocations"] == allocations
-
-
-def test_bf16_rows_captured_next_to_other_calls_that_use_the_workspace():
-    from helpers import device_projection, run_qlinear
-    rng = np.random.default_rng(60)
-    M, N, K = 40, 512, 1024
-    wc, wb = _random_rows(rng, N, K)
-    t, ws = weight(wc, wb)
-    x = dev(bf16(rng.standard_normal((M, K))))
-    p = device_projection(torch.from_numpy(rng.standard_normal((512, 3584)).astype(np.float32)).to(DEV), 4, 64)
-    xq = dev(bf16(rng.standard_normal((M, 3584))))
-    q0, y0 = run_qlinear(p, xq), linear(x, None, t, ws, M, N, K)
-    ss.subspec_reserve(max(ss.subspec_fp8_linear_workspace_bytes(M, N, K, 0), ss.subspec_qlinear_plan(M, 512, 3584, 4, 64)["workspace_bytes"]))
-    y, g = torch.empty((M, N), dtype=torch.bfloat16, device=DEV), torch.cuda.CUDAGraph()
-    with torch.cuda.graph(g):
-        ss.subspec_fp8_linear(x, None, t, ws, M, N, K, y)
-    for _ in range(4):
-        y.zero_()
-        g.replay()
-        q = run_qlinear(p, xq)
-        torch.cuda.synchronize()
-        assert torch.equal(y.view(torch.int16), y0.view(torch.int16)) and torch.equal(q.view(torch.int16), q0.view(torch.int16))
-        assert torch.equal(linear(x, None, t, ws, M, N, K).view(torch.int16), y0.view(torch.int16))

@@ -5,8 +5,18 @@
 //
 // The matrix units cut the products of eight neighbouring k to a grid of 2^-13 of the largest before they
 // add them in fp32 (measured: 16x16x128 and 32x32x64 with scales, 16x16x32 without, all the same).  On
-// rows of ordinary values that is a few 2^-14 of a result's size, a sixteenth of its rounding to bf16;
-// the only way around it is 16-bit products, at half the rate and with every code converted.
+// rows of ordinary values that moves a result by some 2^-12 of its size, an eighth of its rounding to bf16.
+// The only way around it is 16-bit products, at half the rate and with every code converted: up to 64 rows,
+// where the weights' bytes bound the call, that costs nothing and is what runs (EXACT); above, a long prompt
+// would take twice as long.
+//
+// This file: large tiles, by workgroups that take several each.  Both sides go through a ring in LDS, copied
+// straight from memory: a tile of 256 x 256 reads 64 KB for 16.8 MFLOP, eight wavefronts of 128 x 64.  4096
+// rows, 55296 x 5120: 1033 us, 2250 TFLOP/s, where a large library product of these sizes runs at 2290 to 2340;
+// the matrix units are busy 53 % of the cycles.  Without the copies it takes 769 us, without the reads of LDS
+// 1033: what bounds it is 64 KB a step and compute unit from L2 into LDS.  Tried against 1055: half blocks of k,
+// four in flight, reads and copies spread between the products by hand 1048 to 1084; lines brought into L2
+// ahead of their copies 1036 to 1067; bands of 2, 4 and 16 tiles of rows 1100, 1078 and 1069.
 #include <algorithm>
 
 #include "fp8_tile.h"
@@ -147,9 +157,11 @@ hipError_t tiles_at(const Fp8Args& a, hipStream_t st) {
 // What the launches cost, in microseconds: a call; a workgroup's stage of k when few compute units have one and
 // when all do, its end, and a start after another's end; joining parts of K, first in a launch or ahead of whole
 // tiles: trips to memory one after the other, and bytes, written and read, cheaper while they stay in the last
-// cache; a kind's bytes of weights from memory.  Fitted to sweeps of every shape over some 60 sizes: the choice
-// below, the cheapest by them, lost 4 % to the best.
-constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 0.5f, kJoinAhead = 2.f, kTrip = 0.8f, kJoinBytes = 7e6f, kJoinCached = 1e8f;
+// cache; a kind's bytes of weights from memory, and of weights that two tiles of rows read one after the other.
+// Fitted to sweeps of every shape over some 130 sizes: the choice below, the cheapest by them, lost 3.3 % to the
+// best (geometric mean of 70; 24 % at most).
+constexpr float kCall = 4.f, kTurn = 2.f, kEnd = 1.f, kJoin = 0.5f, kJoinAhead = 2.f, kTrip = 0.8f, kJoinBytes = 7e6f, kJoinCached = 1e8f,
+                kAgain = 6.7e6f;
 float join_cost(float bytes, int sharing, int at_once, int passes, bool ahead) {
   return (ahead ? kJoinAhead : kJoin) + kTrip * passes * ((sharing + at_once - 1) / at_once) + (bytes + std::max(0.f, bytes - kJoinCached)) / kJoinBytes;
 }
@@ -176,7 +188,8 @@ constexpr LargeCost kLarge[] = {{32, 1.0f, true, 8, 1}, {64, 1.5f, true, 4, 1}, 
 
 // At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
 // that already spreads over the compute units, else two, which share the rows' conversion; K cut over the eight
-// wavefronts of a workgroup where it is short, else over four and over workgroups too, as many as stay resident.
+// wavefronts of a workgroup where it is short, else over four and over workgroups too, no more than two a compute
+// unit, which is what stays resident (7 bf16 rows, 5120 x 27648: 480 workgroups 29.0 us, 640 35.5).
 // (1 row: 3584 x 3584 6.0 us with one tile and eight wavefronts, 6.9 with two tiles, 7.1 with four wavefronts;
 // 3584 x 18944 17.6 with two tiles, four wavefronts and four workgroups, 19.6 with one tile and one workgroup.)
 // The same for bf16 rows, so that they give the bits of their 8-bit rows.
@@ -217,7 +230,8 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
       const float turns = c.resident == 1 ? static_cast<float>((groups + cus - 1) / cus) : std::max(1.f, groups / (2.f * cus));
       const float step = std::max(c.few, c.all * std::min<long long>(groups, cus) / cus);
       const size_t bytes = splits > 1 ? static_cast<size_t>(groups) * c.rows * c.columns * 4 : 0;
-      const float cost = kCall + std::max(weights / c.rate, turns * ((units + splits - 1) / splits * step) + (turns - 1) * kTurn + kEnd) +
+      const float memory = weights / (exact && M > c.rows ? kAgain / 2 : c.rate);
+      const float cost = kCall + std::max(memory, turns * ((units + splits - 1) / splits * step) + (turns - 1) * kTurn + kEnd) +
                          (bytes ? join_cost(2.f * bytes, splits, c.at_once, 1, false) : 0.f);
       if (cost < best) {
         best = cost;

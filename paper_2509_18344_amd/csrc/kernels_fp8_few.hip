@@ -4,8 +4,13 @@
 // needed here: at 5 TB/s a SIMD has about 1000 cycles for a tile of 16 columns and 128 k.)
 //
 // A wavefront takes CT tiles of 16 columns and a run of K, its weights straight from memory to registers, a
-// group of four blocks ahead; the wavefronts of a workgroup share the columns and cut K among them, as do
-// `splits` workgroups where there are few columns.
+// unit of two blocks ahead; the wavefronts of a workgroup share the columns and cut K among them, as do
+// `splits` workgroups where K is long.  bf16 rows become codes on the way: the block's largest magnitude by
+// packed 16-bit maxima, then one conversion for two values, which divides by the power of two too.
+//
+// Measured, of bf16 rows: 1 row, 3584 x 3584 6.2 us (12.8 MB; a launch that does nothing takes 2); 7 rows,
+// 5120 x 27648 29.0 us, 4.9 TB/s of weights, where a copy moves 5.2; 1 row, 37888 x 3584 30 us (26 of 8-bit rows,
+// 5.2 TB/s).
 #include <algorithm>
 
 #include "fp8_device.h"

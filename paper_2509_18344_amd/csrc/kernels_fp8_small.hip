@@ -1,6 +1,13 @@
 // The product in 8-bit floating point where tiles are few: a workgroup takes one smaller tile, or a run of its
 // K, and its wavefronts cut every stage's blocks of k among them too, so that a short tile still keeps all its
 // wavefronts busy and most of the sums over K meet in LDS.
+//
+// A step costs a round trip of its copies (0.6 us) while few compute units have one, then their bytes: 66 KB
+// a compute unit in 1.4 us, 12 TB/s out of L2 (64 x 64); with exact products (up to 64 rows) the conversion
+// of codes to bf16, 1.5 us for 64 x 128 x 256.  Measured: 289 rows, 7168 x 5120: 24.6 us in 224 workgroups of
+// 96 x 128, where 128 x 128 takes 30 in 168 and large tiles of 128 x 256 with K in two 30; 49 rows, 3584 x 18944:
+// 22.7 us in 224 workgroups of 64 x 64, four a tile (37 in large tiles); 32 rows, 55296 x 5120: 52.5 us, 5.4 TB/s
+// of weights, with two workgroups a compute unit, whose starts and ends overlap (59 with one).
 #include <algorithm>
 
 #include "fp8_tile.h"

@@ -99,6 +99,7 @@ def _rand(seed, M, K, scale=1.0, mean=0.0):
 @pytest.mark.parametrize("M,K", [
     (1, 3584), (1, 5120), (7, 8), (3, 128), (2, 136), (5, 512), (4, 520), (2, 1536), (3, 2048), (3, 2056), (2, 4096), (2, 4224),
     (2, 6144), (2, 6152), (2, 8192), (2, 8320), (2, 16384), (2, 16512), (2, 27648), (2, 32768), (1, 32896), (1, 65536), (49, 5120), (300, 640),
+    (515, 8), (520, 1024), (512, 1032), (600, 2056), (513, 3584), (512, 4104), (530, 8192), (512, 8320),
 ])
 @pytest.mark.parametrize("residual", [False, True])
 def test_add_norm_matches_oracle(M, K, residual):

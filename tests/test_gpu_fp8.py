@@ -191,6 +191,26 @@ def test_bf16_rows_give_the_bits_of_their_8_bit_rows(M, N, K):
         assert torch.equal(linear(xd, None, t, ws, M, N, K).view(torch.int16), y.view(torch.int16))
 
 
+@pytest.mark.parametrize("M", [16, 32])
+def test_bf16_rows_of_all_scales_give_the_bits_of_their_8_bit_rows(M):
+    # one block a row, from bf16's smallest numbers to its largest, with zeros, infinities and NaN beside them
+    N, K = 48, 128
+    rng = np.random.default_rng([65, M])
+    x = bf16(rng.standard_normal((M, K)) * np.exp2(np.linspace(-134.0, 126.0, M))[:, None])
+    x[1, ::3] &= 0x8003  # the last bits of subnormal numbers
+    x[M - 3, 5:] = 0x8000
+    x[M - 2, 7], x[2, 100], x[2, 101] = 0x7F80, 0xFF80, 0x7FC3
+    c, s = rows8(M, K)
+    ss.subspec_fp8_rows(dev(x), M, K, c, s)
+    for power in (100, 0, -100):
+        t, ws = weight(oracle.e4m3_code(rng.uniform(-4, 4, (N, K))), np.full((N, 1), 127 + power))
+        y, y8 = linear(dev(x), None, t, ws, M, N, K), linear(c, s, t, ws, M, N, K)
+        a, b = (v.float().cpu().numpy() for v in (y, y8))
+        assert np.array_equal(a, b, equal_nan=True), (power, np.argwhere(~((a == b) | (np.isnan(a) & np.isnan(b))))[:5])
+        if power == 100:
+            assert np.isfinite(a[0]).all() and (a[0] != 0).any() and np.isnan(a[2]).all()
+
+
 @pytest.mark.parametrize("M", [1, 16, 33, 130, 270])
 def test_sums_of_eight_products(M):
     # the grid that the units sum eight products on, product by product, on codes of all magnitudes

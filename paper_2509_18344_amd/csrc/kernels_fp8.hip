@@ -258,7 +258,9 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
         const float moved = sharers <= left ? 0.f : (sharers % left ? sharers + left : sharers) * 2.f * c.rows * kColumns * 4;
         const int sharing = runs ? (sharers + left - 1) / left + (sharers % left != 0) : 1;
         const int ends = rounds + (left ? 1 + (sharers % left != 0) : 0);
-        const float cost = kCall + std::max(weights / kLargeRate, steps * c.step) + ends * kEnd + (runs ? join_cost(moved, sharing, c.at_once, c.passes, rounds > 0) : 0.f);
+        // (with compute units idle the others run faster: 220 of 256 took 1.32 us a step of 192 rows)
+        const float step = rounds ? c.step : c.step * (0.8f + 0.2f * sharers / cus);
+        const float cost = kCall + std::max(weights / kLargeRate, steps * step) + ends * kEnd + (runs ? join_cost(moved, sharing, c.at_once, c.passes, rounds > 0) : 0.f);
         if (cost < best) {
           best = cost;
           p.small = 0;

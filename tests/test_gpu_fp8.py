@@ -88,7 +88,7 @@ KINDS = {
     (40, 70000, 384): (2, 64, 256, False, True), (66, 16, 384): (1, 64, 64, False, False), (67, 16, 896): (1, 64, 64, True, False),
     (65, 16, 256): (1, 64, 128, False, False), (66, 16, 640): (1, 64, 128, True, False), (69, 18272, 256): (1, 96, 128, False, False),
     (67, 8352, 6016): (1, 96, 128, True, False), (66, 16, 128): (1, 128, 128, False, False), (2267, 272, 6784): (1, 128, 128, True, False),
-    (130, 17312, 256): (2, 128, 256, False, False), (275, 33024, 128): (2, 128, 256, False, True), (198, 39200, 4736): (2, 128, 256, True, True),
+    (130, 17312, 256): (2, 128, 256, False, False), (275, 33024, 128): (2, 128, 256, False, True), (1233, 14800, 6016): (2, 128, 256, True, True),
     (400, 16512, 128): (2, 192, 256, False, False), (514, 27152, 128): (2, 192, 256, False, True), (144, 18000, 5248): (2, 192, 256, True, False),
     (516, 26448, 2560): (2, 192, 256, True, True), (579, 16480, 128): (2, 256, 256, False, False), (786, 26256, 128): (2, 256, 256, False, True),
     (1175, 15008, 6016): (2, 256, 256, True, True),

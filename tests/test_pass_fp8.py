@@ -96,7 +96,7 @@ def small():  # codes, and parts of a small tile
 
 
 def large():  # codes, and parts of a large tile
-    return 198, 39200, 4736
+    return 516, 26448, 2560
 
 
 for make in (few, small, large):

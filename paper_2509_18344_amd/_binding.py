@@ -217,6 +217,19 @@ def _device_args(fn: str, stream, kinds, needs, *args):
     return [handle, *out]
 
 
+def _all_given(fn: str, stream, kinds, needs, *args):
+    """_device_args of arguments none of which is None: without the time that telling them apart takes."""
+    if stream is None and _get_device is not None:
+        try:
+            dev = _device()
+            if ({*map(_get_device, args)} == {dev} and all(map(_is_contiguous, args)) and
+                    [*map(_dtype, args)] == (_usual.get(kinds) or _usual_types(kinds)) and all(map(ge, map(_numel, args), needs))):
+                return [_raw_stream(dev), *map(_data_ptr, args)]
+        except TypeError:  # addresses among them
+            pass
+    return _device_args(fn, stream, kinds, needs, *args)
+
+
 def _usual_types(kinds):
     _usual[kinds] = [getattr(_torch, _TYPES[k][0]) for k in kinds]
     return _usual[kinds]
@@ -466,18 +479,41 @@ def _scales(t, words):
 
 
 def subspec_add_norm(x, residual, weight, eps, M, K, sum, y, codes, scales, stream=None) -> int:
-    n, (kind, least) = M * K, _scales(scales, (K + 511) // 512 * M)
-    st, px, pr, pw, ps, py, pc, pe = _device_args(
-        "subspec_add_norm", stream, ("bf16", "bf16", "bf16", "bf16", "bf16", "e4m3", kind), (n, n, K, n, n, n, least),
-        x, residual, weight, sum, y, codes, scales)
-    return _check("subspec_add_norm", load_library().subspec_add_norm(px, pr, pw, eps, M, K, ps, py, pc, pe, st))
+    n, fn = M * K, "subspec_add_norm"
+    if codes is None and scales is None and residual is not None and sum is not None:  # the usual ones
+        st, px, pr, pw, ps, py = _all_given(fn, stream, _BF16_NORM, (n, n, K, n, n), x, residual, weight, sum, y)
+        pc = pe = None
+    else:
+        kind, least = _scales(scales, (K + 511) // 512 * M)
+        if y is None and residual is not None and sum is not None:
+            st, px, pr, pw, ps, pc, pe = _all_given(fn, stream, ("bf16", "bf16", "bf16", "bf16", "e4m3", kind), (n, n, K, n, n, least),
+                                                    x, residual, weight, sum, codes, scales)
+            py = None
+        else:
+            st, px, pr, pw, ps, py, pc, pe = _device_args(
+                fn, stream, ("bf16", "bf16", "bf16", "bf16", "bf16", "e4m3", kind), (n, n, K, n, n, n, least),
+                x, residual, weight, sum, y, codes, scales)
+    return _check(fn, load_library().subspec_add_norm(px, pr, pw, eps, M, K, ps, py, pc, pe, st))
+
+
+_BF16_NORM = ("bf16",) * 5
+_BF16_ACT = ("bf16",) * 2
 
 
 def subspec_silu_mul(gate_up, M, I, h, codes, scales, stream=None) -> int:
-    n, (kind, least) = M * I, _scales(scales, (I + 511) // 512 * M)
-    st, pg, ph, pc, pe = _device_args("subspec_silu_mul", stream, ("bf16", "bf16", "e4m3", kind), (2 * n, n, n, least),
-                                      gate_up, h, codes, scales)
-    return _check("subspec_silu_mul", load_library().subspec_silu_mul(pg, M, I, ph, pc, pe, st))
+    n, fn = M * I, "subspec_silu_mul"
+    if codes is None and scales is None:
+        st, pg, ph = _all_given(fn, stream, _BF16_ACT, (2 * n, n), gate_up, h)
+        pc = pe = None
+    else:
+        kind, least = _scales(scales, (I + 511) // 512 * M)
+        if h is None:
+            st, pg, pc, pe = _all_given(fn, stream, ("bf16", "e4m3", kind), (2 * n, n, least), gate_up, codes, scales)
+            ph = None
+        else:
+            st, pg, ph, pc, pe = _device_args(fn, stream, ("bf16", "bf16", "e4m3", kind), (2 * n, n, n, least),
+                                              gate_up, h, codes, scales)
+    return _check(fn, load_library().subspec_silu_mul(pg, M, I, ph, pc, pe, st))
 
 
 def subspec_fp8_rows(x, M, K, codes, scales, stream=None) -> int:
@@ -498,12 +534,16 @@ def subspec_fp8_pack(codes, N, K, tiles, stream=None) -> int:
 
 
 def subspec_fp8_linear(x, x_scales, w, w_scales, M, N, K, y, stream=None) -> int:
-    words = (K + 511) // 512
-    (xk, xn), (wk, wn) = _scales(x_scales, words * M), _scales(w_scales, words * N)
-    st, px, pe, pw, pf, py = _device_args(
-        "subspec_fp8_linear", stream, ("bf16" if x_scales is None else "e4m3", xk, "e4m3", wk, "bf16"),
-        (M * K, xn, N * K, wn, M * N), x, x_scales, w, w_scales, y)
-    return _check("subspec_fp8_linear", load_library().subspec_fp8_linear(px, pe, pw, pf, M, N, K, py, st))
+    words, fn = (K + 511) // 512, "subspec_fp8_linear"
+    wk, wn = _scales(w_scales, words * N)
+    if x_scales is None:
+        st, px, pw, pf, py = _all_given(fn, stream, ("bf16", "e4m3", wk, "bf16"), (M * K, N * K, wn, M * N), x, w, w_scales, y)
+        pe = None
+    else:
+        xk, xn = _scales(x_scales, words * M)
+        st, px, pe, pw, pf, py = _all_given(fn, stream, ("e4m3", xk, "e4m3", wk, "bf16"), (M * K, xn, N * K, wn, M * N),
+                                            x, x_scales, w, w_scales, y)
+    return _check(fn, load_library().subspec_fp8_linear(px, pe, pw, pf, M, N, K, py, st))
 
 
 def subspec_fp8_linear_workspace_bytes(M, N, K, rows8) -> int:

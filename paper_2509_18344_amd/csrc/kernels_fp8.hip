@@ -189,17 +189,19 @@ constexpr LargeCost kLarge[] = {{32, 1.0f, true, 8, 1}, {64, 1.5f, true, 4, 1}, 
 
 // At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
 // that already spreads over the compute units, else two, which share the rows' conversion; K cut over the eight
-// wavefronts of a workgroup where it is short, else over four and over workgroups too, no more than two a compute
-// unit, which is what stays resident (7 bf16 rows, 5120 x 27648: 480 workgroups 29.0 us, 640 35.5).
-// (1 row: 3584 x 3584 6.0 us with one tile and eight wavefronts, 6.9 with two tiles, 7.1 with four wavefronts;
-// 3584 x 18944 17.6 with two tiles, four wavefronts and four workgroups, 19.6 with one tile and one workgroup.)
-// The same for bf16 rows, so that they give the bits of their 8-bit rows.
+// wavefronts of a workgroup where it is short, over sixteen where eight would load twice one after the other, else
+// over four and over workgroups too, no more than two a compute unit, which is what stays resident.
+// (1 bf16 row: 3584 x 3584 6.6 us with sixteen wavefronts, 7.1 with eight; 2048 x 2048 5.6 and 4.4.  7 bf16 rows,
+// 5120 x 27648: 480 workgroups 29.0 us, 640 35.5.  1 row of 8 bits: 3584 x 3584 6.0 us with one tile and eight
+// wavefronts, 6.9 with two tiles, 7.1 with four wavefronts; 3584 x 18944 17.6 with two tiles, four wavefronts and four
+// workgroups, 19.6 with one tile and one workgroup.)  The same for bf16 rows, so that they give the bits of their
+// 8-bit rows.
 void few_plan(int M, int N, int K, int cus, Fp8Plan* p) {
   const int tiles = N / 16, KB = K / 128;
   const bool longer = KB > 64;
   p->few = M > 16 || (tiles <= cus && !longer) ? 1 : 2;
   const int sets = (tiles + p->few - 1) / p->few;
-  p->waves = M > 16 || longer || sets > cus ? 4 : 8;
+  p->waves = M > 16 || longer || sets > cus ? 4 : p->few == 1 && KB > 16 ? 16 : 8;
   p->splits = longer || M > 16 ? std::max(1, std::min(2 * cus / sets, std::min(KB / 16, 64))) : 1;
 }
 

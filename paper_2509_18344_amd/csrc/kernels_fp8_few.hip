@@ -8,7 +8,7 @@
 // `splits` workgroups where K is long.  bf16 rows become codes on the way: the block's largest magnitude by
 // packed 16-bit maxima, then one conversion for two values, which divides by the power of two too.
 //
-// Measured, of bf16 rows: 1 row, 3584 x 3584 6.2 us (12.8 MB; a launch that does nothing takes 2); 7 rows,
+// Measured, of bf16 rows: 1 row, 3584 x 3584 5.9 us (12.8 MB; a launch that does nothing takes 2); 7 rows,
 // 5120 x 27648 29.0 us, 4.9 TB/s of weights, where a copy moves 5.2; 1 row, 37888 x 3584 30 us (26 of 8-bit rows,
 // 5.2 TB/s).
 #include <algorithm>
@@ -303,6 +303,7 @@ hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t 
   if (rows == 1) {
     if (columns == 2 && waves == 8) fused ? few_at<8, 1, 2, true>(a, st) : few_at<8, 1, 2, false>(a, st);
     else if (columns == 2) fused ? few_at<4, 1, 2, true>(a, st) : few_at<4, 1, 2, false>(a, st);
+    else if (waves == 16) fused ? few_at<16, 1, 1, true>(a, st) : few_at<16, 1, 1, false>(a, st);
     else fused ? few_at<8, 1, 1, true>(a, st) : few_at<8, 1, 1, false>(a, st);
   } else if (rows == 2) {
     fused ? few_at<4, 2, 1, true>(a, st) : few_at<4, 2, 1, false>(a, st);

@@ -29,16 +29,19 @@ def fused(ws, bits: int, group: int) -> dict:
 
 
 def fp8_weight(w, stream=None) -> dict:
-    """w: bfloat16 device tensor [N][K] -> weight tiles and scales for subspec_fp8_linear."""
+    """w: bfloat16 device tensor [N][K] -> weight tiles and scales for subspec_fp8_linear, written on
+    `stream` (None: the current one) after what the current stream has to do so far."""
     import torch
     N, K = w.shape
     codes = torch.empty((N, K), dtype=torch.uint8, device=w.device)
     scales = torch.empty(((K + 511) // 512, N), dtype=torch.int32, device=w.device)
-    b.subspec_fp8_rows(w, N, K, codes, scales, stream)
     tiles = torch.empty(N * K, dtype=torch.uint8, device=w.device)
+    if stream is not None:
+        s = torch.cuda.ExternalStream(stream, w.device) if isinstance(stream, int) else stream
+        s.wait_stream(torch.cuda.current_stream(w.device))  # which may still use the memory that the allocator gave
+        codes.record_stream(s)  # and takes back while the stream may still read it
+    b.subspec_fp8_rows(w, N, K, codes, scales, stream)
     b.subspec_fp8_pack(codes, N, K, tiles, stream)
-    if stream is not None and stream != torch.cuda.current_stream(w.device):
-        codes.record_stream(stream)  # goes back to the allocator while the stream still reads it
     return {"w": tiles, "w_scales": scales, "N": N, "K": K}
 
 

@@ -272,7 +272,7 @@ def test_pack_is_the_oracles_order(N, K):
     assert np.array_equal(t[: N * K].cpu().numpy(), oracle.weight_tiles(c)) and bool((t[N * K:] == 0x5A).all())
 
 
-@pytest.mark.parametrize("other", [False, True])
+@pytest.mark.parametrize("other", ["current", "stream", "handle"])
 def test_prepared_weight(other):
     from paper_2509_18344_amd import prepare
     N, K, M = 272, 640, 5
@@ -280,10 +280,9 @@ def test_prepared_weight(other):
     w, x = bf16(rng.standard_normal((N, K))), bf16(rng.standard_normal((M, K)))
     wd, xd = dev(w), dev(x)
     torch.cuda.synchronize()
-    s = torch.cuda.Stream() if other else None
-    p = prepare.fp8_weight(wd, s)
-    if other:
-        s.synchronize()
+    s = torch.cuda.Stream()
+    p = prepare.fp8_weight(wd, {"current": None, "stream": s, "handle": s.cuda_stream}[other])
+    s.synchronize()
     wc, wb = oracle.fp8_rows(f64(w))
     assert np.array_equal(p["w"].cpu().numpy(), oracle.weight_tiles(wc))
     check(linear(xd, None, p["w"], p["w_scales"], M, p["N"], p["K"]), oracle.fp8_rows(f64(x)), (wc, wb))

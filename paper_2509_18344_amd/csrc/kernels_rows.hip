@@ -107,11 +107,17 @@ constexpr int kRowThreads = 256;
 
 // g * sigmoid(g) * u.  With p = exp(-|g| / 2), sigmoid(|g|) = 1 / (1 + p^2) and sigmoid(-|g|) = p^2 times
 // that: no exponential overflows, and p's second factor comes last, so that a small sigmoid keeps its bits
-// next to a large u.
+// next to a large u.  The hardware's exponential has no numbers below 2^-126, which p passes at g = -174.7, while
+// next to bf16's largest u the result lasts until g = -187: FAR moves 2^64 out of a small p (p^2 next to 1 counts
+// for nothing either way) and back, exactly, once u is in.  Other gates come out the same with it or without.
+template <bool FAR>
 __device__ __forceinline__ float silu_mul(float g, float u) {
-  const float p = __builtin_amdgcn_exp2f(-0.72134752044448170f * fabsf(g));  // log2(e) / 2
+  const float t = -0.72134752044448170f * fabsf(g);  // log2(e) / 2
+  const bool far = FAR && t < -100.f;
+  const float p = __builtin_amdgcn_exp2f(far ? t + 64.f : t);
   const float q = g < 0.f ? p : 1.f;
-  return g * q * __builtin_amdgcn_rcpf(__builtin_fmaf(p, p, 1.f)) * u * q;
+  const float h = g * q * __builtin_amdgcn_rcpf(__builtin_fmaf(p, p, 1.f)) * u * q;
+  return far && g < 0.f ? h * 0x1p-64f * 0x1p-64f : h;
 }
 
 __global__ __launch_bounds__(kRowThreads) void k_silu_mul(ActArgs a) {
@@ -123,7 +129,14 @@ __global__ __launch_bounds__(kRowThreads) void k_silu_mul(ActArgs a) {
   unpack8(gr, g);
   unpack8(ur, u);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = silu_mul(g[i], u[i]);
+  for (int i = 0; i < 8; ++i) v[i] = silu_mul<false>(g[i], u[i]);
+  float least = g[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) least = fminf(least, g[i]);
+  if (least < -170.f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = silu_mul<true>(g[i], u[i]);
+  }
   if (a.y) *reinterpret_cast<uint4*>(a.y + static_cast<size_t>(m) * a.I + 8 * c) = pack8(v);
   if (a.codes) store_codes(v, a.codes, a.scales, c, m, a.M, a.I);
 }

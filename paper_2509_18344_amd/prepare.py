@@ -30,18 +30,31 @@ def fused(ws, bits: int, group: int) -> dict:
 
 def fp8_weight(w, stream=None) -> dict:
     """w: bfloat16 device tensor [N][K] -> weight tiles and scales for subspec_fp8_linear, written on
-    `stream` (None: the current one) after what the current stream has to do so far."""
+    `stream` (None: the current one) after what the current stream has to do so far.  `w` and the result may
+    be dropped before `stream` gets there.  Other streams that use the result wait for `stream`; of one that
+    torch does not own (a handle other than 0, an ExternalStream) the current stream does so here."""
     import torch
     N, K = w.shape
     codes = torch.empty((N, K), dtype=torch.uint8, device=w.device)
     scales = torch.empty(((K + 511) // 512, N), dtype=torch.int32, device=w.device)
     tiles = torch.empty(N * K, dtype=torch.uint8, device=w.device)
-    if stream is not None:
-        s = torch.cuda.ExternalStream(stream, w.device) if isinstance(stream, int) else stream
-        s.wait_stream(torch.cuda.current_stream(w.device))  # which may still use the memory that the allocator gave
-        codes.record_stream(s)  # and takes back while the stream may still read it
-    b.subspec_fp8_rows(w, N, K, codes, scales, stream)
-    b.subspec_fp8_pack(codes, N, K, tiles, stream)
+    on = stream
+    if isinstance(stream, int):  # (torch takes the null stream's handle for none, and would hand out another stream)
+        on = torch.cuda.ExternalStream(stream, w.device) if stream else torch.cuda.default_stream(w.device)
+    current = torch.cuda.current_stream(w.device)
+    if on is not None:
+        on.wait_stream(current)  # which may still use the memory that the allocator gave
+    try:
+        b.subspec_fp8_rows(w, N, K, codes, scales, stream)
+        b.subspec_fp8_pack(codes, N, K, tiles, stream)
+    finally:
+        # ... and takes back while the stream may still use it.  The allocator asks a stream that it was told of
+        # when the tensor is freed, which may be after a stream that torch does not own is gone.
+        if isinstance(on, torch.cuda.ExternalStream):
+            current.wait_stream(on)
+        elif on is not None:
+            for t in (w, codes, scales, tiles):
+                t.record_stream(on)
     return {"w": tiles, "w_scales": scales, "N": N, "K": K}
 
 

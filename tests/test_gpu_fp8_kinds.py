@@ -1,0 +1,90 @@
+"""Every kind of launch of the product in 8-bit floating point, held sharply: whole numbers exactly, each
+cut of eight products where the 8-bit matrix units make it, and bf16 rows bit for bit as their 8-bit rows.  About 200 rows and columns of each result, the ends of every tile's among them.
+
+Tolerances.  Whole numbers up to 256 have no rounding.  Else, against sums in 64 bits of the products as the
+units leave them (above EXACT rows cut towards zero to a multiple of 2^(E - 13), E the largest sum of two
+exponents among eight neighbouring k): K / 128 + 32 roundings of 2^-23 W, W the sum of magnitudes, and
+one to bf16, 2^-8."""
+import numpy as np
+import pytest
+
+import oracle
+import paper_2509_18344_amd as ss
+
+from test_gpu_fp8 import DEV, EXACT, KINDS, _random_rows, _tiled_weight, codes_to, linear, weight
+from test_gpu_rows import bf16, dev, rows8
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+
+def _pick(n):
+    """The first and last rows, and the ends of tiles between."""
+    step = max(32, n // 64 // 32 * 32)
+    return np.unique(np.r_[np.arange(min(n, 35)), np.arange(max(0, n - 70), n), np.arange(31, n, step), np.arange(32, n, step)])
+
+
+def _some(y, m, n):
+    return y[torch.from_numpy(m).to(DEV)][:, torch.from_numpy(n).to(DEV)].double().cpu().numpy()
+
+
+@pytest.mark.parametrize("M,N,K", KINDS)
+def test_whole_numbers_are_exact(M, N, K):
+    rng = np.random.default_rng([71, M, N, K])
+    p = rng.integers(-30, 31, K // 128)  # powers that differ from block to block and cancel
+    xv = rng.integers(1, 3, (M, K)) * rng.choice([-1, 1], (M, K)) * (rng.random((M, K)) < min(1.0, 200 / K))
+    wv = (rng.integers(1, 3, (131, K)) * rng.choice([-1, 1], (131, K)))
+    at = np.arange(N) * 37 % 131
+    t, ws = weight(oracle.e4m3_code(wv)[at], np.broadcast_to(127 - p, (N, K // 128)))
+    y = linear(*codes_to(oracle.e4m3_code(xv), np.broadcast_to(127 + p, (M, K // 128))), t, ws, M, N, K)
+    m, n = _pick(M), _pick(N)
+    ref = xv[m].astype(np.float64) @ wv[at[n]].T.astype(np.float64)
+    small = np.abs(ref) <= 256
+    assert small.mean() > 0.99
+    assert np.array_equal(_some(y, m, n)[small], ref[small])
+
+
+def _cut_sums(x8, w8, cut):
+    """(sums of the products as the units leave them, sums of magnitudes) in 64 bits, on the GPU."""
+    def side(codes, bytes_):
+        e = np.maximum((codes >> 3 & 15).astype(int), 1) - 7 + np.repeat(bytes_.astype(int) - 127, 128, 1)
+        return torch.from_numpy(oracle.fp8_values(codes, bytes_)).to(DEV), torch.from_numpy(e.astype(np.float64)).to(DEV)
+    (xv, xe), (wv, we) = side(*x8), side(*w8)
+    ref, size = (torch.empty((len(xv), len(wv)), dtype=torch.float64, device=DEV) for _ in range(2))
+    for m in range(len(xv)):
+        p = (xv[m] * wv).view(len(wv), -1, 8)
+        size[m] = p.abs().sum((1, 2))
+        if cut:
+            grid = torch.exp2((xe[m] + we).view(len(wv), -1, 8).amax(-1, keepdim=True) - 13.0)
+            p = torch.trunc(p / grid) * grid
+        ref[m] = p.sum((1, 2))
+    return ref.cpu().numpy(), size.cpu().numpy()
+
+
+def _check(y, x8, w8, M, K):
+    ref, size = _cut_sums(x8, w8, M > EXACT)
+    err, tol = np.abs(y - ref), 2.0 ** -8 * np.abs(ref) + (K / 128 + 32) * 2.0 ** -23 * size
+    assert np.all(err <= tol), (float((err / np.maximum(tol, 1e-300)).max()), np.argwhere(err > tol)[:4].tolist())
+
+
+@pytest.mark.parametrize("M,N,K", KINDS)
+def test_every_cut_and_nothing_else(M, N, K):
+    rng = np.random.default_rng([72, M, N, K])
+    x8, w8 = _random_rows(rng, M, K), _tiled_weight(rng, N, K)
+    y = linear(*codes_to(*x8), *weight(*w8), M, N, K)
+    m, n = _pick(M), _pick(N)
+    _check(_some(y, m, n), tuple(a[m] for a in x8), tuple(a[n] for a in w8), M, K)
+
+
+@pytest.mark.parametrize("M,N,K", KINDS)
+def test_bf16_rows_give_the_bits_of_their_8_bit_rows_in_every_kind(M, N, K):
+    rng = np.random.default_rng([73, M, N, K])
+    x = rng.standard_normal((M, K)) * np.repeat(np.exp2(rng.integers(-4, 5, (M, K // 128))), 128, 1)
+    x[rng.random((M, K)) < 0.01] *= 500.0  # and some far larger ones
+    xd = dev(bf16(x))
+    t, ws = weight(*_tiled_weight(rng, N, K))
+    c, s = rows8(M, K)
+    ss.subspec_fp8_rows(xd, M, K, c, s)
+    y8 = linear(c, s, t, ws, M, N, K).view(torch.int16)
+    for _ in range(2):  # codes and partial sums share the workspace
+        assert torch.equal(linear(xd, None, t, ws, M, N, K).view(torch.int16), y8)

@@ -68,6 +68,10 @@ __device__ __forceinline__ bf16x8_t fp8_as_bf16(uint32_t lo, uint32_t hi, float 
 
 // Whether codes under this scale are normal bf16 numbers and finite: they span 2^-9 .. 448.
 __device__ __forceinline__ bool fp8_plain(uint32_t scale_byte) { return scale_byte - 16u < 224u; }
+// Whether codes or'ed together are all zeros, of either sign.  A block of zeros has the smallest scale, yet any power
+// makes bf16 zeros of them: a row of padding must not send the rows beside it down the way of far scales, whose
+// sums round elsewhere and which takes longer (64 rows, 55296 x 5120, one of them zeros: 75.3 us, 68.8 so; 66 without).
+__device__ __forceinline__ bool fp8_zeros(uint32_t any) { return (any & 0x7F7F7F7Fu) == 0; }
 __device__ __forceinline__ float fp8_power(uint32_t scale_byte) { return __uint_as_float(scale_byte << 23); }
 
 // Where the scale byte of block b of row m lies.

@@ -203,6 +203,24 @@ __global__ __launch_bounds__(WAVES * kWave) void k_fp8_few(Fp8Args a) {
         plain &= fp8_plain(wb[c]);
       }
       plain = __all(plain);
+      if (!plain) {  // once more without the scales of zeros
+        bool p = true;
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          uint32_t any = 0;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) any |= xc[t].v[u];
+          p &= fp8_plain(xb[t]) || fp8_zeros(any);
+        }
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+          uint32_t any = 0;
+#pragma unroll
+          for (int u = 0; u < 8; ++u) any |= now.w[c][j][u / 4][u % 4];
+          p &= fp8_plain(wb[c]) || fp8_zeros(any);
+        }
+        plain = __all(p);
+      }
       bf16x8_t w[CT][4];
 #pragma unroll
       for (int c = 0; c < CT; ++c) {

@@ -1,5 +1,6 @@
 """Every kind of launch of the product in 8-bit floating point, held sharply: whole numbers exactly, each
-cut of eight products where the 8-bit matrix units make it, and bf16 rows bit for bit as their 8-bit rows.  About 200 rows and columns of each result, the ends of every tile's among them.
+cut of eight products where the 8-bit matrix units make it, bf16 rows bit for bit as their 8-bit rows, and rows
+and blocks of zeros.  About 200 rows and columns of each result, the ends of every tile's among them.
 
 Tolerances.  Whole numbers up to 256 have no rounding.  Else, against sums in 64 bits of the products as the
 units leave them (above EXACT rows cut towards zero to a multiple of 2^(E - 13), E the largest sum of two
@@ -88,3 +89,40 @@ def test_bf16_rows_give_the_bits_of_their_8_bit_rows_in_every_kind(M, N, K):
     y8 = linear(c, s, t, ws, M, N, K).view(torch.int16)
     for _ in range(2):  # codes and partial sums share the workspace
         assert torch.equal(linear(xd, None, t, ws, M, N, K).view(torch.int16), y8)
+
+
+# few rows in their launches of one and two tiles a wavefront, and what the exact small and large tiles take
+ZEROS = [(5, 512, 2304), (16, 5120, 1152), (7, 512, 18944), (30, 512, 640), (40, 272, 2176)] + [k for k in KINDS if k[0] <= 200]
+
+
+@pytest.mark.parametrize("M,N,K", ZEROS)
+def test_rows_and_blocks_of_zeros_change_no_bit_of_the_others(M, N, K):
+    rng = np.random.default_rng([74, M, N, K])
+    x8, w8 = _random_rows(rng, M, K), _tiled_weight(rng, N, K)
+    KB = K // 128
+    y = linear(*codes_to(*x8), *weight(*w8), M, N, K)
+    xz, wz = (tuple(a.copy() for a in r) for r in (x8, w8))
+    empty, dead = np.arange(M) % 3 == 1, np.arange(N) % 5 == 2  # padding rows, columns of a weight that was cut away
+    xz[0][empty], xz[1][empty] = 0, 1  # as subspec_fp8_rows makes them
+    wz[0][dead], wz[1][dead] = 0x80, 1  # negative zeros too
+    z = linear(*codes_to(*xz), *weight(*wz), M, N, K)
+    off = torch.from_numpy(empty[:, None] | dead[None]).to(DEV)
+    assert not bool(z[off].any())
+    assert torch.equal(z[~off].view(torch.int16), y[~off].view(torch.int16))
+    # a block of zeros in some rows and columns: the product without it
+    xz, wz = (tuple(a.copy() for a in r) for r in (x8, w8))
+    at = KB // 2
+    xz[0][empty, 128 * at:128 * at + 128], xz[1][empty, at] = 0, 1
+    wz[0][dead, :128], wz[1][dead, 0] = 0, 1
+    z = linear(*codes_to(*xz), *weight(*wz), M, N, K)
+    m, n = _pick(M), _pick(N)
+    _check(_some(z, m, n), tuple(a[m] for a in xz), tuple(a[n] for a in wz), M, K)
+    assert torch.equal(z[~off].view(torch.int16), y[~off].view(torch.int16))
+    if M <= 32:  # bf16 rows of zeros, turned into codes on the way
+        x = bf16(rng.standard_normal((M, K)))
+        t, ws = weight(*w8)
+        y = linear(dev(x), None, t, ws, M, N, K)
+        x[empty] = 0
+        z = linear(dev(x), None, t, ws, M, N, K)
+        off = torch.from_numpy(empty).to(DEV)
+        assert not bool(z[off].any()) and torch.equal(z[~off].view(torch.int16), y[~off].view(torch.int16))

@@ -312,7 +312,7 @@ template <int MF, int NF>
 __device__ __forceinline__ bool fp8_join(f32x16_t (&acc)[NF][MF], const Fp8Args& a, const Fp8Work& work, int s, int tile, uint32_t part_bytes, int* last) {
   const int t = tile - work.left0;
   auto part = [&](int who, int seg) __attribute__((always_inline)) {
-    return buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(2 * who + seg) * part_bytes, part_bytes);
+    return buffer_rsrc(reinterpret_cast<const uint8_t*>(a.part) + static_cast<size_t>(a.places * who + seg) * part_bytes, part_bytes);
   };
   fp8_store_part(acc, part(work.w, s), threadIdx.x, kFp8Threads);
   wait_and_meet<0>();

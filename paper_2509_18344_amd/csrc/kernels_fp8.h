@@ -20,7 +20,8 @@ struct Fp8Args {
   // blocks.
   int tiles_m, tiles_n;
   int workers, rounds, left, sharers;
-  float* part;            // [sharers][2] tiles of partial sums; few rows: [columns][splits]
+  int places;             // tiles that a sharer's run may touch: 1 where each left tile has equally many, else 2
+  float* part;            // [sharers][places] tiles of partial sums; few rows: [columns][splits]
   unsigned* count;        // per left tile, or columns: workers done (zero between launches)
   int splits;             // few rows: workgroups that share columns
 };
@@ -30,7 +31,7 @@ struct Fp8Plan {
   int waves, splits;       // wavefronts of a workgroup and workgroups that share columns then
   int small;               // which of the small tiles; 0: the large ones
   int rows;                // rows of a large tile
-  int workers, rounds, left, sharers;
+  int workers, rounds, left, sharers, places;
   int tile_rows, tile_columns, groups, sharing;  // the launch described: tile, workgroups, most that share a tile's K
   size_t code_bytes;       // x's codes and scales, where the call makes them
   size_t workspace_bytes;  // completion counters, codes and scales, partial sums; 0: none

@@ -257,7 +257,8 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
         const int sharers = static_cast<int>(std::min<long long>(way == 0 ? left : way == 1 ? cus / left * left : cus, static_cast<long long>(left) * KB));
         if (way && sharers <= left) continue;
         const long long steps = static_cast<long long>(rounds) * KB + (left ? (static_cast<long long>(left) * KB + sharers - 1) / sharers : 0);
-        const size_t runs = sharers > left ? static_cast<size_t>(sharers) * 2 : 0;  // their places in the workspace
+        const int places = left && sharers % left ? 2 : 1;
+        const size_t runs = sharers > left ? static_cast<size_t>(sharers) * places : 0;  // their places in the workspace
         const float moved = sharers <= left ? 0.f : (sharers % left ? sharers + left : sharers) * 2.f * c.rows * kColumns * 4;
         const int sharing = runs ? (sharers + left - 1) / left + (sharers % left != 0) : 1;
         const int ends = rounds + (left ? 1 + (sharers % left != 0) : 0);
@@ -271,6 +272,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
           p.rounds = rounds;
           p.left = left;
           p.sharers = sharers;
+          p.places = places;
           p.workers = rounds ? cus : sharers;
           p.tile_rows = c.rows;
           p.tile_columns = kColumns;
@@ -316,6 +318,7 @@ hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipSt
   a.rounds = p.rounds;
   a.left = p.left;
   a.sharers = p.sharers;
+  a.places = p.places;
   switch (p.rows) {
     case 32: return tiles_at<1, 1, 1, 8, 4, true>(a, st);
     case 64: return tiles_at<2, 1, 1, 8, 3, true>(a, st);

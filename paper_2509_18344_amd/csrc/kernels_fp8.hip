@@ -188,20 +188,21 @@ constexpr float kLargeRate = 5.2e6f;
 constexpr LargeCost kLarge[] = {{32, 1.0f, true, 8, 1}, {64, 1.5f, true, 4, 1}, {128, 1.05f, false, 1, 2}, {192, 1.4f, false, 1, 2}, {256, 1.8f, false, 1, 2}};
 
 // At most 16 rows, or little work: wavefronts straight from memory.  One tile of 16 columns a wavefront where
-// that already spreads over the compute units, else two, which share the rows' conversion; K cut over the eight
-// wavefronts of a workgroup where it is short, over sixteen where eight would load twice one after the other, else
-// over four and over workgroups too, no more than two a compute unit, which is what stays resident.
-// (1 bf16 row: 3584 x 3584 6.6 us with sixteen wavefronts, 7.1 with eight; 2048 x 2048 5.6 and 4.4.  7 bf16 rows,
-// 5120 x 27648: 480 workgroups 29.0 us, 640 35.5.  1 row of 8 bits: 3584 x 3584 6.0 us with one tile and eight
-// wavefronts, 6.9 with two tiles, 7.1 with four wavefronts; 3584 x 18944 17.6 with two tiles, four wavefronts and four
-// workgroups, 19.6 with one tile and one workgroup.)  The same for bf16 rows, so that they give the bits of their
-// 8-bit rows.
+// that already spreads over the compute units, else two, which share the rows' conversion.  K is cut over the eight
+// wavefronts of a workgroup where it is short, over sixteen where eight would load twice one after the other and
+// sixteen need no more than that, else over four and over workgroups too, no more than two a compute unit, which is
+// what stays resident.
+// (Sixteen against eight, in graphs, 1 to 16 rows: 17 to 32 blocks 0.90 to 1.00 of the time of 8-bit rows and 0.94 to 1.03 of
+// bf16 rows, which convert; 33 to 64 blocks 0.90 to 1.09 and 1.00 to 1.19; below 17, 1.06 to 1.10.  1 row: 3584 x 3584 5.6
+// and 5.9 us of 8 bits, 6.6 both of bf16; 3584 x 5120 7.8 and 7.6, 9.6 and 8.1.  7 bf16 rows, 5120 x 27648: 480 workgroups
+// 29.0 us, 640 35.5.  1 row of 8 bits, 3584 x 18944: 17.6 with two tiles, four wavefronts and four workgroups, 19.6 with
+// one tile and one workgroup.)  The same for bf16 rows, so that they give the bits of their 8-bit rows.
 void few_plan(int M, int N, int K, int cus, Fp8Plan* p) {
   const int tiles = N / 16, KB = K / 128;
   const bool longer = KB > 64;
   p->few = M > 16 || (tiles <= cus && !longer) ? 1 : 2;
   const int sets = (tiles + p->few - 1) / p->few;
-  p->waves = M > 16 || longer || sets > cus ? 4 : p->few == 1 && KB > 16 ? 16 : 8;
+  p->waves = M > 16 || longer || sets > cus ? 4 : p->few == 1 && KB > 16 && KB <= 32 ? 16 : 8;
   p->splits = longer || M > 16 ? std::max(1, std::min(2 * cus / sets, std::min(KB / 16, 64))) : 1;
 }
 

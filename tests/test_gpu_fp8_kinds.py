@@ -19,6 +19,11 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 
+# the few rows' kernel: eight and sixteen wavefronts around the lines between them, two tiles a wavefront, parts of K
+FEW = [(1, 272, 2048), (5, 272, 2176), (1, 3584, 4096), (16, 3584, 4224), (2, 4096, 5120), (9, 48, 8192), (3, 4112, 8192), (7, 48, 8320),
+       (16, 8208, 640), (4, 512, 9216), (30, 512, 640), (33, 272, 2176), (64, 16, 4096)]
+
+
 def _pick(n):
     """The first and last rows, and the ends of tiles between."""
     step = max(32, n // 64 // 32 * 32)
@@ -29,7 +34,7 @@ def _some(y, m, n):
     return y[torch.from_numpy(m).to(DEV)][:, torch.from_numpy(n).to(DEV)].double().cpu().numpy()
 
 
-@pytest.mark.parametrize("M,N,K", KINDS)
+@pytest.mark.parametrize("M,N,K", [*KINDS, *FEW])
 def test_whole_numbers_are_exact(M, N, K):
     rng = np.random.default_rng([71, M, N, K])
     p = rng.integers(-30, 31, K // 128)  # powers that differ from block to block and cancel
@@ -68,7 +73,7 @@ def _check(y, x8, w8, M, K):
     assert np.all(err <= tol), (float((err / np.maximum(tol, 1e-300)).max()), np.argwhere(err > tol)[:4].tolist())
 
 
-@pytest.mark.parametrize("M,N,K", KINDS)
+@pytest.mark.parametrize("M,N,K", [*KINDS, *FEW])
 def test_every_cut_and_nothing_else(M, N, K):
     rng = np.random.default_rng([72, M, N, K])
     x8, w8 = _random_rows(rng, M, K), _tiled_weight(rng, N, K)
@@ -77,7 +82,7 @@ def test_every_cut_and_nothing_else(M, N, K):
     _check(_some(y, m, n), tuple(a[m] for a in x8), tuple(a[n] for a in w8), M, K)
 
 
-@pytest.mark.parametrize("M,N,K", KINDS)
+@pytest.mark.parametrize("M,N,K", [*KINDS, *FEW])
 def test_bf16_rows_give_the_bits_of_their_8_bit_rows_in_every_kind(M, N, K):
     rng = np.random.default_rng([73, M, N, K])
     x = rng.standard_normal((M, K)) * np.repeat(np.exp2(rng.integers(-4, 5, (M, K // 128))), 128, 1)
@@ -87,6 +92,7 @@ def test_bf16_rows_give_the_bits_of_their_8_bit_rows_in_every_kind(M, N, K):
     c, s = rows8(M, K)
     ss.subspec_fp8_rows(xd, M, K, c, s)
     y8 = linear(c, s, t, ws, M, N, K).view(torch.int16)
+    assert ss.subspec_fp8_linear_plan(M, N, K)[0] == (KINDS[M, N, K][0] if (M, N, K) in KINDS else 0)
     for _ in range(2):  # codes and partial sums share the workspace
         assert torch.equal(linear(xd, None, t, ws, M, N, K).view(torch.int16), y8)
 

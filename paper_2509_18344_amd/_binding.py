@@ -106,6 +106,9 @@ def load_library():
         "subspec_fp8_linear": (I, [P, P, P, P, I, I, I, P, P]),
         "subspec_fp8_linear_workspace_bytes": (S, [I, I, I, I]),
         "subspec_fp8_linear_plan": (I, [I, I, I, P, P, P, P, P]),
+        "subspec_fp8_linear_exact": (I, [P, P, P, P, I, I, I, P, P]),
+        "subspec_fp8_linear_exact_workspace_bytes": (S, [I, I, I, I]),
+        "subspec_fp8_linear_exact_plan": (I, [I, I, I, P, P, P, P, P]),
         "subspec_prefetch_create": (I, [S, I, ctypes.POINTER(ctypes.c_void_p)]),
         "subspec_prefetch_destroy": (I, [P]),
         "subspec_prefetch_begin": (I, [P, P, S, ctypes.POINTER(ctypes.c_longlong)]),
@@ -533,28 +536,35 @@ def subspec_fp8_pack(codes, N, K, tiles, stream=None) -> int:
     return _check("subspec_fp8_pack", load_library().subspec_fp8_pack(pc, N, K, pt, st))
 
 
-def subspec_fp8_linear(x, x_scales, w, w_scales, M, N, K, y, stream=None) -> int:
-    words, fn = (K + 511) // 512, "subspec_fp8_linear"
-    wk, wn = _scales(w_scales, words * N)
-    if x_scales is None:
-        st, px, pw, pf, py = _all_given(fn, stream, ("bf16", "e4m3", wk, "bf16"), (M * K, N * K, wn, M * N), x, w, w_scales, y)
-        pe = None
-    else:
-        xk, xn = _scales(x_scales, words * M)
-        st, px, pe, pw, pf, py = _all_given(fn, stream, ("e4m3", xk, "e4m3", wk, "bf16"), (M * K, xn, N * K, wn, M * N),
-                                            x, x_scales, w, w_scales, y)
-    return _check(fn, load_library().subspec_fp8_linear(px, pe, pw, pf, M, N, K, py, st))
+def _fp8_linear(fn):
+    def call(x, x_scales, w, w_scales, M, N, K, y, stream=None) -> int:
+        words = (K + 511) // 512
+        wk, wn = _scales(w_scales, words * N)
+        if x_scales is None:
+            st, px, pw, pf, py = _all_given(fn, stream, ("bf16", "e4m3", wk, "bf16"), (M * K, N * K, wn, M * N), x, w, w_scales, y)
+            pe = None
+        else:
+            xk, xn = _scales(x_scales, words * M)
+            st, px, pe, pw, pf, py = _all_given(fn, stream, ("e4m3", xk, "e4m3", wk, "bf16"), (M * K, xn, N * K, wn, M * N),
+                                                x, x_scales, w, w_scales, y)
+        return _check(fn, getattr(load_library(), fn)(px, pe, pw, pf, M, N, K, py, st))
+
+    def workspace_bytes(M, N, K, rows8) -> int:
+        return int(getattr(load_library(), fn + "_workspace_bytes")(M, N, K, int(rows8)))
+
+    def plan(M, N, K):
+        """(kernel, rows, columns, workgroups, sharing) of the launch."""
+        v = [ctypes.c_int() for _ in range(5)]
+        _check(fn + "_plan", getattr(load_library(), fn + "_plan")(M, N, K, *map(ctypes.byref, v)))
+        return tuple(x.value for x in v)
+
+    for f, name in ((call, fn), (workspace_bytes, fn + "_workspace_bytes"), (plan, fn + "_plan")):
+        f.__name__ = f.__qualname__ = name
+    return call, workspace_bytes, plan
 
 
-def subspec_fp8_linear_workspace_bytes(M, N, K, rows8) -> int:
-    return int(load_library().subspec_fp8_linear_workspace_bytes(M, N, K, int(rows8)))
-
-
-def subspec_fp8_linear_plan(M, N, K):
-    """(kernel, rows, columns, workgroups, sharing) of the launch."""
-    v = [ctypes.c_int() for _ in range(5)]
-    _check("subspec_fp8_linear_plan", load_library().subspec_fp8_linear_plan(M, N, K, *map(ctypes.byref, v)))
-    return tuple(x.value for x in v)
+subspec_fp8_linear, subspec_fp8_linear_workspace_bytes, subspec_fp8_linear_plan = _fp8_linear("subspec_fp8_linear")
+subspec_fp8_linear_exact, subspec_fp8_linear_exact_workspace_bytes, subspec_fp8_linear_exact_plan = _fp8_linear("subspec_fp8_linear_exact")
 
 
 class Prefetcher:

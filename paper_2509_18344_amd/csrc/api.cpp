@@ -1480,16 +1480,18 @@ int subspec_fp8_pack(const void* codes, int N, int K, void* tiles, hipStream_t s
   return SUBSPEC_OK;
 }
 
-size_t subspec_fp8_linear_workspace_bytes(int M, int N, int K, int rows8) {
+namespace {
+
+size_t fp8_workspace_bytes(int M, int N, int K, int rows8, bool exact) {
   if (fp8_linear_check(M, N, K) || (rows8 != 0 && rows8 != 1)) return 0;
-  return subspec::fp8_plan(M, N, K, rows8 != 0, device_cus()).workspace_bytes;
+  return subspec::fp8_plan(M, N, K, rows8 != 0, exact, device_cus()).workspace_bytes;
 }
 
-int subspec_fp8_linear_plan(int M, int N, int K, int* kernel, int* rows, int* columns, int* workgroups, int* sharing) {
+int fp8_describe(int M, int N, int K, bool exact, int* kernel, int* rows, int* columns, int* workgroups, int* sharing) {
   if (!kernel || !rows || !columns || !workgroups || !sharing) return fail(SUBSPEC_EINVAL, "null pointer argument");
   const int rc = fp8_linear_check(M, N, K);
   if (rc) return rc;
-  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, true, device_cus());
+  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, true, exact, device_cus());
   *kernel = p.few ? 0 : p.small ? 1 : 2;
   *rows = p.tile_rows;
   *columns = p.tile_columns;
@@ -1498,14 +1500,14 @@ int subspec_fp8_linear_plan(int M, int N, int K, int* kernel, int* rows, int* co
   return SUBSPEC_OK;
 }
 
-int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K,
-                       void* y, hipStream_t stream) {
+int fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K, void* y,
+               bool exact, hipStream_t stream) {
   if (!x || !w || !w_scales || !y) return fail(SUBSPEC_EINVAL, "fp8_linear: null pointer argument");
   if (!aligned16(x) || !aligned16(w) || !aligned16(y) || !aligned_to(x_scales, 4) || !aligned_to(w_scales, 4))
     return fail(SUBSPEC_EINVAL, "fp8_linear: x, w and y must be 16-byte and scales 4-byte aligned");
   int rc = fp8_linear_check(M, N, K);
   if (rc) return rc;
-  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, x_scales != nullptr, device_cus());
+  const subspec::Fp8Plan p = subspec::fp8_plan(M, N, K, x_scales != nullptr, exact, device_cus());
   void* ws = nullptr;
   if (p.workspace_bytes) {
     rc = get_workspace(p.workspace_bytes, stream, &ws);
@@ -1523,6 +1525,27 @@ int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, c
   const hipError_t e = subspec::launch_fp8_linear(p, a, ws, stream);
   if (e != hipSuccess) return hip_fail(e, "fp8_linear launch");
   return SUBSPEC_OK;
+}
+
+}  // namespace
+
+size_t subspec_fp8_linear_workspace_bytes(int M, int N, int K, int rows8) { return fp8_workspace_bytes(M, N, K, rows8, false); }
+size_t subspec_fp8_linear_exact_workspace_bytes(int M, int N, int K, int rows8) { return fp8_workspace_bytes(M, N, K, rows8, true); }
+
+int subspec_fp8_linear_plan(int M, int N, int K, int* kernel, int* rows, int* columns, int* workgroups, int* sharing) {
+  return fp8_describe(M, N, K, false, kernel, rows, columns, workgroups, sharing);
+}
+int subspec_fp8_linear_exact_plan(int M, int N, int K, int* kernel, int* rows, int* columns, int* workgroups, int* sharing) {
+  return fp8_describe(M, N, K, true, kernel, rows, columns, workgroups, sharing);
+}
+
+int subspec_fp8_linear(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K,
+                       void* y, hipStream_t stream) {
+  return fp8_linear(x, x_scales, w, w_scales, M, N, K, y, false, stream);
+}
+int subspec_fp8_linear_exact(const void* x, const uint32_t* x_scales, const void* w, const uint32_t* w_scales, int M, int N, int K,
+                             void* y, hipStream_t stream) {
+  return fp8_linear(x, x_scales, w, w_scales, M, N, K, y, true, stream);
 }
 
 int subspec_tree_plan(int R, int V, int k, int* chunks, int* chunk_len, int* list_len) {

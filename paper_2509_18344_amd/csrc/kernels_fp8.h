@@ -36,7 +36,7 @@ struct Fp8Plan {
   size_t code_bytes;       // x's codes and scales, where the call makes them
   size_t workspace_bytes;  // completion counters, codes and scales, partial sums; 0: none
 };
-Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus);
+Fp8Plan fp8_plan(int M, int N, int K, bool rows8, bool exact, int cus);  // exact: at any number of rows
 hipError_t launch_fp8_linear(const Fp8Plan& p, Fp8Args a, void* workspace, hipStream_t st);
 hipError_t launch_fp8_few(const Fp8Args& a, int columns, int waves, hipStream_t st);
 hipError_t launch_fp8_small(const Fp8Args& a, int kind, hipStream_t st);

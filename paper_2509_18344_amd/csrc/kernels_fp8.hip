@@ -208,12 +208,13 @@ void few_plan(int M, int N, int K, int cus, Fp8Plan* p) {
 
 }  // namespace
 
-Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
+Fp8Plan fp8_plan(int M, int N, int K, bool rows8, bool exact, int cus) {
   Fp8Plan p{};
   const int KB = K / 128;
-  const bool exact = M <= kFp8ExactRows;
+  const bool few = M <= kFp8ExactRows;
+  exact = exact || few;
   size_t parts = 0;
-  if (M <= 16 || (exact && static_cast<long long>(N) * K <= 1 << 21)) {
+  if (M <= 16 || (few && static_cast<long long>(N) * K <= 1 << 21)) {
     few_plan(M, N, K, cus, &p);
     p.tile_rows = 16 * ((M + 15) / 16);
     p.tile_columns = 16 * p.few;
@@ -249,7 +250,7 @@ Fp8Plan fp8_plan(int M, int N, int K, bool rows8, int cus) {
       }
     }
     for (const LargeCost& c : kLarge) {
-      if (c.exact != exact || (exact && c.rows < M)) continue;
+      if (c.exact != exact || (few && c.rows < M)) continue;
       const long long tiles = static_cast<long long>((M + c.rows - 1) / c.rows) * ((N + kColumns - 1) / kColumns);
       const int rounds = static_cast<int>(tiles / cus), left = static_cast<int>(tiles % cus);
       // The tiles left over whole, in as many equal runs each as there are compute units for, or in runs of all

@@ -8,9 +8,9 @@
 // `splits` workgroups where K is long.  bf16 rows become codes on the way: the block's largest magnitude by
 // packed 16-bit maxima, then one conversion for two values, which divides by the power of two too.
 //
-// Measured, of bf16 rows: 1 row, 3584 x 3584 6.1 us (12.8 MB; a launch that does nothing takes 2); 7 rows,
-// 5120 x 27648 29.0 us, 4.9 TB/s of weights, where a copy moves 5.2; 1 row, 37888 x 3584 30 us (26 of 8-bit rows,
-// 5.2 TB/s).
+// Measured in a trace, of bf16 rows: 1 row, 3584 x 3584 6.3 us (12.8 MB; a launch that does nothing takes 2; 6.6 a call in
+// a graph of them, 5.6 of 8-bit rows); 7 rows, 5120 x 27648 29.0 us, 4.9 TB/s of weights, where a copy moves 5.2; 1 row,
+// 37888 x 3584 30 us (26 of 8-bit rows, 5.2 TB/s).
 #include <algorithm>
 
 #include "fp8_device.h"

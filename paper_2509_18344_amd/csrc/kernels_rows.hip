@@ -10,7 +10,8 @@
 // bf16), so a block of 128 is a DPP row of 16 lanes.
 //
 // Measured: norm of 4096 rows of 5120 with the addition 32.3 us, 168 MB at 5.2 TB/s, which is a large copy's rate;
-// activation of 4096 rows of 27648 132 us, 679 MB at 5.1 TB/s; 8-bit rows of 4096 x 5120 14 us, 63 MB at 4.5 TB/s.
+// activation of 4096 rows of 27648 132 us, 679 MB at 5.1 TB/s (112 into 8-bit rows, 567 MB); 8-bit rows of 4096 x 5120
+// 14.8 us and back 14.1, 63 MB at 4.3 and 4.5 TB/s, of 4096 x 27648 67 us and 68, 5.0 TB/s.
 // One row 2.4 us, of which a launch that does nothing is about 2; a call from Python costs 4.2 to 5.9.
 #include "fp8_device.h"
 
@@ -179,7 +180,8 @@ void add_norm_at(const NormArgs& a, hipStream_t st) {
 
 // Few rows: 8 values a thread, so that a row's loads, squares and sums spread widest (49 rows of 3584: 2.93 us,
 // 3.11 with 16 values a thread; of 5120 3.13 and 3.24).  Many: 16, for fewer wavefronts at the sum (4096 rows of 512:
-// 4.4 us, 4.7 with 8; of 3584 18.4 and 18.9).  More where a workgroup of 1024 needs them.
+// 4.4 us, 4.7 with 8; of 3584 18.4 and 18.9).  More where a workgroup of 1024 needs them (64 for rows past 32768, which
+// spill 28 bytes a lane).
 hipError_t launch_add_norm(const NormArgs& a, hipStream_t st) {
   const int n = a.K / 8;
   const bool few = a.M < 512;
